@@ -31,7 +31,8 @@
  * Kernels run asynchronously on `stream` (a hipStream_t; NULL = the default
  * stream), so device-side faults surface at the caller's next synchronisation.
  * ckks_last_error() returns a thread-local description of the last failure.
- * Device pointers must be 16-byte aligned.  Entry points taking a context are
+ * Device pointers must be 16-byte aligned unless stated (int32 lists of a cache
+ * and 4-bit weights: the element).  Entry points taking a context are
  * safe to call concurrently on different streams; outputs must not alias
  * inputs unless stated.
  */
@@ -170,6 +171,51 @@ int ckks_linear_mac_scalar_noalloc(const ckks_ctx* ctx, const uint32_t* w_enc,
                                    const uint32_t* ct_in, uint32_t* ct_out,
                                    uint32_t d_out, uint32_t d_in, uint32_t limbs,
                                    void* stream);
+
+/* ---- Layers over 4-bit weights ---------------------------------------------
+ *
+ * A layer whose weights are 4-bit numbers u in 0..15 with one scale, and
+ * optionally one zero point z, per `group` consecutive inputs of an output:
+ * w[j][i] = scales[j][i / group] (u[j][i] - z[j][i / group]), z = 8 without
+ * zero points.  The plaintext of a weight is (u - z) rint(scales * scale), rint
+ * rounding half to even: the scale is rounded once and the small integer kept,
+ * within 15/2 of the rounding of each product.  Encoded weights take 1/2 byte
+ * and 8 limbs / group bytes (16 limbs / group with zero points) a weight, against 4
+ * limbs bytes for ckks_linear_encode_scalar's, so layers stay resident
+ * (section 4.2) that did not.
+ *
+ * group is a positive multiple of 32 (the last group of a row may be shorter;
+ * one scale a row: d_in rounded up to a multiple of 32). */
+
+/* Bytes of the encoded weights ((size_t)-1 for an invalid request; 0 for an
+ * empty layer).  zeros: 1 with zero points, 0 without. */
+size_t ckks_q4_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs,
+                            int zeros);
+
+/* Encode 4-bit weights for `limbs` limbs.
+ *   w4      device uint8 [d_out][(d_in + 1) / 2]: input 2m of a row in the low
+ *           half of byte m, input 2m + 1 in the high half.
+ *   scales  device fp32 [d_out][ceil(d_in / group)]; |scales * scale| < 2^63 and finite.
+ *   zeros   device uint8 [d_out][ceil(d_in / group)], of which the low four
+ *           bits count, or NULL.
+ *   w_q4    device, ckks_q4_weight_bytes(..., zeros != NULL) bytes, in a layout of
+ *           the library's own; must not overlap the inputs.
+ * w4 and zeros need no alignment, scales 4 bytes.  Run once per layer. */
+int ckks_linear_encode_q4(const ckks_ctx* ctx, const uint8_t* w4, const float* scales, const uint8_t* zeros,
+                          uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, double scale, void* w_q4,
+                          void* stream);
+
+/* ct x pt MAC with 4-bit weights:  ct_out[j][c][l][k] = sum_i (u[j][i] - z)
+ * rint(scales * scale) ct_in[i][c][l][k] mod q_l, as ckks_linear_mac_scalar over
+ * the same plaintexts.
+ *   w_q4    ckks_linear_encode_q4's output for the same d_out, d_in, group,
+ *           limbs and kind (zeros: 1 with zero points, 0 without).
+ *   ct_in   device uint32 [d_in][2][limbs][N];  ct_out [d_out][2][limbs][N], which
+ *           must not overlap ct_in or w_q4 (CKKS_E_INVALID_ARG).
+ * d_out <= 524280 and d_in <= 2^24.  No workspace.  d_out == 0 is a no-op;
+ * d_in == 0 writes zeros. */
+int ckks_linear_mac_q4(const ckks_ctx* ctx, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
+                       uint32_t d_in, uint32_t group, uint32_t limbs, int zeros, void* stream);
 
 /* ct x pt MAC with full-polynomial NTT-form weights (the fallback-encode
  * path of section 4.2): slot-wise
@@ -311,6 +357,101 @@ size_t ckks_bsgs_workspace_bytes(const ckks_ctx* ctx, uint32_t count, uint32_t n
  * must not partially overlap either. */
 int ckks_add(const ckks_ctx* ctx, const uint32_t* ct_a, const uint32_t* ct_b, uint32_t count, uint32_t limbs,
              uint32_t* ct_out, void* stream);
+
+/* ---- Paged cache of ciphertext rows ----------------------------------------
+ *
+ * The encrypted K/V cache of a decoding server (section 4.1's KV backends; about
+ * 1.25 MiB a token and layer, section 6.2): sequences of rows, one row a token
+ * (row_cts ciphertexts, e.g. its K and its V), kept in pages of page_rows rows
+ * that sequences with a common prefix share.  All arrays are the caller's, on
+ * the device; the struct itself is read on the host during a call.  Lengths,
+ * tables and holders are kept up by the kernels, in stream order, so a serving
+ * step needs no copy to the host; calls on one cache must be ordered by
+ * the caller (one stream, or events).
+ *
+ * `seq`, `src`, `dst`, `pos`, `row0`, `keep` are device int32 arrays.  A request
+ * that cannot be served changes nothing and says why in `status` (device int32
+ * [count], or NULL). */
+typedef struct ckks_cache {
+  uint32_t* pool;     /* [pages][page_rows][row_cts][2][limbs][N]                  */
+  int32_t* refs;      /* [pages]: sequences that hold the page; 0: free           */
+  int32_t* table;     /* [seqs][max_pages]: page of each position; -1 past the end */
+  int32_t* lens;      /* [seqs]: rows of the sequence                              */
+  uint32_t pages;     /* <= 2^30                                                   */
+  uint32_t page_rows;
+  uint32_t row_cts;   /* <= 65536                                                  */
+  uint32_t limbs;
+  uint32_t seqs;      /* <= 65536                                                  */
+  uint32_t max_pages; /* pages a sequence can have; max_pages page_rows < 2^31     */
+} ckks_cache;
+
+/* Request status. */
+enum ckks_cache_status {
+  CKKS_CACHE_OK = 0,
+  CKKS_CACHE_BAD_REQUEST = 1, /* a number out of range, or a sequence that the call names in conflict */
+  CKKS_CACHE_TABLE_FULL = 2,  /* more rows than max_pages pages hold */
+  CKKS_CACHE_NO_PAGES = 3     /* the free pages do not suffice for the call: nothing was appended */
+};
+
+/* Calls on a cache that take a workspace (ckks_cache_workspace_bytes). */
+enum ckks_cache_op {
+  CKKS_CACHE_APPEND = 1, /* a = count, b = rows */
+  CKKS_CACHE_COMPACT = 2 /* a, b unused          */
+};
+
+/* Empty cache: no holders, no pages, no rows (the pool is left as it is). */
+int ckks_cache_init(const ckks_ctx* ctx, const ckks_cache* cache, void* stream);
+
+/* Append rows to `count` sequences, each named once (others are bad requests):
+ * request i appends input rows row0[i] .. row0[i+1] - 1, or row i where row0 is
+ * NULL.  Requests get the free pages with the lowest numbers, in request order.
+ * A partly filled last page that other sequences hold too is copied first (its
+ * filled rows); where every holder appends in this call the last request
+ * keeps it in place.  If the free pages do not suffice for all requests that
+ * could be served, none is (CKKS_CACHE_NO_PAGES).
+ *   row0  [count + 1], ascending, at most `rows` (else every request is bad); or NULL.
+ *   rows_in  device uint32 [rows][row_cts][2][limbs][N]; must not overlap the cache.
+ *   workspace  ckks_cache_workspace_bytes(ctx, cache, CKKS_CACHE_APPEND, count, rows)
+ *   bytes, 256-byte aligned.  count <= 65536, rows < 2^31. */
+int ckks_cache_append(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* row0,
+                      uint32_t count, const uint32_t* rows_in, uint32_t rows, int32_t* status, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Fork: sequence dst[i] lets go of what it holds and holds src[i]'s rows, sharing
+ * its pages.  One source may have many targets; a target that two requests
+ * name, or that is also a source, makes those requests bad.  count <= 65536. */
+int ckks_cache_fork(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* src, const int32_t* dst, uint32_t count,
+                    int32_t* status, void* stream);
+
+/* Shorten sequence seq[i] to its first keep[i] rows (keep NULL: to none),
+ * letting go of the pages past them; a longer keep changes nothing, a negative one
+ * counts as 0.  Sequences named twice are bad requests.  count <= 65536. */
+int ckks_cache_free(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* keep, uint32_t count,
+                    int32_t* status, void* stream);
+
+/* Compact the pool: held pages at or past the number of held pages move into the
+ * free pages below it, both in ascending order, and the tables follow; pages
+ * from *live on are free afterwards (weights may take their place).
+ *   live  device int32 [1], the number of held pages; or NULL.
+ *   workspace  ckks_cache_workspace_bytes(ctx, cache, CKKS_CACHE_COMPACT, 0, 0) bytes,
+ *   256-byte aligned. */
+int ckks_cache_compact(const ckks_ctx* ctx, const ckks_cache* cache, int32_t* live, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* rows_out[r] = row pos[r] of sequence seq[r], zeros where there is none.
+ *   rows_out  device uint32 [count][row_cts][2][limbs][N]; must not overlap the cache. */
+int ckks_cache_gather(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* pos,
+                      uint32_t count, uint32_t* rows_out, void* stream);
+
+/* ckks_decrypt of row pos[r] of sequence seq[r] (zeros where there is none), read
+ * through the table: the trusted side's read of the cache before attention.
+ *   s_ntt  device uint32 [limbs][N];  m  device uint32 [count][row_cts][limbs][N],
+ *   which must not overlap the cache or s_ntt. */
+int ckks_cache_decrypt(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* pos,
+                       const uint32_t* s_ntt, uint32_t count, uint32_t* m, void* stream);
+
+/* Workspace of a call on the cache in bytes ((size_t)-1 for an invalid request). */
+size_t ckks_cache_workspace_bytes(const ckks_ctx* ctx, const ckks_cache* cache, int op, uint32_t a, uint32_t b);
 
 /* Workspace size in bytes for `op` (ckks_op) with the given sizes; 0 when
  * none is needed; (size_t)-1 for an invalid request. */

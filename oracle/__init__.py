@@ -22,6 +22,8 @@ the FHE decode cost-breakdown table of section 6.1):
 * ``encode``  -- CKKS canonical-embedding encode/decode by direct O(N^2) sums.
 * ``rlwe``    -- symmetric RLWE encryption / decryption used to make and check
   the encrypted inputs of the end-to-end checks.
+* ``q4``      -- the layer over 4-bit group-scaled weights, as integers.
+* ``cache``   -- the paged cache of ciphertext rows, one row at a time.
 * ``linear``  -- the modular MAC (scalar and full-polynomial weights) by direct
   modular sums, and rescaling by its CRT closed form.
 

@@ -40,11 +40,27 @@ CKKS_OP_RESCALE = 2
 CKKS_OP_ENCODE_POLY = 3
 CKKS_OP_ROTATE = 4
 
+CKKS_CACHE_OK = 0
+CKKS_CACHE_BAD_REQUEST = 1
+CKKS_CACHE_TABLE_FULL = 2
+CKKS_CACHE_NO_PAGES = 3
+
+CKKS_CACHE_APPEND = 1
+CKKS_CACHE_COMPACT = 2
+
 CKKS_MAC_AUTO = 0
 CKKS_MAC_VALU = 1
 CKKS_MAC_MFMA = 2
 
 _u32, _i32, _sz, _vp, _dbl = ctypes.c_uint32, ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_double
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("pool", _vp), ("refs", _vp), ("table", _vp), ("lens", _vp), ("pages", _u32), ("page_rows", _u32),
+                ("row_cts", _u32), ("limbs", _u32), ("seqs", _u32), ("max_pages", _u32)]
+
+
+_cp = ctypes.POINTER(_CacheStruct)
 _SIGS = {
     "ckks_ctx_create": (_i32, [ctypes.POINTER(_vp), _u32, _u32, ctypes.POINTER(_u32), _i32]),
     "ckks_ctx_destroy": (_i32, [_vp]),
@@ -58,6 +74,9 @@ _SIGS = {
     "ckks_linear_encode_poly": (_i32, [_vp, _vp, _u32, _u32, _dbl, _vp, _vp]),
     "ckks_linear_mac_scalar": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp, _sz, _vp]),
     "ckks_linear_mac_scalar_noalloc": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
+    "ckks_q4_weight_bytes": (_sz, [_vp, _u32, _u32, _u32, _u32, _i32]),
+    "ckks_linear_encode_q4": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _dbl, _vp, _vp]),
+    "ckks_linear_mac_q4": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _i32, _vp]),
     "ckks_linear_mac_poly": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "ckks_rescale": (_i32, [_vp, _vp, _vp, _u32, _u32, _vp, _sz, _vp]),
     "ckks_encrypt": (_i32, [_vp, _vp, _vp, _vp, _vp, _u32, _u32, _vp, _vp]),
@@ -69,6 +88,14 @@ _SIGS = {
     "ckks_linear_bsgs": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _vp, _vp, _sz, _vp, _vp]),
     "ckks_bsgs_workspace_bytes": (_sz, [_vp, _u32, _u32, _u32]),
     "ckks_add": (_i32, [_vp, _vp, _vp, _u32, _u32, _vp, _vp]),
+    "ckks_cache_init": (_i32, [_vp, _cp, _vp]),
+    "ckks_cache_append": (_i32, [_vp, _cp, _vp, _vp, _u32, _vp, _u32, _vp, _vp, _sz, _vp]),
+    "ckks_cache_fork": (_i32, [_vp, _cp, _vp, _vp, _u32, _vp, _vp]),
+    "ckks_cache_free": (_i32, [_vp, _cp, _vp, _vp, _u32, _vp, _vp]),
+    "ckks_cache_compact": (_i32, [_vp, _cp, _vp, _vp, _sz, _vp]),
+    "ckks_cache_gather": (_i32, [_vp, _cp, _vp, _vp, _u32, _vp, _vp]),
+    "ckks_cache_decrypt": (_i32, [_vp, _cp, _vp, _vp, _vp, _u32, _vp, _vp]),
+    "ckks_cache_workspace_bytes": (_sz, [_vp, _cp, _i32, _u32, _u32]),
     "ckks_workspace_bytes": (_sz, [_vp, _i32, _u32, _u32, _u32]),
     "ckks_rescaled_scale": (_dbl, [_vp, _dbl, _u32]),
     "ckks_last_error": (ctypes.c_char_p, []),
@@ -320,6 +347,131 @@ def ckks_add(ctx: Context, ct_a, ct_b, count: int, limbs: int, ct_out, stream=No
     nb = count * 2 * limbs * ctx.n * 4
     _check(_lib.ckks_add(ctx.handle, _ptr(ct_a, "ct_a", nb, 4), _ptr(ct_b, "ct_b", nb, 4), count, limbs,
                          _ptr(ct_out, "ct_out", nb, 4), _stream(stream)), "ckks_add")
+
+
+def ckks_q4_weight_bytes(ctx: Context, d_out: int, d_in: int, group: int, limbs: int, zeros: bool = False) -> int:
+    v = _lib.ckks_q4_weight_bytes(ctx.handle, d_out, d_in, group, limbs, int(zeros))
+    if v == ctypes.c_size_t(-1).value:
+        raise ValueError("invalid 4-bit weight request")
+    return int(v)
+
+
+def ckks_linear_encode_q4(ctx: Context, w4, scales, zeros, d_out: int, d_in: int, group: int, limbs: int, scale: float,
+                          w_q4, stream=None) -> None:
+    """zeros may be None (every zero point is 8)."""
+    need = ckks_q4_weight_bytes(ctx, d_out, d_in, group, limbs, zeros is not None)
+    per_row = -(-d_in // group)
+    if scales is not None and scales.dtype.is_floating_point is False:
+        raise ValueError(f"scales must be float32 (got {scales.dtype})")
+    _check(_lib.ckks_linear_encode_q4(
+        ctx.handle, _ptr(w4, "w4", d_out * ((d_in + 1) // 2), 1), _ptr(scales, "scales", d_out * per_row * 4, 4),
+        _ptr(zeros, "zeros", d_out * per_row, 1, True), d_out, d_in, group, limbs, float(scale),
+        _ptr(w_q4, "w_q4", need, w_q4.element_size() if w_q4 is not None else 1), _stream(stream)),
+        "ckks_linear_encode_q4")
+
+
+def ckks_linear_mac_q4(ctx: Context, w_q4, ct_in, ct_out, d_out: int, d_in: int, group: int, limbs: int,
+                       zeros: bool = False, stream=None) -> None:
+    ct_words = 2 * limbs * ctx.n if d_out else 0
+    need = ckks_q4_weight_bytes(ctx, d_out, d_in, group, limbs, zeros)
+    _check(_lib.ckks_linear_mac_q4(
+        ctx.handle, _ptr(w_q4, "w_q4", need, w_q4.element_size() if w_q4 is not None else 1),
+        _ptr(ct_in, "ct_in", d_in * ct_words * 4, 4), _ptr(ct_out, "ct_out", d_out * ct_words * 4, 4),
+        d_out, d_in, group, limbs, int(zeros), _stream(stream)), "ckks_linear_mac_q4")
+
+
+class Cache:
+    """A ckks_cache over tensors of the caller's: pool [pages][page_rows][row_cts][2][limbs][N], refs [pages],
+    table [seqs][max_pages], lens [seqs], all int32.  The tensors are kept alive, not copied."""
+
+    def __init__(self, ctx: Context, pool, refs, table, lens):
+        if pool.dim() != 6 or pool.shape[3] != 2 or pool.shape[5] != ctx.n:
+            raise ValueError(f"pool must be [pages][page_rows][row_cts][2][limbs][{ctx.n}] (got {tuple(pool.shape)})")
+        if table.dim() != 2:
+            raise ValueError("table must be [seqs][max_pages]")
+        self.pages, self.page_rows, self.row_cts, _, self.limbs, self.n = pool.shape
+        self.seqs, self.max_pages = table.shape
+        self.pool, self.refs, self.table, self.lens = pool, refs, table, lens
+        self.row_bytes = self.row_cts * 2 * self.limbs * self.n * 4
+        self.struct = _CacheStruct(
+            _ptr(pool, "pool", self.pages * self.page_rows * self.row_bytes, 4), _ptr(refs, "refs", self.pages * 4, 4),
+            _ptr(table, "table", self.seqs * self.max_pages * 4, 4), _ptr(lens, "lens", self.seqs * 4, 4),
+            self.pages, self.page_rows, self.row_cts, self.limbs, self.seqs, self.max_pages)
+
+    @classmethod
+    def empty(cls, ctx: Context, pages: int, page_rows: int, row_cts: int, limbs: int, seqs: int, max_pages: int,
+              stream=None) -> "Cache":
+        dev = ctx.device
+        c = cls(ctx, empty_u32((pages, page_rows, row_cts, 2, limbs, ctx.n), dev), empty_u32((pages,), dev),
+                empty_u32((seqs, max_pages), dev), empty_u32((seqs,), dev))
+        ckks_cache_init(ctx, c, stream)
+        return c
+
+
+def _status(status, count: int):
+    return _ptr(status, "status", count * 4, 4, True)
+
+
+def _workspace(workspace):
+    if workspace is None:
+        return None, 0
+    return _ptr(workspace, "workspace", 0, workspace.element_size()), workspace.numel() * workspace.element_size()
+
+
+def ckks_cache_workspace_bytes(ctx: Context, cache: Cache, op: int, a: int = 0, b: int = 0) -> int:
+    v = _lib.ckks_cache_workspace_bytes(ctx.handle, ctypes.byref(cache.struct), op, a, b)
+    if v == ctypes.c_size_t(-1).value:
+        raise ValueError("invalid workspace request")
+    return int(v)
+
+
+def ckks_cache_init(ctx: Context, cache: Cache, stream=None) -> None:
+    _check(_lib.ckks_cache_init(ctx.handle, ctypes.byref(cache.struct), _stream(stream)), "ckks_cache_init")
+
+
+def ckks_cache_append(ctx: Context, cache: Cache, seq, row0, rows, workspace, status=None, stream=None) -> None:
+    """rows [n][row_cts][2][limbs][N]; row0 int32 [len(seq) + 1], or None for one row a sequence."""
+    count, n = seq.numel(), rows.shape[0]
+    ws, wb = _workspace(workspace)
+    _check(_lib.ckks_cache_append(
+        ctx.handle, ctypes.byref(cache.struct), _ptr(seq, "seq", count * 4, 4),
+        _ptr(row0, "row0", (count + 1) * 4, 4, True), count, _ptr(rows, "rows", n * cache.row_bytes, 4), n,
+        _status(status, count), ws, wb, _stream(stream)), "ckks_cache_append")
+
+
+def ckks_cache_fork(ctx: Context, cache: Cache, src, dst, status=None, stream=None) -> None:
+    count = dst.numel()
+    _check(_lib.ckks_cache_fork(
+        ctx.handle, ctypes.byref(cache.struct), _ptr(src, "src", count * 4, 4), _ptr(dst, "dst", count * 4, 4), count,
+        _status(status, count), _stream(stream)), "ckks_cache_fork")
+
+
+def ckks_cache_free(ctx: Context, cache: Cache, seq, keep=None, status=None, stream=None) -> None:
+    count = seq.numel()
+    _check(_lib.ckks_cache_free(
+        ctx.handle, ctypes.byref(cache.struct), _ptr(seq, "seq", count * 4, 4), _ptr(keep, "keep", count * 4, 4, True),
+        count, _status(status, count), _stream(stream)), "ckks_cache_free")
+
+
+def ckks_cache_compact(ctx: Context, cache: Cache, live=None, workspace=None, stream=None) -> None:
+    ws, wb = _workspace(workspace)
+    _check(_lib.ckks_cache_compact(ctx.handle, ctypes.byref(cache.struct), _ptr(live, "live", 4, 4, True), ws, wb,
+                                   _stream(stream)), "ckks_cache_compact")
+
+
+def ckks_cache_gather(ctx: Context, cache: Cache, seq, pos, rows, stream=None) -> None:
+    count = seq.numel()
+    _check(_lib.ckks_cache_gather(
+        ctx.handle, ctypes.byref(cache.struct), _ptr(seq, "seq", count * 4, 4), _ptr(pos, "pos", count * 4, 4), count,
+        _ptr(rows, "rows", count * cache.row_bytes, 4), _stream(stream)), "ckks_cache_gather")
+
+
+def ckks_cache_decrypt(ctx: Context, cache: Cache, seq, pos, s_ntt, m, stream=None) -> None:
+    count = seq.numel()
+    _check(_lib.ckks_cache_decrypt(
+        ctx.handle, ctypes.byref(cache.struct), _ptr(seq, "seq", count * 4, 4), _ptr(pos, "pos", count * 4, 4),
+        _ptr(s_ntt, "s_ntt", cache.limbs * ctx.n * 4 if count else 0, 4), count,
+        _ptr(m, "m", count * cache.row_bytes // 2, 4), _stream(stream)), "ckks_cache_decrypt")
 
 
 def empty_workspace(nbytes: int, device: int = 0):

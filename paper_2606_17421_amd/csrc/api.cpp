@@ -7,11 +7,15 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
 #include "ckks_internal.hpp"
 
+static_assert(CKKS_CACHE_OK == ckks::kCacheOk && CKKS_CACHE_BAD_REQUEST == ckks::kCacheBadRequest &&
+                  CKKS_CACHE_TABLE_FULL == ckks::kCacheTableFull && CKKS_CACHE_NO_PAGES == ckks::kCacheNoPages,
+              "request status in the header and the kernels");
 static_assert(CKKS_NOALLOC_SCRATCH_BYTES == ckks::kNoAllocScratchBytes, "scratch size in the header and the library");
 
 struct ckks_ctx {
@@ -195,6 +199,13 @@ int check_limbs(const ckks_ctx* ctx, uint32_t limbs, uint32_t min_limbs) {
 int check_ptr(const void* p, const char* name) {
   if (!p) return fail(CKKS_E_INVALID_ARG, "%s is null", name);
   if (!aligned16(p)) return fail(CKKS_E_INVALID_ARG, "%s is not 16-byte aligned", name);
+  return CKKS_OK;
+}
+
+// A list of 4-byte elements.
+int check_list(const void* p, const char* name) {
+  if (!p) return fail(CKKS_E_INVALID_ARG, "%s is null", name);
+  if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(CKKS_E_INVALID_ARG, "%s is not 4-byte aligned", name);
   return CKKS_OK;
 }
 
@@ -796,6 +807,278 @@ int ckks_add(const ckks_ctx* ctx, const uint32_t* ct_a, const uint32_t* ct_b, ui
   DeviceGuard guard(ctx->device);
   hipError_t he = ckks::launch_ct_add(ctx->t, ct_a, ct_b, count, limbs, ct_out, static_cast<hipStream_t>(stream));
   return he == hipSuccess ? ok() : hip_fail(he, "add launch");
+}
+
+static bool q4_group_ok(uint32_t group) { return group > 0 && group % 32 == 0; }
+
+size_t ckks_q4_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs,
+                            int zeros) {
+  if (!ctx || limbs < 1 || limbs > ctx->L || !q4_group_ok(group) || (zeros != 0 && zeros != 1) ||
+      check_mac_shapes(d_out, d_in) != CKKS_OK)
+    return static_cast<size_t>(-1);
+  return ckks::q4_weight_bytes(d_out, d_in, group, limbs, zeros != 0);
+}
+
+int ckks_linear_encode_q4(const ckks_ctx* ctx, const uint8_t* w4, const float* scales, const uint8_t* zeros,
+                          uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, double scale, void* w_q4,
+                          void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(d_out, d_in)) return rc;
+  if (!q4_group_ok(group)) return fail(CKKS_E_INVALID_ARG, "group=%u is not a positive multiple of 32", group);
+  if (!(scale > 0.0) || !std::isfinite(scale)) return fail(CKKS_E_INVALID_ARG, "scale must be finite and > 0");
+  if (d_out == 0 || d_in == 0) return ok();
+  if (!w4) return fail(CKKS_E_INVALID_ARG, "w4 is null");
+  if (int rc = check_list(scales, "scales")) return rc;
+  if (int rc = check_ptr(w_q4, "w_q4")) return rc;
+  const size_t groups = (size_t(d_in) + group - 1) / group;
+  const size_t out_b = ckks::q4_weight_bytes(d_out, d_in, group, limbs, zeros != nullptr);
+  if (overlaps(w_q4, out_b, w4, size_t(d_out) * ((d_in + 1) / 2)) || overlaps(w_q4, out_b, scales, d_out * groups * 4) ||
+      (zeros && overlaps(w_q4, out_b, zeros, d_out * groups)))
+    return fail(CKKS_E_INVALID_ARG, "w_q4 overlaps an input");
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_encode_q4(ctx->t, w4, scales, zeros, d_out, d_in, group, limbs, scale, w_q4,
+                                        static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "encode_q4 launch");
+}
+
+int ckks_linear_mac_q4(const ckks_ctx* ctx, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
+                       uint32_t d_in, uint32_t group, uint32_t limbs, int zeros, void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(d_out, d_in)) return rc;
+  if (!q4_group_ok(group)) return fail(CKKS_E_INVALID_ARG, "group=%u is not a positive multiple of 32", group);
+  if (zeros != 0 && zeros != 1) return fail(CKKS_E_INVALID_ARG, "zeros must be 0 or 1 (got %d)", zeros);
+  if (d_out == 0) return ok();
+  if (int rc = check_ptr(ct_out, "ct_out")) return rc;
+  const size_t ct_row = size_t(2) * limbs * ctx->n * 4;
+  const size_t out_b = size_t(d_out) * ct_row;
+  DeviceGuard guard(ctx->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d_in == 0) {
+    hipError_t e = ckks::launch_zero(ct_out, size_t(d_out) * 2 * limbs * ctx->n, s);
+    return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
+  }
+  if (int rc = check_ptr(w_q4, "w_q4")) return rc;
+  if (int rc = check_ptr(ct_in, "ct_in")) return rc;
+  if (overlaps(ct_out, out_b, ct_in, size_t(d_in) * ct_row) ||
+      overlaps(ct_out, out_b, w_q4, ckks::q4_weight_bytes(d_out, d_in, group, limbs, zeros != 0)))
+    return fail(CKKS_E_INVALID_ARG, "ct_out overlaps ct_in or w_q4");
+  hipError_t e = ckks::launch_mac_q4(ctx->t, w_q4, ct_in, ct_out, d_out, d_in, group, limbs, zeros != 0, s);
+  return e == hipSuccess ? ok() : hip_fail(e, "mac_q4 launch");
+}
+
+// ---- paged cache ------------------------------------------------------------
+
+namespace {
+
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* name;
+};
+
+// The cache as the kernels see it, or why it is no cache.
+int check_cache(const ckks_ctx* ctx, const ckks_cache* k, ckks::Cache* out) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (!k) return fail(CKKS_E_INVALID_ARG, "null cache");
+  if (int rc = check_limbs(ctx, k->limbs, 1)) return rc;
+  if (k->pages < 1 || k->pages > (1u << 30) || k->page_rows < 1 || k->row_cts < 1 || k->row_cts > 65536 || k->seqs < 1 ||
+      k->seqs > ckks::kCacheMaxSeqs || k->max_pages < 1 || uint64_t(k->max_pages) * k->page_rows > 0x7FFFFFFFull)
+    return fail(CKKS_E_INVALID_ARG, "bad cache sizes (pages=%u, page_rows=%u, row_cts=%u, seqs=%u, max_pages=%u)", k->pages,
+                k->page_rows, k->row_cts, k->seqs, k->max_pages);
+  out->row_words = size_t(k->row_cts) * 2 * k->limbs * ctx->n;
+  if (out->row_words * k->page_rows > (size_t(1) << 60) / k->pages)
+    return fail(CKKS_E_INVALID_ARG, "cache pool too large");
+  if (int rc = check_ptr(k->pool, "pool")) return rc;
+  if (int rc = check_list(k->refs, "refs")) return rc;
+  if (int rc = check_list(k->table, "table")) return rc;
+  if (int rc = check_list(k->lens, "lens")) return rc;
+  out->pool = k->pool;
+  out->refs = k->refs;
+  out->table = k->table;
+  out->lens = k->lens;
+  out->pages = k->pages;
+  out->page_rows = k->page_rows;
+  out->row_cts = k->row_cts;
+  out->limbs = k->limbs;
+  out->seqs = k->seqs;
+  out->max_pages = k->max_pages;
+  return CKKS_OK;
+}
+
+// Nothing that a call writes shares bytes with the cache's arrays, another
+// output or an input.
+int check_apart(const ckks::Cache& c, std::initializer_list<Span> writes, std::initializer_list<Span> reads) {
+  const Span own[] = {{c.pool, c.row_words * c.page_rows * c.pages * 4, "pool"},
+                      {c.refs, size_t(c.pages) * 4, "refs"},
+                      {c.table, size_t(c.seqs) * c.max_pages * 4, "table"},
+                      {c.lens, size_t(c.seqs) * 4, "lens"}};
+  auto clash = [](const Span& a, const Span& b) { return a.p && b.p && a.bytes && b.bytes && overlaps(a.p, a.bytes, b.p, b.bytes); };
+  auto told = [](const Span& a, const Span& b) { return fail(CKKS_E_INVALID_ARG, "%s overlaps %s", a.name, b.name); };
+  for (size_t i = 0; i < 4; ++i) {
+    for (size_t j = i + 1; j < 4; ++j)
+      if (clash(own[i], own[j])) return told(own[i], own[j]);
+    for (const Span& w : writes)
+      if (clash(w, own[i])) return told(w, own[i]);
+    for (const Span& r : reads)
+      if (clash(r, own[i])) return told(r, own[i]);
+  }
+  for (auto w = writes.begin(); w != writes.end(); ++w) {
+    for (auto v = w + 1; v != writes.end(); ++v)
+      if (clash(*w, *v)) return told(*w, *v);
+    for (const Span& r : reads)
+      if (clash(*w, r)) return told(*w, r);
+  }
+  return CKKS_OK;
+}
+
+int check_count(uint32_t count) {
+  return count <= ckks::kCacheMaxSeqs ? CKKS_OK
+                                      : fail(CKKS_E_INVALID_ARG, "count=%u too large (max %u)", count, ckks::kCacheMaxSeqs);
+}
+
+int check_status(const int32_t* status) {
+  return reinterpret_cast<uintptr_t>(status) & 3 ? fail(CKKS_E_INVALID_ARG, "status is not 4-byte aligned") : CKKS_OK;
+}
+
+int check_workspace(const void* p, size_t have, size_t need) {
+  if (!p || have < need) return fail(CKKS_E_WORKSPACE, "cache workspace %zu bytes < %zu required", have, need);
+  if (reinterpret_cast<uintptr_t>(p) & 255) return fail(CKKS_E_INVALID_ARG, "workspace is not 256-byte aligned");
+  return CKKS_OK;
+}
+
+}  // namespace
+
+int ckks_cache_init(const ckks_ctx* ctx, const ckks_cache* cache, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (int rc = check_apart(c, {}, {})) return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_init(c, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_init launch");
+}
+
+int ckks_cache_append(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* row0,
+                      uint32_t count, const uint32_t* rows_in, uint32_t rows, int32_t* status, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (int rc = check_count(count)) return rc;
+  if (rows > 0x7FFFFFFFu) return fail(CKKS_E_INVALID_ARG, "rows=%u too large", rows);
+  if (count == 0) return ok();
+  if (int rc = check_list(seq, "seq")) return rc;
+  if (row0)
+    if (int rc = check_list(row0, "row0")) return rc;
+  if (rows > 0)
+    if (int rc = check_ptr(rows_in, "rows_in")) return rc;
+  if (int rc = check_status(status)) return rc;
+  const size_t need = ckks::cache_workspace_bytes(c, true, count, rows);
+  if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
+  if (int rc = check_apart(c, {{workspace, need, "workspace"}, {status, size_t(count) * 4, "status"}},
+                           {{seq, size_t(count) * 4, "seq"},
+                            {row0, (size_t(count) + 1) * 4, "row0"},
+                            {rows_in, rows * c.row_words * 4, "rows_in"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_append(c, seq, row0, count, rows_in, rows, status, workspace, ctx->t.num_cus,
+                                           static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_append launch");
+}
+
+int ckks_cache_fork(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* src, const int32_t* dst, uint32_t count,
+                    int32_t* status, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (int rc = check_count(count)) return rc;
+  if (count == 0) return ok();
+  if (int rc = check_list(src, "src")) return rc;
+  if (int rc = check_list(dst, "dst")) return rc;
+  if (int rc = check_status(status)) return rc;
+  if (int rc = check_apart(c, {{status, size_t(count) * 4, "status"}},
+                           {{src, size_t(count) * 4, "src"}, {dst, size_t(count) * 4, "dst"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_fork(c, src, dst, count, status, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_fork launch");
+}
+
+int ckks_cache_free(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* keep, uint32_t count,
+                    int32_t* status, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (int rc = check_count(count)) return rc;
+  if (count == 0) return ok();
+  if (int rc = check_list(seq, "seq")) return rc;
+  if (keep)
+    if (int rc = check_list(keep, "keep")) return rc;
+  if (int rc = check_status(status)) return rc;
+  if (int rc = check_apart(c, {{status, size_t(count) * 4, "status"}},
+                           {{seq, size_t(count) * 4, "seq"}, {keep, size_t(count) * 4, "keep"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_free(c, seq, keep, count, status, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_free launch");
+}
+
+int ckks_cache_compact(const ckks_ctx* ctx, const ckks_cache* cache, int32_t* live, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (reinterpret_cast<uintptr_t>(live) & 3) return fail(CKKS_E_INVALID_ARG, "live is not 4-byte aligned");
+  const size_t need = ckks::cache_workspace_bytes(c, false, 0, 0);
+  if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
+  if (int rc = check_apart(c, {{workspace, need, "workspace"}, {live, 4, "live"}}, {})) return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_compact(c, live, workspace, ctx->t.num_cus, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_compact launch");
+}
+
+int ckks_cache_gather(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* pos,
+                      uint32_t count, uint32_t* rows_out, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (count == 0) return ok();
+  if (int rc = check_list(seq, "seq")) return rc;
+  if (int rc = check_list(pos, "pos")) return rc;
+  if (int rc = check_ptr(rows_out, "rows_out")) return rc;
+  if (size_t(count) * (c.row_words / 1024) > 0x7FFFFFFFull) return fail(CKKS_E_INVALID_ARG, "count=%u rows too many", count);
+  if (int rc = check_apart(c, {{rows_out, count * c.row_words * 4, "rows_out"}},
+                           {{seq, size_t(count) * 4, "seq"}, {pos, size_t(count) * 4, "pos"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_gather(c, seq, pos, count, rows_out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_gather launch");
+}
+
+int ckks_cache_decrypt(const ckks_ctx* ctx, const ckks_cache* cache, const int32_t* seq, const int32_t* pos,
+                       const uint32_t* s_ntt, uint32_t count, uint32_t* m, void* stream) {
+  ckks::Cache c;
+  if (int rc = check_cache(ctx, cache, &c)) return rc;
+  if (count == 0) return ok();
+  if (int rc = check_list(seq, "seq")) return rc;
+  if (int rc = check_list(pos, "pos")) return rc;
+  if (int rc = check_ptr(s_ntt, "s_ntt")) return rc;
+  if (int rc = check_ptr(m, "m")) return rc;
+  const size_t cts = size_t(count) * c.row_cts;
+  if (cts * c.limbs > 0x7FFFFFFFull / (ctx->log_n == 16 ? 64 : 1))
+    return fail(CKKS_E_INVALID_ARG, "count=%u rows too many", count);
+  if (int rc = check_apart(c, {{m, cts * c.limbs * ctx->n * 4, "m"}},
+                           {{seq, size_t(count) * 4, "seq"},
+                            {pos, size_t(count) * 4, "pos"},
+                            {s_ntt, size_t(c.limbs) * ctx->n * 4, "s_ntt"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_cache_decrypt(ctx->t, c, seq, pos, s_ntt, count, m, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "cache_decrypt launch");
+}
+
+size_t ckks_cache_workspace_bytes(const ckks_ctx* ctx, const ckks_cache* cache, int op, uint32_t a, uint32_t b) {
+  ckks::Cache c;
+  if (check_cache(ctx, cache, &c) != CKKS_OK) return static_cast<size_t>(-1);
+  if (op == CKKS_CACHE_APPEND && a <= ckks::kCacheMaxSeqs && b <= 0x7FFFFFFFu) return ckks::cache_workspace_bytes(c, true, a, b);
+  if (op == CKKS_CACHE_COMPACT) return ckks::cache_workspace_bytes(c, false, 0, 0);
+  return static_cast<size_t>(-1);
 }
 
 size_t ckks_workspace_bytes(const ckks_ctx* ctx, int op, uint32_t a, uint32_t b, uint32_t limbs) {

@@ -47,6 +47,29 @@ struct Tables {
   const double2* dct_tw;       // [M]   exp(-i pi k / (2M))
 };
 
+// A cache of ciphertext rows as the kernels see it (ckks_cache of the public
+// header), with the words of a row.
+constexpr uint32_t kCacheMaxSeqs = 65536;  // an append marks its sequences in LDS
+constexpr int32_t kCacheOk = 0, kCacheBadRequest = 1, kCacheTableFull = 2, kCacheNoPages = 3;
+struct Cache {
+  uint32_t* pool;
+  int32_t* refs;
+  int32_t* table;
+  int32_t* lens;
+  uint32_t pages, page_rows, row_cts, limbs, seqs, max_pages;
+  size_t row_words;
+};
+
+// Row `pos` of sequence `seq`, or null where the sequence holds no such row.
+__device__ __forceinline__ const uint32_t* cache_row(const Cache& c, int32_t seq, int32_t pos) {
+  if (static_cast<uint32_t>(seq) >= c.seqs || pos < 0 || pos >= c.lens[seq]) return nullptr;
+  const uint32_t at = static_cast<uint32_t>(pos) / c.page_rows;
+  if (at >= c.max_pages) return nullptr;
+  const uint32_t page = static_cast<uint32_t>(c.table[static_cast<size_t>(seq) * c.max_pages + at]);
+  if (page >= c.pages) return nullptr;
+  return c.pool + (static_cast<size_t>(page) * c.page_rows + (pos - at * c.page_rows)) * c.row_words;
+}
+
 // ---------------------------------------------------------------------------
 // 30-bit modular arithmetic (q < 2^30, all operands fully reduced unless noted)
 // ---------------------------------------------------------------------------
@@ -160,6 +183,15 @@ hipError_t launch_mac_poly(const Tables& t, const uint32_t* pt, const uint32_t* 
                            uint32_t* ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs,
                            hipStream_t s);
 
+// MAC over 4-bit group-scaled weights (mac_q4.hip).  `group` inputs share a
+// scale: a multiple of 32.  Layout of the encoded weights: mac_q4.hip.
+size_t q4_weight_bytes(uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, bool zeros);
+hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* scales, const uint8_t* zeros,
+                            uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, double scale, void* w_q4,
+                            hipStream_t s);
+hipError_t launch_mac_q4(const Tables& t, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
+                         uint32_t d_in, uint32_t group, uint32_t limbs, bool zeros, hipStream_t s);
+
 size_t rescale_workspace_bytes(const Tables& t, uint32_t count, uint32_t limbs);
 hipError_t launch_rescale(const Tables& t, const uint32_t* ct_in, uint32_t* ct_out, uint32_t count,
                           uint32_t limbs, void* workspace, hipStream_t s);
@@ -173,6 +205,8 @@ hipError_t launch_encrypt(const Tables& t, const uint32_t* pt, const uint32_t* s
                           const int32_t* e, uint32_t count, uint32_t limbs, uint32_t* ct, hipStream_t s);
 hipError_t launch_decrypt(const Tables& t, const uint32_t* ct, const uint32_t* s_ntt, uint32_t count,
                           uint32_t limbs, uint32_t* m, hipStream_t s);
+hipError_t launch_cache_decrypt(const Tables& t, const Cache& c, const int32_t* seq, const int32_t* pos,
+                                const uint32_t* s_ntt, uint32_t count, uint32_t* m, hipStream_t s);
 hipError_t launch_refresh(const Tables& t, const uint32_t* ct_in, uint32_t limbs_in, const uint32_t* s_ntt,
                           const uint32_t* a, const int32_t* e, uint32_t count, uint32_t limbs_out,
                           uint32_t* ct_out, hipStream_t s);
@@ -193,5 +227,19 @@ hipError_t launch_ct_add(const Tables& t, const uint32_t* a, const uint32_t* b, 
                          uint32_t* out, hipStream_t s);
 hipError_t launch_bsgs(const Tables& t, const uint32_t* pt, const uint32_t* ct, uint32_t count, uint32_t n1,
                        uint32_t n2, const uint32_t* ksk, void* workspace, uint32_t* out, hipStream_t s);
+
+// Paged cache (cache.hip).
+size_t cache_workspace_bytes(const Cache& c, bool append, uint32_t count, uint32_t rows);
+hipError_t launch_cache_init(const Cache& c, hipStream_t s);
+hipError_t launch_cache_free(const Cache& c, const int32_t* seq, const int32_t* keep, uint32_t count, int32_t* status,
+                             hipStream_t s);
+hipError_t launch_cache_fork(const Cache& c, const int32_t* src, const int32_t* dst, uint32_t count, int32_t* status,
+                             hipStream_t s);
+hipError_t launch_cache_append(const Cache& c, const int32_t* seq, const int32_t* row0, uint32_t count,
+                               const uint32_t* rows_in, uint32_t rows, int32_t* status, void* workspace,
+                               uint32_t num_cus, hipStream_t s);
+hipError_t launch_cache_compact(const Cache& c, int32_t* live, void* workspace, uint32_t num_cus, hipStream_t s);
+hipError_t launch_cache_gather(const Cache& c, const int32_t* seq, const int32_t* pos, uint32_t count, uint32_t* out,
+                               hipStream_t s);
 
 }  // namespace ckks

@@ -197,6 +197,27 @@ __global__ __launch_bounds__(RefreshPlan<LOGN>::P::T, RefreshPlan<LOGN>::kWavesP
   }
 }
 
+// Where a decryption finds ciphertext c: in one array [count][2][limbs][N], or
+// row by row through the page table of a cache (row c / row_cts of the list,
+// null where the sequence holds no such row; its coefficients are zeros).
+struct PackedSource {
+  static constexpr bool kMayMiss = false;
+  const uint32_t* ct;
+  uint32_t limbs, log_n;
+  __device__ __forceinline__ const uint32_t* at(size_t c) const { return ct + ((c * 2 * limbs) << log_n); }
+};
+struct PagedSource {
+  static constexpr bool kMayMiss = true;
+  Cache cache;
+  const int32_t *seq, *pos;
+  uint32_t limbs, log_n;
+  __device__ __forceinline__ const uint32_t* at(size_t c) const {
+    const uint32_t r = static_cast<uint32_t>(c / cache.row_cts), part = static_cast<uint32_t>(c - size_t(r) * cache.row_cts);
+    const uint32_t* row = cache_row(cache, seq[r], pos[r]);
+    return row ? row + ((static_cast<size_t>(part) * 2 * limbs) << log_n) : nullptr;
+  }
+};
+
 // Two-kernel refresh for N <= 2^15: the same arithmetic as the fused kernel,
 // with each transform in a workgroup of its own and the whole-row plan's
 // occupancy (two workgroups per CU up to 2^14, one at 2^15).
@@ -207,10 +228,10 @@ __global__ __launch_bounds__(RefreshPlan<LOGN>::P::T, RefreshPlan<LOGN>::kWavesP
 //     the value mod q_l plus the fresh error, the forward transform, and
 //     c0 = . - a (.) s written coalesced;
 // c1 = a: rows from 2 on by (2), rows 0 and 1 (the scratch) copied afterwards.
-template <int LOGN>
+template <int LOGN, class Source>
 __global__ __launch_bounds__((WholePlan<LOGN, true>::P::T), (WholePlan<LOGN, true>::kWavesPerSimd)) void dec_intt_kernel(
-    Tables tb, const uint32_t* __restrict__ ct_in, uint32_t limbs_in, const uint32_t* __restrict__ s_ntt,
-    uint32_t limbs_used, uint32_t* __restrict__ out, uint32_t out_gstride) {
+    Tables tb, Source src, const uint32_t* __restrict__ s_ntt, uint32_t limbs_used, uint32_t* __restrict__ out,
+    uint32_t out_gstride) {
   using P = typename WholePlan<LOGN, true>::P;
   constexpr int LOGE = WholePlan<LOGN, true>::LOGE;
   constexpr int N = P::B;
@@ -219,8 +240,17 @@ __global__ __launch_bounds__((WholePlan<LOGN, true>::P::T), (WholePlan<LOGN, tru
   const uint32_t l = blockIdx.x % limbs_used, t = threadIdx.x;
   const uint32_t q = tb.q[l], mu = tb.barrett[l];
   const uint32_t vofs = pos_coalesced<LOGE>(t, 0) * 4;
-  const auto r_c0 = row_rsrc(ct_in + ((c * 2) * limbs_in + l) * N, N);
-  const auto r_c1 = row_rsrc(ct_in + ((c * 2 + 1) * limbs_in + l) * N, N);
+  uint32_t* r = out + (c * out_gstride + l) * N;
+  const uint32_t* ct = src.at(c);
+  if constexpr (Source::kMayMiss) {
+    if (!ct) {
+#pragma unroll
+      for (int j = 0; j < P::E; ++j) r[P::template pos<0>(t, j)] = 0;
+      return;
+    }
+  }
+  const auto r_c0 = row_rsrc(ct + static_cast<size_t>(l) * N, N);
+  const auto r_c1 = row_rsrc(ct + (static_cast<size_t>(src.limbs) + l) * N, N);
   const auto r_s = row_rsrc(s_ntt + static_cast<size_t>(l) * N, N);
   uint32_t v[P::E], xb[P::E], xs[P::E];
 #pragma unroll
@@ -235,7 +265,6 @@ __global__ __launch_bounds__((WholePlan<LOGN, true>::P::T), (WholePlan<LOGN, tru
   const size_t tl = static_cast<size_t>(l) << LOGN;
   inv_block<LOGN, LOGN, LOGE>(v, t, 0, tb.inv + tl, tb.inv_shoup + tl, q, lds);
   const uint32_t ni = tb.ninv[l], nis = tb.ninv_shoup[l];
-  uint32_t* r = out + (c * out_gstride + l) * N;
 #pragma unroll
   for (int j = 0; j < P::E; ++j) r[P::template pos<0>(t, j)] = mul_shoup(v[j], ni, nis, q);
 }
@@ -523,11 +552,12 @@ __global__ __launch_bounds__(1 << (kBlkLogB - kBlkLogE)) void rlwe16_blocks_comb
                          {row_rsrc(c0 + (static_cast<size_t>(limbs) << 16), n), t * 4}, q, mu);
 }
 
-// Inverse block pass of c0 + c1 (.) s, limbs l < limbs_used of ct [count][2][ct_limbs][N],
+// Inverse block pass of c0 + c1 (.) s, limbs l < limbs_used of the source's ciphertexts,
 // into row c * out_gstride + l of `out` (the column pass follows).
+template <class Source>
 __global__ __launch_bounds__(1 << (kBlkLogB - kBlkLogE)) void dec16_blocks_kernel(
-    Tables tb, const uint32_t* __restrict__ ct, uint32_t ct_limbs, const uint32_t* __restrict__ s_ntt,
-    uint32_t limbs_used, uint32_t* __restrict__ out, uint32_t out_gstride) {
+    Tables tb, Source src, const uint32_t* __restrict__ s_ntt, uint32_t limbs_used, uint32_t* __restrict__ out,
+    uint32_t out_gstride) {
   using P = Plan<kBlkLogB, kBlkLogE>;
   __shared__ uint32_t lds[P::lds_words];
   const size_t r = blockIdx.x / kBlocksPerRow;
@@ -536,8 +566,17 @@ __global__ __launch_bounds__(1 << (kBlkLogB - kBlkLogE)) void dec16_blocks_kerne
   const uint32_t l = static_cast<uint32_t>(r % limbs_used);
   const uint32_t q = tb.q[l], mu = tb.barrett[l];
   const size_t boff = static_cast<size_t>(blk) << kBlkLogB, tl = static_cast<size_t>(l) << 16;
-  const uint32_t* c0 = ct + (((c * 2) * ct_limbs + l) << 16) + boff + t;
-  const uint32_t* c1 = c0 + (static_cast<size_t>(ct_limbs) << 16);
+  uint32_t* o = out + ((c * out_gstride + l) << 16) + boff;
+  const uint32_t* ct = src.at(c);
+  if constexpr (Source::kMayMiss) {
+    if (!ct) {
+#pragma unroll
+      for (int j = 0; j < P::E; ++j) __builtin_nontemporal_store(0u, &o[P::template pos<0>(t, j)]);
+      return;
+    }
+  }
+  const uint32_t* c0 = ct + tl + boff + t;
+  const uint32_t* c1 = c0 + (static_cast<size_t>(src.limbs) << 16);
   const uint32_t* sp = s_ntt + tl + boff + t;
   uint32_t v[P::E], x1[P::E], xs[P::E];
 #pragma unroll
@@ -550,7 +589,6 @@ __global__ __launch_bounds__(1 << (kBlkLogB - kBlkLogE)) void dec16_blocks_kerne
   for (int j = 0; j < P::E; ++j) v[j] = add_mod(v[j], mul_mod_barrett(x1[j], xs[j], q, mu), q);
   wave_relayout<kBlkLogB, kBlkLogE, true>(v, t, lds);
   inv_block<16, kBlkLogB, kBlkLogE>(v, t, blk, tb.inv + tl, tb.inv_shoup + tl, q, lds);
-  uint32_t* o = out + ((c * out_gstride + l) << 16) + boff;
 #pragma unroll
   for (int j = 0; j < P::E; ++j) __builtin_nontemporal_store(v[j], &o[P::template pos<0>(t, j)]);
 }
@@ -563,11 +601,30 @@ hipError_t launch_encrypt_whole(const Tables& t, const uint32_t* pt, const uint3
   return hipGetLastError();
 }
 
-template <int LOGN>
-hipError_t launch_decrypt_whole(const Tables& t, const uint32_t* ct, const uint32_t* s_ntt, uint32_t count,
-                                uint32_t limbs, uint32_t* m, hipStream_t s) {
-  dec_intt_kernel<LOGN><<<count * limbs, WholePlan<LOGN, true>::P::T, 0, s>>>(t, ct, limbs, s_ntt, limbs, m, limbs);
+template <int LOGN, class Source>
+hipError_t launch_decrypt_whole(const Tables& t, const Source& src, const uint32_t* s_ntt, uint32_t count, uint32_t* m,
+                                hipStream_t s) {
+  dec_intt_kernel<LOGN><<<count * src.limbs, WholePlan<LOGN, true>::P::T, 0, s>>>(t, src, s_ntt, src.limbs, m,
+                                                                                 src.limbs);
   return hipGetLastError();
+}
+
+// Every limb of the source's first `count` ciphertexts.
+template <class Source>
+hipError_t decrypt_source(const Tables& t, const Source& src, const uint32_t* s_ntt, uint32_t count, uint32_t* m,
+                          hipStream_t s) {
+  switch (t.log_n) {
+    case 10: return launch_decrypt_whole<10>(t, src, s_ntt, count, m, s);
+    case 11: return launch_decrypt_whole<11>(t, src, s_ntt, count, m, s);
+    case 12: return launch_decrypt_whole<12>(t, src, s_ntt, count, m, s);
+    case 13: return launch_decrypt_whole<13>(t, src, s_ntt, count, m, s);
+    case 14: return launch_decrypt_whole<14>(t, src, s_ntt, count, m, s);
+    case 15: return launch_decrypt_whole<15>(t, src, s_ntt, count, m, s);
+    default: break;
+  }
+  dec16_blocks_kernel<<<count * src.limbs * kBlocksPerRow, 1 << (kBlkLogB - kBlkLogE), 0, s>>>(t, src, s_ntt, src.limbs,
+                                                                                              m, src.limbs);
+  return launch_ntt16_cols(t, m, static_cast<size_t>(count) * src.limbs, src.limbs, true, s, src.limbs);
 }
 
 template <int LOGN>
@@ -576,7 +633,7 @@ hipError_t launch_refresh_two(const Tables& t, const uint32_t* ct_in, uint32_t l
                               uint32_t* ct_out, hipStream_t s) {
   constexpr uint32_t T = WholePlan<LOGN, true>::P::T;
   dec_intt_kernel<LOGN><<<dim3(2 * count), T, 0, s>>>(
-      t, ct_in, limbs_in, s_ntt, 2, ct_out + static_cast<size_t>(limbs_out) * t.n, 2 * limbs_out);
+      t, PackedSource{ct_in, limbs_in, t.log_n}, s_ntt, 2, ct_out + static_cast<size_t>(limbs_out) * t.n, 2 * limbs_out);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   dte_lift_ntt_kernel<LOGN><<<dim3(count * limbs_out), T, 0, s>>>(t, e, s_ntt, a, limbs_out, ct_out);
@@ -618,18 +675,12 @@ hipError_t launch_encrypt(const Tables& t, const uint32_t* pt, const uint32_t* s
 
 hipError_t launch_decrypt(const Tables& t, const uint32_t* ct, const uint32_t* s_ntt, uint32_t count,
                           uint32_t limbs, uint32_t* m, hipStream_t s) {
-  switch (t.log_n) {
-    case 10: return launch_decrypt_whole<10>(t, ct, s_ntt, count, limbs, m, s);
-    case 11: return launch_decrypt_whole<11>(t, ct, s_ntt, count, limbs, m, s);
-    case 12: return launch_decrypt_whole<12>(t, ct, s_ntt, count, limbs, m, s);
-    case 13: return launch_decrypt_whole<13>(t, ct, s_ntt, count, limbs, m, s);
-    case 14: return launch_decrypt_whole<14>(t, ct, s_ntt, count, limbs, m, s);
-    case 15: return launch_decrypt_whole<15>(t, ct, s_ntt, count, limbs, m, s);
-    default: break;
-  }
-  dec16_blocks_kernel<<<count * limbs * kBlocksPerRow, 1 << (kBlkLogB - kBlkLogE), 0, s>>>(t, ct, limbs, s_ntt, limbs, m,
-                                                                                          limbs);
-  return launch_ntt16_cols(t, m, static_cast<size_t>(count) * limbs, limbs, true, s, limbs);
+  return decrypt_source(t, PackedSource{ct, limbs, t.log_n}, s_ntt, count, m, s);
+}
+
+hipError_t launch_cache_decrypt(const Tables& t, const Cache& c, const int32_t* seq, const int32_t* pos,
+                                const uint32_t* s_ntt, uint32_t count, uint32_t* m, hipStream_t s) {
+  return decrypt_source(t, PagedSource{c, seq, pos, c.limbs, t.log_n}, s_ntt, count * c.row_cts, m, s);
 }
 
 hipError_t launch_refresh(const Tables& t, const uint32_t* ct_in, uint32_t limbs_in, const uint32_t* s_ntt,
@@ -668,8 +719,8 @@ hipError_t launch_refresh(const Tables& t, const uint32_t* ct_in, uint32_t limbs
   // which writes every c1 row.
   const uint32_t gs = 2 * limbs_out;
   uint32_t* dec = ct_out + static_cast<size_t>(limbs_out) * t.n;
-  dec16_blocks_kernel<<<count * 2 * kBlocksPerRow, 1 << (kBlkLogB - kBlkLogE), 0, s>>>(t, ct_in, limbs_in, s_ntt, 2, dec,
-                                                                                      gs);
+  dec16_blocks_kernel<<<count * 2 * kBlocksPerRow, 1 << (kBlkLogB - kBlkLogE), 0, s>>>(
+      t, PackedSource{ct_in, limbs_in, t.log_n}, s_ntt, 2, dec, gs);
   hipError_t err = launch_ntt16_cols(t, dec, static_cast<size_t>(count) * 2, 2, true, s, gs);
   if (err != hipSuccess) return err;
   const size_t quads = static_cast<size_t>(count) * (t.n / 4);

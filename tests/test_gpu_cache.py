@@ -1,0 +1,385 @@
+"""GPU parity of the paged ciphertext cache against the oracle: random runs of
+all calls with every array compared after each, the refusals of requests, page
+exhaustion, copy-on-write, rows that are not there, tables that hold nonsense,
+offsets past 32 bits, streams and graphs.  Rows are copied, so there is no
+tolerance."""
+import numpy as np
+import pytest
+
+from oracle import cache as OC
+from oracle import rlwe as OR
+from workloads import gen
+
+gpu = pytest.mark.gpu
+
+_CTX = {}
+
+
+def ctx_for(ck, log_n, limbs):
+    key = (log_n, limbs)
+    if key not in _CTX:
+        _CTX[key] = ck.Context(log_n, limbs)
+    return _CTX[key]
+
+
+def ints(ck, v):
+    import torch
+    return torch.tensor(np.asarray(v, np.int32), device="cuda")
+
+
+class Pair:
+    """The library's cache and the oracle's, given the same calls."""
+
+    def __init__(self, ck, ctx, pages, page_rows, row_cts, limbs, seqs, max_pages):
+        self.ck, self.ctx = ck, ctx
+        self.dev = ck.Cache.empty(ctx, pages, page_rows, row_cts, limbs, seqs, max_pages)
+        self.dev.pool.zero_()
+        self.ref = OC.Cache(pages, page_rows, (row_cts, 2, limbs, ctx.n), seqs, max_pages)
+
+    def status(self, count):
+        s = self.ck.empty_u32((count,))
+        s.fill_(-7)
+        return s
+
+    def append(self, seq, rows, row0=None):
+        ck = self.ck
+        st = self.status(len(seq))
+        ws = ck.empty_workspace(ck.ckks_cache_workspace_bytes(self.ctx, self.dev, ck.CKKS_CACHE_APPEND, len(seq), len(rows)))
+        ws.fill_(-1)
+        ck.ckks_cache_append(self.ctx, self.dev, ints(ck, seq), None if row0 is None else ints(ck, row0), ck.to_device(rows),
+                             ws, st)
+        want = self.ref.append(seq, rows, row0)
+        assert st.tolist() == want
+        return want
+
+    def fork(self, src, dst):
+        st = self.status(len(src))
+        self.ck.ckks_cache_fork(self.ctx, self.dev, ints(self.ck, src), ints(self.ck, dst), st)
+        want = self.ref.fork(src, dst)
+        assert st.tolist() == want
+        return want
+
+    def free(self, seq, keep=None):
+        st = self.status(len(seq))
+        self.ck.ckks_cache_free(self.ctx, self.dev, ints(self.ck, seq), None if keep is None else ints(self.ck, keep), st)
+        want = self.ref.free(seq, keep)
+        assert st.tolist() == want
+        return want
+
+    def compact(self):
+        ck = self.ck
+        live = self.status(1)
+        ws = ck.empty_workspace(ck.ckks_cache_workspace_bytes(self.ctx, self.dev, ck.CKKS_CACHE_COMPACT))
+        ws.fill_(-1)
+        ck.ckks_cache_compact(self.ctx, self.dev, live, ws)
+        assert live.item() == self.ref.compact()
+
+    def gather(self, seq, pos):
+        out = self.ck.empty_u32((len(seq),) + tuple(self.dev.pool.shape[2:]))
+        out.fill_(-1)
+        self.ck.ckks_cache_gather(self.ctx, self.dev, ints(self.ck, seq), ints(self.ck, pos), out)
+        want = self.ref.gather(seq, pos)
+        assert np.array_equal(self.ck.to_host_u32(out), want)
+        return want
+
+    def same(self):
+        assert self.dev.lens.tolist() == self.ref.lens.tolist()
+        assert self.dev.refs.tolist() == self.ref.refs.tolist()
+        assert np.array_equal(self.dev.table.cpu().numpy(), self.ref.table)
+        assert np.array_equal(self.ck.to_host_u32(self.dev.pool), self.ref.pool)
+
+
+def some_rows(rng, count, row_cts, limbs, n):
+    return rng.integers(0, 1 << 30, (count, row_cts, 2, limbs, n), dtype=np.uint32)
+
+
+@gpu
+@pytest.mark.parametrize("page_rows,row_cts,limbs", [(1, 1, 1), (3, 2, 1), (4, 1, 2), (5, 3, 3)])
+def test_random_runs(gpu_lib, page_rows, row_cts, limbs):
+    rng = np.random.default_rng(page_rows)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 14, page_rows, row_cts, limbs, 7, 4)
+    seen = set()
+    for _ in range(120):
+        do = max(0, rng.integers(-2, 5))
+        if do == 0:
+            seq = rng.integers(-1, 8, rng.integers(1, 4)).tolist()
+            row0 = np.concatenate([[0], np.cumsum(rng.integers(0, 5, len(seq)))])
+            if rng.integers(4) == 0:
+                row0 = None
+            rows = some_rows(rng, len(seq) - rng.integers(2) if row0 is None else int(row0[-1]), row_cts, limbs, 1024)
+            seen.update(p.append(seq, rows, row0))
+        elif do == 1:
+            seen.update(p.fork(rng.integers(-1, 8, 3).tolist(), rng.integers(-1, 8, 3).tolist()))
+        elif do == 2:
+            keep = rng.integers(-2, 12, 2).tolist() if rng.integers(2) else None
+            seen.update(p.free(rng.integers(-1, 8, 2).tolist(), keep))
+        elif do == 3:
+            p.compact()
+        else:
+            p.gather(rng.integers(-1, 8, 9).tolist(), rng.integers(-2, 12, 9).tolist())
+        p.same()
+    assert {0, 1} <= seen   # served and bad requests; exhaustion and full tables have a test of their own
+
+
+@gpu
+@pytest.mark.parametrize("holders", [2, 3, 70])
+@pytest.mark.parametrize("everyone", [True, False])
+def test_copy_on_write_of_one_page(gpu_lib, holders, everyone):
+    """Many holders of one partly filled page append at once: all copy it, or, where no other
+    holder is left, the last request keeps it."""
+    rng = np.random.default_rng(holders)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), holders + 3, 4, 1, 1, holders + 1, 3)
+    p.append([0], some_rows(rng, 3, 1, 1, 1024), [0, 3])
+    p.fork([0] * (holders - 1), list(range(1, holders)))
+    who = rng.permutation(holders if everyone else holders - 1).tolist()
+    assert set(p.append(who, some_rows(rng, len(who), 1, 1, 1024))) == {0}
+    p.same()
+    p.gather(list(range(holders)) * 5, sum([[k] * holders for k in range(5)], []))
+
+
+@gpu
+def test_many_requests(gpu_lib):
+    """More requests and pages than one workgroup has threads, ragged counts with zeros among them."""
+    rng = np.random.default_rng(9)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 2600, 2, 1, 1, 2100, 4)
+    p.append(list(range(1500)), some_rows(rng, 1500, 1, 1, 1024))
+    p.fork(list(range(600)), list(range(1500, 2100)))
+    p.free(rng.permutation(1500)[:700].tolist() + [3, 3])
+    counts = rng.integers(0, 3, 1300)
+    row0 = np.concatenate([[0], np.cumsum(counts)])
+    p.append(rng.permutation(2100)[:1300].tolist(), some_rows(rng, int(row0[-1]), 1, 1, 1024), row0)
+    p.same()
+    p.compact()
+    p.same()
+
+
+@gpu
+def test_row0_out_of_order_serves_nobody(gpu_lib):
+    rng = np.random.default_rng(10)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 8, 2, 1, 1, 4, 4)
+    rows = some_rows(rng, 6, 1, 1, 1024)
+    for row0 in ([0, 3, 2, 6], [-1, 0, 1, 2], [0, 2, 4, 7]):
+        assert p.append([0, 1, 2], rows, row0) == [OC.BAD_REQUEST] * 3
+        p.same()
+
+
+@gpu
+def test_exhaustion_changes_nothing_and_a_full_table_is_passed_over(gpu_lib):
+    rng = np.random.default_rng(11)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 3, 2, 1, 1, 4, 2)
+    assert p.append([0, 1], some_rows(rng, 7, 1, 1, 1024), [0, 2, 7]) == [OC.OK, OC.TABLE_FULL]
+    assert p.append([1, 2], some_rows(rng, 7, 1, 1, 1024), [0, 3, 7]) == [OC.NO_PAGES] * 2
+    p.same()
+    assert p.append([1, 0], some_rows(rng, 4, 1, 1, 1024), [0, 4, 4]) == [OC.OK] * 2   # the last two pages, and no row
+    assert p.append([3], some_rows(rng, 1, 1, 1, 1024)) == [OC.NO_PAGES]
+    p.free([0])
+    assert p.append([3], some_rows(rng, 1, 1, 1, 1024)) == [OC.OK]
+    p.same()
+
+
+@gpu
+@pytest.mark.parametrize("held", [0, 1, 6])
+def test_compact_with_nothing_to_move(gpu_lib, held):
+    rng = np.random.default_rng(12)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 6, 1, 1, 1, 6, 2)
+    if held:
+        p.append(list(range(held)), some_rows(rng, held, 1, 1, 1024))
+    p.compact()
+    p.same()
+
+
+@gpu
+@pytest.mark.parametrize("log_n,limbs,row_cts", [(10, 3, 2), (12, 2, 1), (13, 2, 3), (14, 1, 1), (15, 2, 1), (16, 2, 2)])
+def test_decrypt_through_the_table(gpu_lib, log_n, limbs, row_cts):
+    """Rows of encryptions come back as the residues that the oracle decrypts; rows that are not
+    there as zeros; and the packed decryption of the gathered rows agrees."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, log_n, limbs)
+    qs, n = ctx.moduli, ctx.n
+    rng = np.random.default_rng(600 + log_n)
+    s = gen.ternary_secret(rng, n)
+    s_ntt = ck.to_device(np.stack([np.mod(s, q) for q in qs]).astype(np.uint32))
+    ck.ckks_ntt(ctx, s_ntt, 1, limbs)
+    p = Pair(ck, ctx, 6, 2, row_cts, limbs, 3, 3)
+    rows = np.stack([gen.uniform_residues(rng, (row_cts, 2), qs, n) for _ in range(5)])
+    p.append([1, 0], rows, [0, 3, 5])
+    seq, pos = [0, 1, 2, 1, 0, 5, 1, 0], [1, 2, 0, 0, 2, 0, 1, -1]
+    m = ck.empty_u32((len(seq), row_cts, limbs, n))
+    m.fill_(-1)
+    ck.ckks_cache_decrypt(ctx, p.dev, ints(ck, seq), ints(ck, pos), s_ntt, m)
+    got = ck.to_host_u32(m)
+    want = p.ref.gather(seq, pos)
+    for r in range(len(seq)):
+        if not want[r].any():
+            assert not got[r].any()
+            continue
+        for k in range(row_cts):
+            assert np.array_equal(got[r, k], OR.decrypt_residues(want[r, k].astype(np.uint64), s, qs, ctx.roots, log_n))
+    flat = ck.empty_u32((len(seq) * row_cts, limbs, n))
+    ck.ckks_decrypt(ctx, ck.to_device(want), s_ntt, len(seq) * row_cts, limbs, flat)
+    assert np.array_equal(ck.to_host_u32(flat).reshape(got.shape), got)
+
+
+@gpu
+def test_a_table_of_nonsense_reads_as_absent(gpu_lib):
+    ck = gpu_lib
+    rng = np.random.default_rng(13)
+    p = Pair(ck, ctx_for(ck, 10, 3), 4, 2, 1, 1, 2, 3)
+    p.append([0], some_rows(rng, 4, 1, 1, 1024), [0, 4])
+    p.dev.table[0, 0] = 4                         # past the pool
+    p.dev.lens[1] = 1 << 30                       # longer than its table
+    out = ck.empty_u32((4, 1, 2, 1, 1024))
+    ck.ckks_cache_gather(p.ctx, p.dev, ints(ck, [0, 0, 1, 1]), ints(ck, [0, 2, 0, 1 << 29]), out)
+    got = ck.to_host_u32(out)
+    assert not got[0].any() and not got[2].any() and not got[3].any()
+    assert np.array_equal(got[1], p.ref.gather([0], [2])[0])
+    ck.ckks_cache_free(p.ctx, p.dev, ints(ck, [0, 1]))
+    assert p.dev.lens.tolist() == [0, 0] and p.dev.refs[:4].sum().item() == 1   # the page whose entry was lost
+
+
+@gpu
+def test_offsets_past_32_bits(gpu_lib):
+    """A pool of 20 GiB whose low pages are held: appended rows, a copied page, gathered and
+    decrypted rows lie past 2^32 words."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 16, 8)
+    cache = ck.Cache.empty(ctx, 640, 2, 4, 8, 4, 3)      # pages of 32 MiB
+    cache.refs[:600] = 1
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randint(0, 1 << 29, (3, 4, 2, 8, ctx.n), generator=g, device="cuda", dtype=torch.int32)
+    ws = ck.empty_workspace(ck.ckks_cache_workspace_bytes(ctx, cache, ck.CKKS_CACHE_APPEND, 2, 3))
+    status = ints(ck, [9, 9])
+    ck.ckks_cache_append(ctx, cache, ints(ck, [0, 1]), ints(ck, [0, 1, 2]), rows[:2], ws, status)
+    ck.ckks_cache_fork(ctx, cache, ints(ck, [0]), ints(ck, [2]))
+    ck.ckks_cache_append(ctx, cache, ints(ck, [2]), None, rows[2:], ws, status[:1])
+    assert status.tolist() == [0, 0]
+    assert cache.table[:, 0].tolist() == [600, 601, 602, -1] and cache.lens.tolist() == [1, 1, 2, 0]
+    out = torch.empty_like(rows)
+    seq, pos = ints(ck, [1, 2, 2]), ints(ck, [0, 0, 1])
+    ck.ckks_cache_gather(ctx, cache, seq, pos, out)
+    assert torch.equal(out, rows[[1, 0, 2]])
+    m, flat = ck.empty_u32((3, 4, 8, ctx.n)), ck.empty_u32((3, 4, 8, ctx.n))
+    s_ntt = rows[0, 0, 0].contiguous()
+    ck.ckks_cache_decrypt(ctx, cache, seq, pos, s_ntt, m)
+    ck.ckks_decrypt(ctx, out, s_ntt, 12, 8, flat)
+    assert torch.equal(m, flat)
+    cache.refs[:597] = 0
+    live = ints(ck, [0])
+    ck.ckks_cache_compact(ctx, cache, live, ck.empty_workspace(ck.ckks_cache_workspace_bytes(ctx, cache, ck.CKKS_CACHE_COMPACT)))
+    assert live.item() == 6 and cache.table[:, 0].tolist() == [3, 4, 5, -1]
+    ck.ckks_cache_gather(ctx, cache, seq, pos, out)
+    assert torch.equal(out, rows[[1, 0, 2]])
+
+
+@gpu
+def test_a_step_on_another_stream_and_in_a_graph(gpu_lib):
+    """Fork, append, decrypt as a graph on a stream of their own, replayed with eager work between:
+    every replay leaves what the eager calls leave."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 3)
+    rng = np.random.default_rng(15)
+    p = Pair(ck, ctx, 16, 4, 2, 2, 6, 4)
+    p.append([0, 1], some_rows(rng, 9, 2, 2, 1024) >> 1, [0, 5, 9])
+    rows = some_rows(rng, 4, 2, 2, 1024) >> 1
+    src, dst, d_rows = ints(ck, [0, 0, 1, 1]), ints(ck, [2, 3, 4, 5]), ck.to_device(rows)
+    seq, pos = ints(ck, [2, 3, 4, 5, 2]), ints(ck, [5, 5, 4, 4, 0])
+    s_ntt = ck.to_device(some_rows(rng, 1, 1, 1, 1024)[0, 0, :2, 0] >> 1)
+    st, m = ints(ck, [9] * 4), ck.empty_u32((5, 2, 2, 1024))
+    ws = ck.empty_workspace(ck.ckks_cache_workspace_bytes(ctx, p.dev, ck.CKKS_CACHE_APPEND, 4, 4))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def step():
+        ck.ckks_cache_fork(ctx, p.dev, src, dst, st, stream=s)
+        ck.ckks_cache_append(ctx, p.dev, dst, None, d_rows, ws, st, stream=s)
+        ck.ckks_cache_decrypt(ctx, p.dev, seq, pos, s_ntt, m, stream=s)
+    step()
+    s.synchronize()
+    p.ref.fork([0, 0, 1, 1], [2, 3, 4, 5])
+    p.ref.append([2, 3, 4, 5], rows)
+    p.same()
+    eager = m.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for _ in range(3):
+        m.fill_(-1)
+        st.fill_(9)
+        ck.ckks_cache_free(ctx, p.dev, ints(ck, [3, 4]))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m, eager) and st.tolist() == [0] * 4
+        p.same()
+    del graph
+
+
+@gpu
+def test_refusals(gpu_lib):
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 3)
+    c = ck.Cache.empty(ctx, 4, 2, 1, 1, 4, 2)
+    rows, seq = ck.empty_u32((2, 1, 2, 1, 1024)), ints(ck, [0, 1])
+    need = ck.ckks_cache_workspace_bytes(ctx, c, ck.CKKS_CACHE_APPEND, 2, 2)
+    ws = ck.empty_workspace(need)
+    bad = ck.CKKS_E_INVALID_ARG
+
+    def code(f, *a, **k):
+        with pytest.raises(ck.CkksError) as e:
+            f(*a, **k)
+        return e.value.code
+    assert code(ck.ckks_cache_append, ctx, c, seq, None, rows, None) == ck.CKKS_E_WORKSPACE
+    assert code(ck.ckks_cache_append, ctx, c, seq, None, rows, ws[: need // 4 - 1]) == ck.CKKS_E_WORKSPACE
+    assert code(ck.ckks_cache_append, ctx, c, seq, None, rows, ck.empty_workspace(need + 4)[1:]) == bad
+    assert code(ck.ckks_cache_append, ctx, c, seq, None, c.pool[0].view(2, 1, 2, 1, 1024), ws) == bad
+    assert "overlaps" in ck.ckks_last_error()
+    assert code(ck.ckks_cache_append, ctx, c, seq, None, rows, ws, c.lens) == bad
+    assert code(ck.ckks_cache_fork, ctx, c, seq, seq + 2, seq) == bad
+    assert code(ck.ckks_cache_free, ctx, c, seq, None, c.table.view(-1)) == bad
+    assert code(ck.ckks_cache_compact, ctx, c, None, None) == ck.CKKS_E_WORKSPACE
+    assert code(ck.ckks_cache_gather, ctx, c, seq, seq, c.pool[0].view(2, 1, 2, 1, 1024)) == bad
+    s_ntt = ck.empty_u32((1, 1024))
+    assert code(ck.ckks_cache_decrypt, ctx, c, seq, seq, s_ntt, c.pool.view(-1)[:2048]) == bad
+    assert code(ck.ckks_cache_decrypt, ctx, c, seq[:1], seq[:1], s_ntt, s_ntt) == bad
+    for f in (lambda: ck.ckks_cache_gather(ctx, c, seq, seq[:1], rows),               # positions missing
+              lambda: ck.ckks_cache_gather(ctx, c, seq, seq, rows[:1]),
+              lambda: ck.ckks_cache_decrypt(ctx, c, seq, seq, s_ntt, s_ntt),
+              lambda: ck.ckks_cache_gather(ctx, c, seq.to(torch.int64), seq, rows),
+              lambda: ck.ckks_cache_workspace_bytes(ctx, c, 3),
+              lambda: ck.Cache(ctx, c.pool.view(4, 2, 1, 2, 1024, 1), c.refs, c.table, c.lens),
+              lambda: ck.Cache(ctx, c.pool, c.refs[:3], c.table, c.lens)):
+        with pytest.raises(ValueError):
+            f()
+    for field, v in (("pages", 0), ("page_rows", 0), ("row_cts", 0), ("limbs", 4), ("limbs", 0), ("seqs", 0),
+                     ("seqs", 65537), ("max_pages", 0), ("max_pages", 1 << 30), ("pool", None), ("refs", None),
+                     ("refs", c.refs.data_ptr() + 2), ("pool", c.pool.data_ptr() + 4), ("lens", c.refs.data_ptr())):
+        was = getattr(c.struct, field)
+        setattr(c.struct, field, v)
+        assert code(ck.ckks_cache_free, ctx, c, seq) == bad, field
+        setattr(c.struct, field, was)
+    none = seq[:0]
+    ck.ckks_cache_append(ctx, c, none, None, rows[:0], None)      # nothing asked, nothing needed
+    ck.ckks_cache_fork(ctx, c, none, none)
+    ck.ckks_cache_free(ctx, c, none)
+    ck.ckks_cache_gather(ctx, c, none, none, rows)
+    ck.ckks_cache_decrypt(ctx, c, none, none, None, rows)
+    assert c.refs.tolist() == [0] * 4 and c.lens.tolist() == [0] * 4
+
+
+def test_null_context_is_rejected_without_a_gpu():
+    import ctypes
+
+    import paper_2606_17421_amd as ck
+    lib = ck._lib
+    bad = ck.CKKS_E_INVALID_ARG
+    assert lib.ckks_cache_init(None, None, None) == bad
+    assert lib.ckks_cache_append(None, None, None, None, 1, None, 1, None, None, 0, None) == bad
+    assert lib.ckks_cache_fork(None, None, None, None, 1, None, None) == bad
+    assert lib.ckks_cache_free(None, None, None, None, 1, None, None) == bad
+    assert lib.ckks_cache_compact(None, None, None, None, 0, None) == bad
+    assert lib.ckks_cache_gather(None, None, None, None, 1, None, None) == bad
+    assert lib.ckks_cache_decrypt(None, None, None, None, None, 1, None, None) == bad
+    assert lib.ckks_cache_workspace_bytes(None, None, 1, 1, 1) == ctypes.c_size_t(-1).value

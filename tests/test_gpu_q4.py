@@ -1,0 +1,267 @@
+"""GPU parity of the layer over 4-bit weights against the oracle, bit for bit
+(residues have one right value, so there is no tolerance): every group kind,
+ragged groups, tiles and steps, one input and one output, zero points, the
+largest sums that valid inputs give, offsets past 32 bits, and the refusals."""
+import numpy as np
+import pytest
+
+from oracle import q4 as OQ
+from workloads import gen
+
+gpu = pytest.mark.gpu
+
+_CTX = {}
+
+
+def ctx_for(ck, log_n, limbs):
+    key = (log_n, limbs)
+    if key not in _CTX:
+        _CTX[key] = ck.Context(log_n, limbs)
+    return _CTX[key]
+
+
+def layer(seed, d_out, d_in, group, zeros):
+    rng = np.random.default_rng(seed)
+    groups = -(-d_in // group)
+    u = rng.integers(0, 16, (d_out, d_in))
+    scales = (rng.normal(0, 0.01, (d_out, groups))).astype(np.float32)
+    z = rng.integers(0, 16, (d_out, groups)).astype(np.uint8) if zeros else None
+    return OQ.pack(u), scales, z
+
+
+def encode(ck, ctx, w4, scales, z, d_out, d_in, group, limbs, scale):
+    need = ck.ckks_q4_weight_bytes(ctx, d_out, d_in, group, limbs, z is not None)
+    enc = ck.empty_workspace(need)
+    enc.fill_(-1)
+    ck.ckks_linear_encode_q4(ctx, ck.to_device(w4), ck.to_device(scales), None if z is None else ck.to_device(z), d_out,
+                             d_in, group, limbs, scale, enc)
+    return enc
+
+
+def run(ck, ctx, w4, scales, z, ct, d_out, group, scale):
+    d_in, _, limbs, n = ct.shape
+    enc = encode(ck, ctx, w4, scales, z, d_out, d_in, group, limbs, scale)
+    out = ck.empty_u32((d_out, 2, limbs, n))
+    out.fill_(-1)
+    ck.ckks_linear_mac_q4(ctx, enc, ck.to_device(ct), out, d_out, d_in, group, limbs, z is not None)
+    return ck.to_host_u32(out)
+
+
+def check(ck, log_n, limbs, d_out, d_in, group, zeros, seed, scale=2.0 ** 26, limbs_used=None, rows=None):
+    ctx = ctx_for(ck, log_n, limbs)
+    used = limbs_used or limbs
+    qs = ctx.moduli[:used]
+    w4, scales, z = layer(seed, d_out, d_in, group, zeros)
+    ct = gen.uniform_residues(np.random.default_rng(seed + 1), (d_in, 2), qs, ctx.n)
+    got = run(ck, ctx, w4, scales, z, ct, d_out, group, scale)
+    rows = list(range(d_out)) if rows is None else rows
+    want = OQ.mac(w4, scales, z, ct, group, scale, qs, rows=rows).astype(np.uint32)
+    assert np.array_equal(got[rows], want)
+    assert np.all(got < np.array(qs, np.uint32)[None, None, :, None])
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 96, 128, 192, 256, 320, 512, 1024])
+def test_groups(gpu_lib, group, zeros):
+    check(gpu_lib, 10, 2, 37, 1100, group, zeros, 100 + group)
+
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("d_in", [1, 2, 31, 32, 33, 63, 65, 127, 129, 255, 257, 1023, 1024, 1025])
+def test_input_counts(gpu_lib, d_in, group):
+    check(gpu_lib, 10, 1, 18, d_in, group, (d_in + group) % 3 == 0, 200 + d_in)
+
+
+@gpu
+@pytest.mark.parametrize("d_out", [1, 15, 16, 17, 63, 64, 65, 128, 130, 257, 513, 600])
+def test_output_counts(gpu_lib, d_out):
+    check(gpu_lib, 10, 2, d_out, 70, 64, d_out % 2 == 1, 300 + d_out)
+
+
+@gpu
+@pytest.mark.parametrize("d_in,group", [(2048, 128), (2049, 64), (3072, 256), (4100, 32), (9000, 128), (2100, 2112)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_deep_contractions(gpu_lib, d_in, group, zeros):
+    check(gpu_lib, 10, 1, 70, d_in, group, zeros, 400 + d_in, rows=[0, 1, 16, 33, 69])
+
+
+@gpu
+@pytest.mark.parametrize("log_n,limbs", [(10, 1), (11, 3), (12, 16), (13, 4), (14, 2), (15, 2), (16, 2)])
+def test_rings(gpu_lib, log_n, limbs):
+    check(gpu_lib, log_n, limbs, 20, 40, 32, log_n % 2 == 0, 500 + log_n)
+
+
+@gpu
+def test_fewer_limbs_than_the_context(gpu_lib):
+    check(gpu_lib, 11, 4, 33, 65, 64, False, 520, limbs_used=2)
+
+
+@gpu
+@pytest.mark.parametrize("group,d_in", [(32, 1024), (64, 1024), (128, 2048), (256, 1024), (256, 1300), (1024, 1024)])
+@pytest.mark.parametrize("residue", [0x3F7F7F7F, 0x3F7F7F80, None])
+@pytest.mark.parametrize("u,z", [(0, None), (15, None), (0, 15), (15, 0)])
+def test_the_largest_sums(gpu_lib, u, z, residue, group, d_in):
+    """Every input at an end of the digits' range (None: q - 1), every weight at an end of its, and a
+    scale of +-8 units, whose sixteenth is the largest centred residue; and scales of 2^61."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 1)
+    q = ctx.moduli[0]
+    groups = -(-d_in // group)
+    ct = np.full((d_in, 2, 1, ctx.n), q - 1 if residue is None else residue, np.uint32)
+    assert ct.max() < q
+    scales = np.empty((4, groups), np.float32)
+    scales[0], scales[1], scales[2], scales[3] = 8, -8, 1.75 * 2.0 ** 61, -(2.0 ** 62)
+    w4 = OQ.pack(np.full((4, d_in), u))
+    zz = None if z is None else np.full((4, groups), z, np.uint8)
+    got = run(ck, ctx, w4, scales, zz, ct, 4, group, 1.0)
+    want = OQ.mac(w4, scales, zz, ct[..., :1], group, 1.0, ctx.moduli).astype(np.uint32)
+    assert np.array_equal(got, np.broadcast_to(want, got.shape))
+
+
+@gpu
+def test_zero_points_count_four_bits(gpu_lib):
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 1)
+    w4, scales, z = layer(530, 16, 64, 32, True)
+    ct = gen.uniform_residues(np.random.default_rng(531), (64, 2), ctx.moduli, ctx.n)
+    a = run(ck, ctx, w4, scales, z, ct, 16, 32, 2.0 ** 26)
+    b = run(ck, ctx, w4, scales, z | 0xA0, ct, 16, 32, 2.0 ** 26)
+    assert np.array_equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("d_out,d_in,group,zeros", [(70, 1100, 128, False), (600, 1030, 64, True)])
+def test_offsets_past_32_bits(gpu_lib, d_out, d_in, group, zeros):
+    """Rows of 4 MiB: the inputs (and the outputs) pass 2^32 bytes; checked on a sample of columns."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 16, 8)
+    w4, scales, z = layer(540, d_out, d_in, group, zeros)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    ct = torch.empty((d_in, 2, 8, ctx.n), dtype=torch.int32, device="cuda")
+    for l, q in enumerate(ctx.moduli):
+        ct[:, :, l] = torch.randint(0, q, (d_in, 2, ctx.n), generator=g, device="cuda", dtype=torch.int32)
+    enc = encode(ck, ctx, w4, scales, z, d_out, d_in, group, 8, 2.0 ** 28)
+    out = ck.empty_u32((d_out, 2, 8, ctx.n))
+    ck.ckks_linear_mac_q4(ctx, enc, ct, out, d_out, d_in, group, 8, zeros)
+    cols = torch.tensor([0, 1, 4097, 32768, 65535], device="cuda")
+    got = out[..., cols].cpu().numpy().view(np.uint32)
+    part = ct[..., cols].cpu().numpy().view(np.uint32)
+    want = OQ.mac(w4, scales, z, part, group, 2.0 ** 28, ctx.moduli).astype(np.uint32)
+    assert np.array_equal(got, want)
+
+
+@gpu
+def test_unaligned_weights_another_stream_and_a_graph(gpu_lib):
+    """4-bit weights and zero points at odd addresses; the calls on a stream of their own; a graph
+    of both, replayed with eager work between, equals the eager result every time."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 11, 2)
+    d_out, d_in, group = 66, 129, 64
+    w4, scales, z = layer(550, d_out, d_in, group, True)
+    ct = gen.uniform_residues(np.random.default_rng(551), (d_in, 2), ctx.moduli, ctx.n)
+    want = OQ.mac(w4, scales, z, ct, group, 2.0 ** 26, ctx.moduli).astype(np.uint32)
+
+    def odd(a):
+        t = torch.empty(a.size + 1, dtype=torch.uint8, device="cuda")[1:].view(a.shape)
+        t.copy_(torch.from_numpy(a))
+        return t
+    d_w4, d_z, d_s, d_ct = odd(w4), odd(z), ck.to_device(scales), ck.to_device(ct)
+    enc = ck.empty_workspace(ck.ckks_q4_weight_bytes(ctx, d_out, d_in, group, 2, True))
+    out = ck.empty_u32((d_out, 2, 2, ctx.n))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def calls():
+        ck.ckks_linear_encode_q4(ctx, d_w4, d_s, d_z, d_out, d_in, group, 2, 2.0 ** 26, enc, stream=s)
+        ck.ckks_linear_mac_q4(ctx, enc, d_ct, out, d_out, d_in, group, 2, True, stream=s)
+    with torch.cuda.stream(s):
+        calls()
+    s.synchronize()
+    assert np.array_equal(ck.to_host_u32(out), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        calls()
+    other = ck.empty_u32((d_out, 2, 2, ctx.n))
+    for _ in range(3):
+        out.fill_(0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(ck.to_host_u32(out), want)
+        ck.ckks_linear_mac_q4(ctx, enc, d_ct, other, d_out, d_in, group, 2, True)
+        torch.cuda.synchronize()
+    assert np.array_equal(ck.to_host_u32(other), want)
+    del graph
+
+
+@gpu
+def test_empty_layers(gpu_lib):
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    out = ck.empty_u32((3, 2, 2, ctx.n))
+    out.fill_(-1)
+    ck.ckks_linear_mac_q4(ctx, None, None, out, 3, 0, 32, 2)
+    assert np.all(ck.to_host_u32(out) == 0)
+    assert ck.ckks_q4_weight_bytes(ctx, 3, 0, 32, 2) == 0
+    out.fill_(7)
+    ck.ckks_linear_mac_q4(ctx, None, None, out, 0, 5, 32, 2)
+    ck.ckks_linear_encode_q4(ctx, None, None, None, 0, 5, 32, 2, 1.0, None)
+    assert np.all(ck.to_host_u32(out) == 7)
+
+
+@gpu
+def test_refusals(gpu_lib):
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    d_out, d_in = 16, 64
+    w4, scales, _ = layer(560, d_out, d_in, 32, False)
+    d_w4, d_s = ck.to_device(w4), ck.to_device(scales)
+    enc = ck.empty_workspace(ck.ckks_q4_weight_bytes(ctx, d_out, d_in, 32, 2))
+    ct, out = ck.empty_u32((d_in, 2, 2, ctx.n)), ck.empty_u32((d_out, 2, 2, ctx.n))
+    for group in (0, 1, 33, 48):
+        with pytest.raises(ValueError):
+            ck.ckks_q4_weight_bytes(ctx, d_out, d_in, group, 2)
+        assert ck._lib.ckks_linear_mac_q4(ctx.handle, enc.data_ptr(), ct.data_ptr(), out.data_ptr(), d_out, d_in, group, 2,
+                                          0, None) == ck.CKKS_E_INVALID_ARG
+        assert "group" in ck.ckks_last_error()
+    for scale in (0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(ck.CkksError) as e:
+            ck.ckks_linear_encode_q4(ctx, d_w4, d_s, None, d_out, d_in, 32, 2, scale, enc)
+        assert e.value.code == ck.CKKS_E_INVALID_ARG
+    raw = ck._lib.ckks_linear_mac_q4
+    at = (enc.data_ptr(), ct.data_ptr(), out.data_ptr())
+    assert raw(ctx.handle, *at, d_out, d_in, 32, 2, 2, None) == ck.CKKS_E_INVALID_ARG       # zeros is 0 or 1
+    assert raw(ctx.handle, *at, d_out, d_in, 32, 3, 0, None) == ck.CKKS_E_INVALID_ARG       # limbs
+    assert raw(ctx.handle, *at, 524281, d_in, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert raw(ctx.handle, *at, d_out, (1 << 24) + 1, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert raw(ctx.handle, None, at[1], at[2], d_out, d_in, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert raw(ctx.handle, at[0] + 4, at[1], at[2], d_out, d_in, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert raw(ctx.handle, at[0], at[1], at[1], d_out, d_in, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert "overlaps" in ck.ckks_last_error()
+    assert raw(ctx.handle, at[0], at[1], at[0], d_out, d_in, 32, 2, 0, None) == ck.CKKS_E_INVALID_ARG
+    with pytest.raises(ValueError):   # half the inputs
+        ck.ckks_linear_mac_q4(ctx, enc, ct[:32], out, d_out, d_in, 32, 2)
+    with pytest.raises(ValueError):   # encoded for fewer outputs
+        ck.ckks_linear_mac_q4(ctx, enc[:4], ct, out, d_out, d_in, 32, 2)
+    with pytest.raises(ValueError):   # scales of whole numbers
+        ck.ckks_linear_encode_q4(ctx, d_w4, d_s.view(torch.int32), None, d_out, d_in, 32, 2, 1.0, enc)
+    with pytest.raises(ValueError):
+        ck.ckks_linear_encode_q4(ctx, d_w4[:, ::2], d_s, None, d_out, d_in // 2, 32, 2, 1.0, enc)
+    whole = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    assert ck._lib.ckks_linear_encode_q4(ctx.handle, whole.data_ptr(), d_s.data_ptr(), None, d_out, d_in, 32, 2, 1.0,
+                                         whole.data_ptr(), None) == ck.CKKS_E_INVALID_ARG
+
+
+def test_null_context_is_rejected_without_a_gpu():
+    import ctypes
+
+    import paper_2606_17421_amd as ck
+    lib = ck._lib
+    assert lib.ckks_linear_mac_q4(None, None, None, None, 1, 1, 32, 1, 0, None) == ck.CKKS_E_INVALID_ARG
+    assert lib.ckks_linear_encode_q4(None, None, None, None, 1, 1, 32, 1, 1.0, None, None) == ck.CKKS_E_INVALID_ARG
+    assert lib.ckks_q4_weight_bytes(None, 1, 1, 32, 1, 0) == ctypes.c_size_t(-1).value
