@@ -22,13 +22,15 @@ constexpr int kStepFrags = 4 * 64;   // 16-byte residue fragments of a step: fou
 constexpr uint32_t kFold = 1024;     // inputs after which the 64-bit sums are reduced
 
 // Encoded weights:
-//   fragments [tile][step][64 lanes] of 8 bytes: the 4-bit v = u - 8 (two's
-//     complement) of row tile*32 + lane%32 and inputs step*32 + 16 (lane/32) + i,
-//     i < 16.  Word d holds i = 8d .. 8d + 7: the low halves of its bytes the
-//     first four, the high halves the last four, so two masks give four bytes
-//     16 v each.  Rows are padded to kWaveRows, steps to whole sub-groups.
+//   fragments [tile][step][64 lanes] of 8 bytes: a 4-bit v of row tile*32 + lane%32
+//     and inputs step*32 + 16 (lane/32) + i, i < 16; v = u - 8 in two's complement,
+//     or u itself with zero points.  Word d holds i = 8d .. 8d + 7: the low halves of
+//     its bytes the first four, the high halves the last four, so two masks give
+//     four bytes 16 v each (8 u with zero points).  Rows are padded to kWaveRows, steps
+//     to whole sub-groups.
 //   scales [limb][tile][sub-group][32 rows] of {sa, sb} (with zero points {sa, sb, nz,
-//     0}): sa = S / 16, sb = 2^16 S / 16 mod q_l, centred; nz = 16 (8 - z).
+//     0}): sa = 2^32 S / 16, sb = 2^48 S / 16 mod q_l (/ 8 with zero points), centred;
+//     nz = -8 z.  The 2^32 is what the closing reduction divides by.
 // A sub-group is what one set of i32 sums covers: 128 or 64 inputs that divide
 // the group, else 32; a group that holds every input is cut freely.
 struct Shape {
@@ -53,7 +55,7 @@ Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, bo
 
 __global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __restrict__ w4, uint32_t d_out,
                                                            uint32_t d_in, uint32_t steps, size_t lanes,
-                                                           uint2* __restrict__ frag) {
+                                                           uint32_t flip, uint2* __restrict__ frag) {
   const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;
   if (idx >= lanes) return;
   const uint32_t lane = idx & 63;
@@ -68,8 +70,8 @@ __global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __rest
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t k = k0 + e;
-      const uint32_t u = row < d_out && k < d_in ? (w[k >> 1] >> (4 * (k & 1))) & 15u : 8u;
-      v |= (u ^ 8u) << (8 * (e & 3) + 4 * (e >> 2));  // u ^ 8 is u - 8 in four bits
+      const uint32_t u = row < d_out && k < d_in ? (w[k >> 1] >> (4 * (k & 1))) & 15u : flip;
+      v |= (u ^ flip) << (8 * (e & 3) + 4 * (e >> 2));  // flip 8: u ^ 8 is u - 8 in four bits
     }
     word[d] = v;
   }
@@ -96,11 +98,10 @@ __global__ __launch_bounds__(kThreads) void q4_scale_kernel(Tables tb, const flo
   if (row < d_out) {
     const size_t at = static_cast<size_t>(row) * groups + static_cast<uint32_t>(static_cast<size_t>(sub) * sub_len / group);
     uint32_t r = reduce_f64_int(rint(static_cast<double>(scales[at]) * scale), q, tb.q_recip[l]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r = (r & 1) ? (r + q) >> 1 : r >> 1;  // r / 16 mod q
+    r = static_cast<uint32_t>((static_cast<uint64_t>(r) << (zeros ? 29 : 28)) % q);  // 2^32 / 8 or 2^32 / 16
     sa = centred(r, q);
     sb = centred(static_cast<uint32_t>((static_cast<uint64_t>(r) << 16) % q), q);
-    if (zeros) nz = 16 * (8 - static_cast<int32_t>(zeros[at] & 15u));
+    if (zeros) nz = -8 * static_cast<int32_t>(zeros[at] & 15u);
   }
   if (zeros)
     reinterpret_cast<int4*>(out)[idx] = make_int4(sa, sb, nz, 0);
@@ -117,17 +118,19 @@ struct Job {
   uint32_t row_bytes, d_out, d_in, steps, subs;
 };
 
-// 8 bytes of a weight fragment -> 16 bytes of 16 v.
+// 8 bytes of a weight fragment -> 16 bytes, 16 v each (8 u with zero points).
+template <bool kZeros>
 __device__ __forceinline__ v4i unpack(uint2 w) {
-  constexpr uint32_t m = 0xf0f0f0f0u;
-  return v4i{static_cast<int>((w.x << 4) & m), static_cast<int>(w.x & m), static_cast<int>((w.y << 4) & m),
-             static_cast<int>(w.y & m)};
+  constexpr uint32_t m = kZeros ? 0x78787878u : 0xf0f0f0f0u;
+  constexpr int up = kZeros ? 3 : 4, down = kZeros ? 1 : 0;
+  return v4i{static_cast<int>((w.x << up) & m), static_cast<int>((w.x >> down) & m), static_cast<int>((w.y << up) & m),
+             static_cast<int>((w.y >> down) & m)};
 }
 
 // The residues of inputs from `first` on, `steps` steps of them, as digit fragments
 // in LDS; inputs past d_in read as zero through the buffer range check.  Thread:
 // one column, 16 consecutive inputs a pass.  With zero points also the
-// sub-groups' sums of the low (balanced) and high 16 bits of the residues.
+// sub-groups' sums of the residues' two low and two high digits.
 template <int kSteps, bool kZeros>
 __device__ __forceinline__ void fill(const Job& job, uint32_t first, uint32_t steps, v4i* lds, int32_t* sums) {
   constexpr int kPasses = 4;
@@ -160,11 +163,12 @@ __device__ __forceinline__ void fill(const Job& job, uint32_t first, uint32_t st
 #pragma unroll
         for (int d = 0; d < 4; ++d) lds[(b >> 1) * kStepFrags + d * 64 + col + 32 * (b & 1)] = f[d];
         if constexpr (kZeros) {
-          int32_t lo = 0, hi = 0;
+          int32_t lo = -16 * 0x8080, hi = 0;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            lo += static_cast<int16_t>(x[p][i]);
-            hi += static_cast<int32_t>((x[p][i] + 0x8000u) >> 16);
+            const uint32_t y = x[p][i] + 0x8080u;
+            lo += static_cast<int32_t>(y & 0xffffu);
+            hi += static_cast<int32_t>(y >> 16);
           }
           const uint32_t sub = (b >> 1) / kSteps;
           atomicAdd(&sums[(sub * 2) * kCols + col], lo);
@@ -175,17 +179,27 @@ __device__ __forceinline__ void fill(const Job& job, uint32_t first, uint32_t st
   }
 }
 
-// T mod q in [0, q) for |T| < 2^62.92: T = hi 2^32 + lo with c32 = 2^32 mod q,
-// centred, gives |t| < 2^59.92 + 2^32, whose quotient estimate from fp64 is
-// within one of the true one and below 2^31 in magnitude (q > 2^29), so the low
-// 32 bits of t - qt q + q in [0, 3q) are exact and two conditional subtractions
-// finish.
-__device__ __forceinline__ uint32_t reduce_i64(int64_t v, uint32_t q, double qr, int32_t c32) {
-  const int64_t t = static_cast<int64_t>(static_cast<int32_t>(v >> 32)) * c32 + static_cast<uint32_t>(v);
-  const int32_t qt = static_cast<int32_t>(floor(static_cast<double>(t) * qr));
-  uint32_t u = static_cast<uint32_t>(t) - static_cast<uint32_t>(qt) * q + q;
-  u = min(u, u - q);
-  return min(u, u - q);
+// T / 2^32 mod q in [0, q) for |T| < 2^61.8 (Montgomery's reduction): with m = T /
+// q mod 2^32 the difference T - m q is a multiple of 2^32, its quotient hi(T) -
+// hi(m q) in (-2^29.8 - q, 2^29.8); 3q (q > 2^29) makes it positive and below 4.74
+// q < 2^32, and three conditional subtractions finish.  A contraction of kFold
+// inputs stays below: |16 v| <= 128 times digit pairs of at most 128 * 257 and 128 +
+// 64 * 256, times centred scales below 2^29, is 2^51.6 an input.
+struct Modulus {
+  uint32_t q, qinv;  // qinv = 1 / q mod 2^32
+};
+__device__ __forceinline__ Modulus modulus(uint32_t q) {
+  uint32_t v = q;  // right mod 2^3 for odd q; each step doubles the bits
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v *= 2u - q * v;
+  return {q, v};
+}
+__device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
+  const uint32_t k = static_cast<uint32_t>(t) * m.qinv;
+  uint32_t u = static_cast<uint32_t>(t >> 32) - __umulhi(k, m.q) + 3 * m.q;
+  u = min(u, u - 2 * m.q);
+  u = min(u, u - m.q);
+  return min(u, u - m.q);
 }
 
 // The wave's 64 rows over the sub-groups [sub0, sub0 + subs), whose residues lie in LDS.
@@ -225,7 +239,7 @@ __device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) w[s][t] = unpack(raw[s][t]);
+      for (int t = 0; t < 2; ++t) w[s][t] = unpack<kZeros>(raw[s][t]);
     const int2 sg[2] = {sc[0], sc[1]};
     const int32_t zg[2] = {nz[0], nz[1]};
     if (g + 1 < subs) load(g + 1);
@@ -288,10 +302,7 @@ __global__ __launch_bounds__(512, 1) void mac_q4_kernel(Tables tb, const uint2* 
   const size_t at = (static_cast<size_t>(c) * limbs + l) * n + k0;
   const Job job = {frag, scales + static_cast<size_t>(l) * tiles * subs * 32 * (kZeros ? 4 : 2), ct_in + at, ct_out + at,
                    2u * limbs * n * 4u, d_out, d_in, steps, subs};
-  const uint32_t q = tb.q[l];
-  const double qr = tb.q_recip[l];
-  const uint32_t p32 = tb.pow256[l * 8 + 4];
-  const int32_t c32 = p32 > (q >> 1) ? static_cast<int32_t>(p32 - q) : static_cast<int32_t>(p32);
+  const Modulus q = modulus(tb.q[l]);
   const uint32_t waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63;
   const uint32_t groups = tiles / 2, each = (groups + splits - 1) / splits;
@@ -318,11 +329,15 @@ __global__ __launch_bounds__(512, 1) void mac_q4_kernel(Tables tb, const uint2* 
         fill<kSteps, kZeros>(job, s0 * kStep, here, lds, sums);
         __syncthreads();
         if (rg < rg1) {
+          if (s0 != 0) {  // the sum so far, reduced, goes on as a product below 2^59
+            const int32_t c32 = centred(tb.pow256[l * 8 + 4], q.q);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                acc[t][r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[t][r], q))) * c32;
+          }
           contract<kSteps, kZeros>(job, rg * 2, s0 / kSteps, here / kSteps, lds, sums, acc);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[t][r] = reduce_i64(acc[t][r], q, qr, c32);
         }
       }
       if (rg >= rg1) continue;
@@ -336,7 +351,7 @@ __global__ __launch_bounds__(512, 1) void mac_q4_kernel(Tables tb, const uint2* 
       for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns; rows past d_out are out of range
         v4i u;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(reduce_i64(acc[t][4 * r4 + r], q, qr, c32));
+        for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(reduce(acc[t][4 * r4 + r], q));
         __builtin_amdgcn_raw_buffer_store_b128(
             u, out, (t * 32 + (lane & 31)) * job.row_bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
       }
@@ -395,7 +410,7 @@ hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* sca
   uint8_t* base = static_cast<uint8_t*>(w_q4);
   const size_t lanes = sh.frag_bytes / 8, total = static_cast<size_t>(limbs) * sh.tiles * sh.subs * 32;
   q4_frag_kernel<<<static_cast<uint32_t>((lanes + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      w4, d_out, d_in, sh.steps, lanes, reinterpret_cast<uint2*>(base));
+      w4, d_out, d_in, sh.steps, lanes, zeros ? 0u : 8u, reinterpret_cast<uint2*>(base));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   q4_scale_kernel<<<static_cast<uint32_t>((total + kThreads - 1) / kThreads), kThreads, 0, s>>>(
