@@ -981,7 +981,7 @@ int ckks_cache_append(const ckks_ctx* ctx, const ckks_cache* cache, const int32_
                             {rows_in, rows * c.row_words * 4, "rows_in"}}))
     return rc;
   DeviceGuard guard(ctx->device);
-  hipError_t e = ckks::launch_cache_append(c, seq, row0, count, rows_in, rows, status, workspace, ctx->t.num_cus,
+  hipError_t e = ckks::launch_cache_append(c, seq, row0, count, rows_in, rows, status, workspace,
                                            static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "cache_append launch");
 }
@@ -1030,7 +1030,7 @@ int ckks_cache_compact(const ckks_ctx* ctx, const ckks_cache* cache, int32_t* li
   if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
   if (int rc = check_apart(c, {{workspace, need, "workspace"}, {live, 4, "live"}}, {})) return rc;
   DeviceGuard guard(ctx->device);
-  hipError_t e = ckks::launch_cache_compact(c, live, workspace, ctx->t.num_cus, static_cast<hipStream_t>(stream));
+  hipError_t e = ckks::launch_cache_compact(c, live, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "cache_compact launch");
 }
 

@@ -237,8 +237,8 @@ hipError_t launch_cache_fork(const Cache& c, const int32_t* src, const int32_t* 
                              hipStream_t s);
 hipError_t launch_cache_append(const Cache& c, const int32_t* seq, const int32_t* row0, uint32_t count,
                                const uint32_t* rows_in, uint32_t rows, int32_t* status, void* workspace,
-                               uint32_t num_cus, hipStream_t s);
-hipError_t launch_cache_compact(const Cache& c, int32_t* live, void* workspace, uint32_t num_cus, hipStream_t s);
+                               hipStream_t s);
+hipError_t launch_cache_compact(const Cache& c, int32_t* live, void* workspace, hipStream_t s);
 hipError_t launch_cache_gather(const Cache& c, const int32_t* seq, const int32_t* pos, uint32_t count, uint32_t* out,
                                hipStream_t s);
 
