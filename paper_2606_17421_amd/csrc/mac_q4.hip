@@ -333,10 +333,15 @@ __device__ __forceinline__ Place place_of(const Tables& tb, const uint2* frag, c
 }
 
 // Inputs that fit the LDS (d_in <= kFold): the workgroup converts its 32 columns once and its
-// waves walk the 64-row groups without further synchronisation.
-constexpr int kWholeWaves = 8, kWholeTiles = 2;
-template <int kSteps, bool kZeros>
-__global__ __launch_bounds__(kWholeWaves * 64, 1) void mac_q4_whole_kernel(
+// waves walk the 64-row groups without further synchronisation.  Eight waves a CU, two a SIMD:
+// one workgroup, or two of four waves where both strips fit the LDS (640 inputs), so that one converts
+// while the other contracts (2^14, 2 limbs, groups of 128, one : two workgroups, us: 128 -> 768
+// 62 : 53, 384 -> 384 70 : 61, 512 -> 512 102 : 90, 384 -> 1536 210 : 200; four waves alone at 768 ->
+// 768 209 against 197).
+constexpr int kWholeTiles = 2;
+constexpr uint32_t kLdsBytes = 160 << 10;
+template <int kSteps, bool kZeros, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
     Tables tb, const uint2* __restrict__ frag, const int32_t* __restrict__ scales, const uint32_t* __restrict__ ct_in,
     uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
     uint32_t tiles, uint32_t splits) {
@@ -349,13 +354,13 @@ __global__ __launch_bounds__(kWholeWaves * 64, 1) void mac_q4_whole_kernel(
   const uint32_t groups = tiles / kWholeTiles, each = (groups + splits - 1) / splits;
   const uint32_t end = min(groups, (at.split + 1) * each);
   constexpr int kPasses = 4;
-  for (uint32_t b0 = 0; b0 < 2 * steps; b0 += kPasses * kWholeWaves * 2) {
+  for (uint32_t b0 = 0; b0 < 2 * steps; b0 += kPasses * kWaves * 2) {
     uint32_t x[kPasses][16];
     fetch<kPasses>(job, 0, b0, 2 * steps, x);
     place<kPasses>(b0, 2 * steps, x, lds);
   }
   __syncthreads();
-  for (uint32_t rg = at.split * each + wave; rg < end; rg += kWholeWaves) {
+  for (uint32_t rg = at.split * each + wave; rg < end; rg += kWaves) {
     int64_t acc[kWholeTiles][16];
     clear<kWholeTiles>(acc);
     contract<kSteps, kZeros, kWholeTiles>(job, rg * kWholeTiles, 0, subs, lds, acc);
@@ -417,11 +422,13 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
   // kernel overlaps the two (2^14, 2 limbs, groups of 128, whole : chunked, us: 1024 -> 128 102 : 93, 256 -> 64
   // 37 : 31, 256 -> 256 43.0 : 42.7, 1024 -> 384 158 : 166, 768 -> 768 196 : 239).
   if (sh.steps * kStep <= kFold && d_out > 256) {
+    const uint32_t strip_bytes = sh.steps * kStepFrags * 16, waves = 2 * strip_bytes <= kLdsBytes ? 4 : 8;
     // Row splits only where the column strips alone leave CUs idle: each split converts the strip again.
-    const uint32_t groups = sh.tiles / kWholeTiles, blocks = (groups + kWholeWaves - 1) / kWholeWaves;
-    const uint32_t want = (t.num_cus + strips - 1) / strips, splits = want < blocks ? want : blocks;
-    mac_q4_whole_kernel<kSteps, kZeros><<<strips * splits, kWholeWaves * 64, size_t(sh.steps) * kStepFrags * 16, s>>>(
-        t, frag, scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs, sh.tiles, splits);
+    const uint32_t groups = sh.tiles / kWholeTiles, blocks = (groups + waves - 1) / waves;
+    const uint32_t want = (t.num_cus * (8 / waves) + strips - 1) / strips, splits = want < blocks ? want : blocks;
+    const auto k = waves == 4 ? mac_q4_whole_kernel<kSteps, kZeros, 4> : mac_q4_whole_kernel<kSteps, kZeros, 8>;
+    k<<<strips * splits, waves * 64, strip_bytes, s>>>(t, frag, scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs,
+                                                      sh.tiles, splits);
   } else {
     const uint32_t splits = (sh.tiles + kDeepWaves - 1) / kDeepWaves;
     mac_q4_deep_kernel<kSteps, kZeros><<<strips * splits, kDeepWaves * 64, 0, s>>>(
