@@ -21,6 +21,8 @@
 // interleaved by hand, fragments read ahead, three or four waves a SIMD with half the
 // rows, 64-byte stores after a transpose over lanes; int8 fragments instead of
 // 4-bit ones gave 4% for twice the memory.
+#include <type_traits>
+
 #include "digits.hpp"
 
 namespace ckks {
@@ -36,16 +38,16 @@ constexpr int kStepFrags = 4 * 64;   // 16-byte residue fragments of a step: fou
 constexpr uint32_t kFold = 1024;     // most inputs between reductions of the 64-bit sums
 
 // Encoded weights:
-//   fragments [tile][step][64 lanes] of 8 bytes: a 4-bit v of row tile*32 + lane%32
-//     and inputs step*32 + 16 (lane/32) + i, i < 16; v = u - 8 in two's complement,
-//     or u itself with zero points.  Word d holds i = 8d .. 8d + 7: the low halves of
-//     its bytes the first four, the high halves the last four, so two masks give
-//     four bytes 16 v each (8 u with zero points).  Rows are padded to kPadRows, steps
-//     to whole sub-groups.
-//   scales [limb][tile][sub-group][32 rows] of {sa, sb} (with zero points {sa, sb, zc,
-//     0}): sa = 2^32 S / 16, sb = 2^48 S / 16 mod q_l (/ 8 with zero points), centred;
-//     zc = -8 z in each of four bytes, as one number.  The 2^32 is what the closing
-//     reduction divides by.
+//   fragments [tile][step][64 lanes] of row tile*32 + lane%32 and inputs step*32 + 16
+//     (lane/32) + i, i < 16; rows are padded to kPadRows, steps to whole sub-groups.
+//     Without zero points 8 bytes: v = u - 8 in four bits, two's complement.  Word d holds i =
+//     8d .. 8d + 7: the low halves of its bytes the first four, the high halves the last four, so
+//     two masks give four bytes 16 v each.
+//     With zero points 16 bytes, 8 (u - z) each: u - z does not fit four bits, and to subtract z
+//     from unpacked bytes takes three operations more a word (3072 -> 768 at 2^14, groups of
+//     64: 1.97 ms with 4-bit u, 1.79 ms so).
+//   scales [limb][tile][sub-group][32 rows] of {sa, sb}: sa = 2^32 S / 16, sb = 2^48 S / 16 mod q_l
+//     (/ 8 with zero points), centred.  The 2^32 is what the closing reduction divides by.
 // A sub-group is what one set of i32 sums covers: 128 or 64 inputs that divide
 // the group, else 32; a group that holds every input is cut freely.
 struct Shape {
@@ -63,34 +65,52 @@ Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, bo
     s.sub_len = group % 128 == 0 ? 128 : group % 64 == 0 ? 64 : 32;
   s.subs = (d_in + s.sub_len - 1) / s.sub_len;
   s.steps = s.subs * (s.sub_len / kStep);
-  s.frag_bytes = static_cast<size_t>(s.tiles) * s.steps * 64 * 8;
-  s.scale_bytes = static_cast<size_t>(limbs) * s.tiles * s.subs * 32 * (zeros ? 16 : 8);
+  s.frag_bytes = static_cast<size_t>(s.tiles) * s.steps * 64 * (zeros ? 16 : 8);
+  s.scale_bytes = static_cast<size_t>(limbs) * s.tiles * s.subs * 32 * 8;
   return s;
 }
 
-__global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __restrict__ w4, uint32_t d_out,
-                                                           uint32_t d_in, uint32_t steps, size_t lanes,
-                                                           uint32_t flip, uint2* __restrict__ frag) {
+// A lane's weight fragment.
+template <bool kZeros>
+using Frag = std::conditional_t<kZeros, v4i, uint2>;
+
+template <bool kZeros>
+__global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __restrict__ w4,
+                                                           const uint8_t* __restrict__ zeros, uint32_t d_out,
+                                                           uint32_t d_in, uint32_t group, uint32_t groups,
+                                                           uint32_t steps, size_t lanes,
+                                                           Frag<kZeros>* __restrict__ frag) {
   const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;
   if (idx >= lanes) return;
   const uint32_t lane = idx & 63;
   const uint32_t step = static_cast<uint32_t>((idx >> 6) % steps), tile = static_cast<uint32_t>((idx >> 6) / steps);
-  const uint32_t row = tile * 32 + (lane & 31);
+  const uint32_t row = tile * 32 + (lane & 31), k0 = step * kStep + 16 * (lane >> 5);
   const uint8_t* w = w4 + static_cast<size_t>(row) * ((d_in + 1) / 2);
-  uint32_t word[2];
+  // past the layer's edges the weight is zero: u = z
+  uint32_t z = 8;
+  if (kZeros && row < d_out && k0 < d_in) z = zeros[static_cast<size_t>(row) * groups + k0 / group] & 15u;
+  auto weight = [&](uint32_t k) { return row < d_out && k < d_in ? (w[k >> 1] >> (4 * (k & 1))) & 15u : z; };
+  if constexpr (kZeros) {
+    v4i f;
 #pragma unroll
-  for (int d = 0; d < 2; ++d) {
-    const uint32_t k0 = step * kStep + 16 * (lane >> 5) + 8 * d;
-    uint32_t v = 0;
+    for (int d = 0; d < 4; ++d) {
+      uint32_t v = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t k = k0 + e;
-      const uint32_t u = row < d_out && k < d_in ? (w[k >> 1] >> (4 * (k & 1))) & 15u : flip;
-      v |= (u ^ flip) << (8 * (e & 3) + 4 * (e >> 2));  // flip 8: u ^ 8 is u - 8 in four bits
+      for (int e = 0; e < 4; ++e) v |= ((8 * (weight(k0 + 4 * d + e) - z)) & 0xffu) << (8 * e);
+      f[d] = static_cast<int>(v);
     }
-    word[d] = v;
+    frag[idx] = f;
+  } else {
+    uint32_t word[2];
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      uint32_t v = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v |= (weight(k0 + 8 * d + e) ^ 8u) << (8 * (e & 3) + 4 * (e >> 2));  // u ^ 8 is u - 8 in four bits
+      word[d] = v;
+    }
+    frag[idx] = make_uint2(word[0], word[1]);
   }
-  frag[idx] = make_uint2(word[0], word[1]);
 }
 
 __device__ __forceinline__ int32_t centred(uint32_t r, uint32_t q) {
@@ -98,10 +118,10 @@ __device__ __forceinline__ int32_t centred(uint32_t r, uint32_t q) {
 }
 
 __global__ __launch_bounds__(kThreads) void q4_scale_kernel(Tables tb, const float* __restrict__ scales,
-                                                            const uint8_t* __restrict__ zeros, uint32_t d_out,
-                                                            uint32_t group, uint32_t groups, uint32_t sub_len,
-                                                            uint32_t subs, uint32_t tiles, size_t total,
-                                                            double scale, int32_t* __restrict__ out) {
+                                                            bool zeros, uint32_t d_out, uint32_t group,
+                                                            uint32_t groups, uint32_t sub_len, uint32_t subs,
+                                                            uint32_t tiles, size_t total, double scale,
+                                                            int2* __restrict__ out) {
   const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][sub][32]
   if (idx >= total) return;
   const uint32_t sub = static_cast<uint32_t>((idx >> 5) % subs);
@@ -109,44 +129,33 @@ __global__ __launch_bounds__(kThreads) void q4_scale_kernel(Tables tb, const flo
   const uint32_t l = static_cast<uint32_t>(lt / tiles);
   const uint32_t row = static_cast<uint32_t>(lt % tiles) * 32 + (idx & 31);
   const uint32_t q = tb.q[l];
-  int32_t sa = 0, sb = 0, zc = 0;
+  int32_t sa = 0, sb = 0;
   if (row < d_out) {
     const size_t at = static_cast<size_t>(row) * groups + static_cast<uint32_t>(static_cast<size_t>(sub) * sub_len / group);
     uint32_t r = reduce_f64_int(rint(static_cast<double>(scales[at]) * scale), q, tb.q_recip[l]);
     r = static_cast<uint32_t>((static_cast<uint64_t>(r) << (zeros ? 29 : 28)) % q);  // 2^32 / 8 or 2^32 / 16
     sa = centred(r, q);
     sb = centred(static_cast<uint32_t>((static_cast<uint64_t>(r) << 16) % q), q);
-    if (zeros) zc = -static_cast<int32_t>(0x08080808u * (zeros[at] & 15u));
   }
-  if (zeros)
-    reinterpret_cast<int4*>(out)[idx] = make_int4(sa, sb, zc, 0);
-  else
-    reinterpret_cast<int2*>(out)[idx] = make_int2(sa, sb);
+  out[idx] = make_int2(sa, sb);
 }
 
 // Where a workgroup finds its part of the layer.
 struct Job {
-  const uint2* frag;       // the whole layer's
-  const int32_t* scales;   // the limb's
+  const void* frag;        // the whole layer's
+  const int2* scales;      // the limb's
   const uint32_t* src;     // input 0's word of column 0 of the workgroup
   uint32_t* dst;           // output 0's
   uint32_t row_bytes, d_out, d_in, steps, subs;
 };
 
-// 8 bytes of a weight fragment -> 16 bytes, 16 v each; with zero points 8 (u - z):
-// 8 u + 128 - 8 z lies in [8, 248] in every byte, so nothing is carried between bytes.
-template <bool kZeros>
-__device__ __forceinline__ v4i unpack(uint2 w, uint32_t zc) {
-  if constexpr (kZeros) {
-    constexpr uint32_t m = 0x78787878u;
-    auto less = [&](uint32_t u) { return static_cast<int>(((u | kBias) + zc) ^ kBias); };
-    return v4i{less((w.x << 3) & m), less((w.x >> 1) & m), less((w.y << 3) & m), less((w.y >> 1) & m)};
-  } else {
-    constexpr uint32_t m = 0xf0f0f0f0u;
-    return v4i{static_cast<int>((w.x << 4) & m), static_cast<int>(w.x & m), static_cast<int>((w.y << 4) & m),
-               static_cast<int>(w.y & m)};
-  }
+// A weight fragment as a matrix operand: 16 v (8 (u - z) with zero points) in each byte.
+__device__ __forceinline__ v4i unpack(uint2 w) {
+  constexpr uint32_t m = 0xf0f0f0f0u;
+  return v4i{static_cast<int>((w.x << 4) & m), static_cast<int>(w.x & m), static_cast<int>((w.y << 4) & m),
+             static_cast<int>(w.y & m)};
 }
+__device__ __forceinline__ v4i unpack(v4i w) { return w; }
 
 // 16 consecutive inputs of one column a thread and pass: pass p of the inputs from
 // `first` on holds blocks b0 + p * blockDim/32 + threadIdx.x/32 of 16 inputs.  Inputs past
@@ -216,31 +225,22 @@ template <int kSteps, bool kZeros, int kTiles>
 __device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_t sub0, uint32_t subs, const v4i* lds,
                                          int64_t (&acc)[kTiles][16]) {
   const uint32_t lane = threadIdx.x & 63;
-  constexpr int kScaleWords = kZeros ? 4 : 2;
-  const uint2* wp[kTiles];
-  const int32_t* sp[kTiles];
+  const Frag<kZeros>* wp[kTiles];
+  const int2* sp[kTiles];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    wp[t] = job.frag + (static_cast<size_t>(tile0 + t) * job.steps + static_cast<size_t>(sub0) * kSteps) * 64;
-    sp[t] = job.scales + (static_cast<size_t>(tile0 + t) * job.subs + sub0) * 32 * kScaleWords;
+    wp[t] = static_cast<const Frag<kZeros>*>(job.frag) +
+            (static_cast<size_t>(tile0 + t) * job.steps + static_cast<size_t>(sub0) * kSteps) * 64;
+    sp[t] = job.scales + (static_cast<size_t>(tile0 + t) * job.subs + sub0) * 32;
   }
-  uint2 raw[kSteps][kTiles];
+  Frag<kZeros> raw[kSteps][kTiles];
   int2 sc[kTiles];
-  uint32_t zc[kTiles];
   auto load = [&](uint32_t g) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) raw[s][t] = wp[t][(g * kSteps + s) * 64 + lane];
-      const int32_t* p = sp[t] + (g * 32 + (lane & 31)) * kScaleWords;
-      if constexpr (kZeros) {
-        const int4 v = *reinterpret_cast<const int4*>(p);
-        sc[t] = make_int2(v.x, v.y);
-        zc[t] = static_cast<uint32_t>(v.z);
-      } else {
-        sc[t] = *reinterpret_cast<const int2*>(p);
-        zc[t] = 0;
-      }
+      sc[t] = sp[t][g * 32 + (lane & 31)];
     }
   };
   load(0);
@@ -249,7 +249,7 @@ __device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) w[s][t] = unpack<kZeros>(raw[s][t], zc[t]);
+      for (int t = 0; t < kTiles; ++t) w[s][t] = unpack(raw[s][t]);
     int2 sg[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) sg[t] = sc[t];
@@ -316,10 +316,10 @@ __device__ __forceinline__ void store(const Job& job, uint32_t tile0, const Modu
 struct Place {
   uint32_t limb, split;
 };
-__device__ __forceinline__ Place place_of(const Tables& tb, const uint2* frag, const int32_t* scales,
+__device__ __forceinline__ Place place_of(const Tables& tb, const void* frag, const int2* scales,
                                           const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out, uint32_t d_in,
                                           uint32_t limbs, uint32_t steps, uint32_t subs, uint32_t tiles, uint32_t splits,
-                                          int scale_words, Job* job) {
+                                          Job* job) {
   const uint32_t G = gridDim.x;
   uint32_t lid = blockIdx.x;
   if ((G & 7u) == 0) lid = (lid & 7u) * (G >> 3) + (lid >> 3);
@@ -327,7 +327,7 @@ __device__ __forceinline__ Place place_of(const Tables& tb, const uint2* frag, c
   const uint32_t l = lc / tiles_n, ntile = lc - l * tiles_n;
   const uint32_t n = tb.n, col0 = ntile * kCols, c = col0 >> tb.log_n, k0 = col0 & (n - 1);
   const size_t at = (static_cast<size_t>(c) * limbs + l) * n + k0;
-  *job = {frag, scales + static_cast<size_t>(l) * tiles * subs * 32 * scale_words, ct_in + at, ct_out + at,
+  *job = {frag, scales + static_cast<size_t>(l) * tiles * subs * 32, ct_in + at, ct_out + at,
           2u * limbs * n * 4u, d_out, d_in, steps, subs};
   return {l, split};
 }
@@ -342,13 +342,13 @@ constexpr int kWholeTiles = 2;
 constexpr uint32_t kLdsBytes = 160 << 10;
 template <int kSteps, bool kZeros, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
-    Tables tb, const uint2* __restrict__ frag, const int32_t* __restrict__ scales, const uint32_t* __restrict__ ct_in,
+    Tables tb, const void* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
     uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
     uint32_t tiles, uint32_t splits) {
   extern __shared__ v4i lds[];
   Job job;
   const Place at = place_of(tb, frag, scales, ct_in, ct_out, d_out, d_in, limbs, steps, subs, tiles, splits,
-                            kZeros ? 4 : 2, &job);
+                            &job);
   const Modulus q = modulus(tb.q[at.limb]);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t groups = tiles / kWholeTiles, each = (groups + splits - 1) / splits;
@@ -376,13 +376,13 @@ constexpr uint32_t kChunk = kDeepWaves;  // steps of a chunk: 16 inputs of one c
 static_assert(kChunk % 4 == 0 && 2 * kChunk * kStep <= kFold, "whole sub-groups, and a reduction every other chunk");
 template <int kSteps, bool kZeros>
 __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
-    Tables tb, const uint2* __restrict__ frag, const int32_t* __restrict__ scales, const uint32_t* __restrict__ ct_in,
+    Tables tb, const void* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
     uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
     uint32_t tiles, uint32_t splits) {
   __shared__ v4i lds[2][kChunk * kStepFrags];
   Job job;
   const Place at = place_of(tb, frag, scales, ct_in, ct_out, d_out, d_in, limbs, steps, subs, tiles, splits,
-                            kZeros ? 4 : 2, &job);
+                            &job);
   const Modulus q = modulus(tb.q[at.limb]);
   const int32_t c32 = centred(tb.pow256[at.limb * 8 + 4], q.q);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -415,8 +415,8 @@ template <int kSteps, bool kZeros>
 hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out,
                   uint32_t d_out, uint32_t d_in, uint32_t limbs, hipStream_t s) {
   const uint8_t* base = static_cast<const uint8_t*>(w_q4);
-  const uint2* frag = reinterpret_cast<const uint2*>(base);
-  const int32_t* scales = reinterpret_cast<const int32_t*>(base + sh.frag_bytes);
+  const void* frag = base;
+  const int2* scales = reinterpret_cast<const int2*>(base + sh.frag_bytes);
   const uint32_t strips = 2 * t.n / kCols * limbs;  // column tiles of every limb
   // Few rows leave most of a whole strip's waves idle behind its one conversion; the chunked
   // kernel overlaps the two (2^14, 2 limbs, groups of 128, whole : chunked, us: 1024 -> 128 102 : 93, 256 -> 64
@@ -450,14 +450,20 @@ hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* sca
                             hipStream_t s) {
   const Shape sh = shape_of(d_out, d_in, group, limbs, zeros != nullptr);
   uint8_t* base = static_cast<uint8_t*>(w_q4);
-  const size_t lanes = sh.frag_bytes / 8, total = static_cast<size_t>(limbs) * sh.tiles * sh.subs * 32;
-  q4_frag_kernel<<<static_cast<uint32_t>((lanes + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      w4, d_out, d_in, sh.steps, lanes, zeros ? 0u : 8u, reinterpret_cast<uint2*>(base));
+  const size_t lanes = static_cast<size_t>(sh.tiles) * sh.steps * 64;
+  const size_t total = static_cast<size_t>(limbs) * sh.tiles * sh.subs * 32;
+  const uint32_t grid = static_cast<uint32_t>((lanes + kThreads - 1) / kThreads);
+  if (zeros)
+    q4_frag_kernel<true><<<grid, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes,
+                                                   reinterpret_cast<v4i*>(base));
+  else
+    q4_frag_kernel<false><<<grid, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes,
+                                                    reinterpret_cast<uint2*>(base));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   q4_scale_kernel<<<static_cast<uint32_t>((total + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      t, scales, zeros, d_out, group, sh.groups, sh.sub_len, sh.subs, sh.tiles, total, scale,
-      reinterpret_cast<int32_t*>(base + sh.frag_bytes));
+      t, scales, zeros != nullptr, d_out, group, sh.groups, sh.sub_len, sh.subs, sh.tiles, total, scale,
+      reinterpret_cast<int2*>(base + sh.frag_bytes));
   return hipGetLastError();
 }
 
