@@ -217,43 +217,46 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
+// A wave's next weights and scales: of one sub-group of kTiles row tiles, loaded a sub-group
+// ahead and across row groups and chunks (768 -> 3072, groups of 128: 3.78 -> 3.69 ms against a fresh start
+// a row group; 3072 -> 768 1.53 -> 1.45 ms).
+template <int kSteps, bool kZeros, int kTiles>
+struct Ahead {
+  Frag<kZeros> raw[kSteps][kTiles];
+  int2 sc[kTiles];
+  __device__ __forceinline__ void load(const Job& job, uint32_t tile0, uint32_t sub) {
+    const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const Frag<kZeros>* w = static_cast<const Frag<kZeros>*>(job.frag) +
+                              (static_cast<size_t>(tile0 + t) * job.steps + static_cast<size_t>(sub) * kSteps) * 64;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) raw[s][t] = w[s * 64 + lane];
+      sc[t] = job.scales[(static_cast<size_t>(tile0 + t) * job.subs + sub) * 32 + (lane & 31)];
+    }
+  }
+};
+
 // A wave's kTiles row tiles from tile0 on over `subs` sub-groups: sub0 + g of the layer,
 // whose residues are sub-group g of the LDS.  Two digits at a time: their sums of a sub-group
 // in i32 (below 128 * 128 * 257 * 128 < 2^30), a = S0 + 2^8 S1, then scale times a into
-// the 64-bit sums.
+// the 64-bit sums.  `next` holds the first sub-group's weights, and is left with those of (tile1, sub1).
 template <int kSteps, bool kZeros, int kTiles>
-__device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_t sub0, uint32_t subs, const v4i* lds,
+__device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_t sub0, uint32_t subs, uint32_t tile1,
+                                         uint32_t sub1, const v4i* lds, Ahead<kSteps, kZeros, kTiles>& next,
                                          int64_t (&acc)[kTiles][16]) {
   const uint32_t lane = threadIdx.x & 63;
-  const Frag<kZeros>* wp[kTiles];
-  const int2* sp[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    wp[t] = static_cast<const Frag<kZeros>*>(job.frag) +
-            (static_cast<size_t>(tile0 + t) * job.steps + static_cast<size_t>(sub0) * kSteps) * 64;
-    sp[t] = job.scales + (static_cast<size_t>(tile0 + t) * job.subs + sub0) * 32;
-  }
-  Frag<kZeros> raw[kSteps][kTiles];
-  int2 sc[kTiles];
-  auto load = [&](uint32_t g) {
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) raw[s][t] = wp[t][(g * kSteps + s) * 64 + lane];
-      sc[t] = sp[t][g * 32 + (lane & 31)];
-    }
-  };
-  load(0);
-  for (uint32_t g = 0; g < subs; ++g) {
+  auto body = [&](uint32_t g) {
     v4i w[kSteps][kTiles];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) w[s][t] = unpack(raw[s][t]);
+      for (int t = 0; t < kTiles; ++t) w[s][t] = unpack(next.raw[s][t]);
     int2 sg[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) sg[t] = sc[t];
-    if (g + 1 < subs) load(g + 1);
+    for (int t = 0; t < kTiles; ++t) sg[t] = next.sc[t];
+    const bool more = g + 1 < subs;
+    next.load(job, more ? tile0 : tile1, more ? sub0 + g + 1 : sub1);
     const v4i* f = lds + static_cast<size_t>(g) * kSteps * kStepFrags + lane;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {  // digits 0 and 1, then 2 and 3
@@ -279,7 +282,13 @@ __device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_
           acc[t][r] += static_cast<int64_t>(sv) * (m[t][0][r] + (m[t][1][r] << 8));
       }
     }
-  }
+  };
+  // The shortest sub-groups' first one stands before the loop: its weights came before the last outputs'
+  // stores, and the loop's wait would cover those too (768 -> 3072, groups of 32: 6.40 -> 6.17 ms; longer
+  // sub-groups lose more to registers: groups of 128 3.69 -> 4.02 ms).
+  uint32_t g = 0;
+  if constexpr (kSteps == 1) body(g++);
+  for (; g < subs; ++g) body(g);
 }
 
 template <int kTiles>
@@ -360,10 +369,15 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
     place<kPasses>(b0, 2 * steps, x, lds);
   }
   __syncthreads();
-  for (uint32_t rg = at.split * each + wave; rg < end; rg += kWaves) {
+  Ahead<kSteps, kZeros, kWholeTiles> next;
+  uint32_t rg = at.split * each + wave;
+  if (rg >= end) return;
+  next.load(job, rg * kWholeTiles, 0);
+  for (; rg < end; rg += kWaves) {
     int64_t acc[kWholeTiles][16];
     clear<kWholeTiles>(acc);
-    contract<kSteps, kZeros, kWholeTiles>(job, rg * kWholeTiles, 0, subs, lds, acc);
+    const uint32_t after = rg + kWaves < end ? rg + kWaves : rg;
+    contract<kSteps, kZeros, kWholeTiles>(job, rg * kWholeTiles, 0, subs, after * kWholeTiles, 0, lds, next, acc);
     store<kWholeTiles>(job, rg * kWholeTiles, q, acc);
   }
 }
@@ -394,6 +408,8 @@ __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
   fetch<1>(job, 0, 0, 2 * kChunk, x);
   place<1>(0, 2 * kChunk, x, lds[0]);
   __syncthreads();
+  Ahead<kSteps, kZeros, kDeepTiles> next;
+  if (mine) next.load(job, tile, 0);
   uint32_t buf = 0;
   for (uint32_t s0 = 0; s0 < steps; s0 += kChunk, buf ^= 1) {
     const bool more = s0 + kChunk < steps;
@@ -403,7 +419,8 @@ __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[0][r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[0][r], q))) * c32;
       }
-      contract<kSteps, kZeros, kDeepTiles>(job, tile, s0 / kSteps, min(kChunk, steps - s0) / kSteps, lds[buf], acc);
+      contract<kSteps, kZeros, kDeepTiles>(job, tile, s0 / kSteps, min(kChunk, steps - s0) / kSteps, tile,
+                                           more ? (s0 + kChunk) / kSteps : 0, lds[buf], next, acc);
     }
     if (more) place<1>(0, 2 * kChunk, x, lds[buf ^ 1]);
     __syncthreads();
