@@ -29,17 +29,20 @@ struct Move {
 
 // One request of an append.
 struct Request {
-  int32_t why;     // kCacheOk: served
+  int32_t why;      // kCacheOk: served
   int32_t seq;
-  int32_t have;    // rows before the call
-  int32_t want;    // rows to append
-  int32_t shared;  // the partly filled last page, where others hold it too; else -1
-  int32_t holders; // of `shared`
-  int32_t last;    // the partly filled last page; -1 where the first new row opens a page
-  int32_t first;   // first input row
-  int32_t copy;    // 1: `shared` is copied before it is written
+  int32_t want;     // rows to append; -1 for a row0 that runs backwards
+  int32_t first;    // first input row
+  uint32_t at;      // whole pages before the call
+  uint32_t part;    // rows on the page after them
+  int32_t last;     // that page; -1 where there is none or the call does not write it
+  int32_t holders;  // of `last`
+  int32_t copy;     // 1: `last` is held by others too and copied before it is written
+  uint32_t need;    // pages from the free ones, the copy's among them
 };
-__device__ __forceinline__ Request no_request() { return {kCacheBadRequest, 0, 0, 0, -1, 0, -1, 0, 0}; }
+__device__ __forceinline__ Request no_request() { return {kCacheBadRequest, 0, 0, 0, 0, 0, -1, 0, 0, 0}; }
+// The first position of the sequence's table that gets a page.
+__device__ __forceinline__ uint32_t first_new(const Request& r) { return r.at + (r.part != 0 && !r.copy); }
 
 // Workspace of an append or a compaction.
 struct Plan {
@@ -236,10 +239,13 @@ __device__ __forceinline__ int32_t asked_rows(const int32_t* row0, uint32_t i, u
 // What an append does, worked out by one workgroup: pages for every request,
 // the tables, lengths and holders, and the list of row moves (first the input rows', then
 // the copied rows').  Each request is looked up once (its sequence, length, table entry
-// and page's holders are four loads that wait for each other) and kept in registers and in
-// `requests`; pages, rows and copies are then dealt out to all threads, each finding its
-// request by bisection of the requests' starts in LDS.  1 row for each of 64 forks, 1024 pages:
-// 20 us with a wave a request, 9 us so.
+// and page's holders are four loads that wait for each other); pages, rows and copies are then
+// dealt out to all threads, each finding its request by bisection of the requests' starts in
+// LDS.  kFew: at most one request a thread, kept in registers and LDS (with both forms in one
+// kernel its code alone, 14 KB, took microseconds to fetch); otherwise requests wait in memory
+// and shared pages are counted by atomics.  1 row for each of 64 forks, 1024 pages: 20 us with a wave
+// a request, 9 us so.
+template <bool kFew>
 __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
     Cache c, const int32_t* __restrict__ seq, const int32_t* __restrict__ row0, uint32_t count,
     const uint32_t* __restrict__ rows_in, uint32_t rows, int32_t* __restrict__ status, Plan p) {
@@ -248,104 +254,107 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
   __shared__ Request reqs[kPlanThreads];
   __shared__ uint32_t page0[kPlanThreads], copy0[kPlanThreads];
   __shared__ __align__(16) int32_t pages[kPlanThreads];  // shared pages of the requests, then the first free pages
-  const uint32_t tid = threadIdx.x;
-  const int32_t P = c.page_rows;
+  const uint32_t tid = threadIdx.x, P = c.page_rows;
+  const uint32_t blocks = kFew ? 1 : (count + kPlanThreads - 1) / kPlanThreads;  // of requests
   const int32_t holders0 = tid < c.pages ? c.refs[tid] : 1;  // of the first pages, looked at further down
-  for (uint32_t w = tid; w < (c.seqs + 31) / 32; w += kPlanThreads) seen[w] = twice[w] = 0;
-  bool astray = false;  // row0 that runs backwards would give one row to two requests: nobody is served
-  for (uint32_t i = tid; i < count; i += kPlanThreads) astray |= asked_rows(row0, i, rows) < 0;
-  astray = __syncthreads_or(astray && row0);
-  for (uint32_t i = tid; i < count; i += kPlanThreads) {
-    const uint32_t s = seq[i];
-    if (s >= c.seqs) continue;
-    const uint32_t bit = 1u << (s & 31);
-    if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
-  }
-  __syncthreads();
+  // What memory says of a request (loads that wait for each other: before any barrier), and
+  // what the call makes of it.
   auto look_up = [&](uint32_t i) {
     Request r = no_request();
     r.seq = seq[i];
     r.want = asked_rows(row0, i, rows);
     r.first = row0 ? row0[i] : static_cast<int32_t>(i);
-    if (astray || static_cast<uint32_t>(r.seq) >= c.seqs || r.want < 0 || (twice[r.seq >> 5] >> (r.seq & 31) & 1)) return r;
-    r.have = held_rows(c, r.seq);
-    if (static_cast<int64_t>(r.have) + r.want > static_cast<int64_t>(c.max_pages) * P) {
-      r.why = kCacheTableFull;
-      return r;
-    }
-    r.why = kCacheOk;
-    if (r.want > 0 && r.have % P != 0) {
-      r.last = c.table[static_cast<size_t>(r.seq) * c.max_pages + r.have / P];
-      if (valid_page(c, r.last)) {
-        r.holders = c.refs[r.last];
-        if (r.holders > 1) r.shared = r.last;
+    if (static_cast<uint32_t>(r.seq) < c.seqs) {
+      const uint32_t have = held_rows(c, r.seq);
+      r.at = have / P;
+      r.part = have - r.at * P;
+      if (r.want > 0 && r.part != 0) {
+        r.last = c.table[static_cast<size_t>(r.seq) * c.max_pages + r.at];
+        if (valid_page(c, r.last)) r.holders = c.refs[r.last];
+        else r.last = -1;
       }
     }
     return r;
   };
-  const Request mine = tid < count ? look_up(tid) : no_request();
-  auto request = [&](uint32_t i) { return i == tid ? mine : look_up(i); };
+  Request mine = tid < count ? look_up(tid) : no_request();
+  for (uint32_t w = tid; w < (c.seqs + 31) / 32; w += kPlanThreads) seen[w] = twice[w] = 0;
+  bool astray = mine.want < 0;  // row0 that runs backwards would give one row to two requests: nobody is served
+  if constexpr (!kFew)
+    for (uint32_t i = tid + kPlanThreads; i < count; i += kPlanThreads) astray |= asked_rows(row0, i, rows) < 0;
+  astray = __syncthreads_or(astray && row0);
+  for (uint32_t b = 0; b < blocks; ++b) {
+    const uint32_t i = b * kPlanThreads + tid;
+    const uint32_t s = i >= count ? c.seqs : b == 0 ? mine.seq : seq[i];
+    if (s >= c.seqs) continue;
+    const uint32_t bit = 1u << (s & 31);
+    if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
+  }
+  __syncthreads();
+  auto judge = [&](Request& r) {
+    if (astray || static_cast<uint32_t>(r.seq) >= c.seqs || r.want < 0 || (twice[r.seq >> 5] >> (r.seq & 31) & 1))
+      r.why = kCacheBadRequest;
+    else if (static_cast<uint64_t>(r.at) * P + r.part + r.want > static_cast<uint64_t>(c.max_pages) * P)
+      r.why = kCacheTableFull;
+    else
+      r.why = kCacheOk;
+  };
+  auto sharing = [](const Request& r) { return r.why == kCacheOk && r.holders > 1; };
   // Where every holder of a shared page is in the call, the last of them keeps it; the
-  // others copy it.  Up to one request a thread they are counted out of LDS, else by atomics.
-  const bool few = count <= kPlanThreads;
-  bool sharing = false;
-  if (few) {
-    pages[tid] = mine.why == kCacheOk ? mine.shared : -1;
-    sharing = pages[tid] >= 0;
-  } else {
-    for (uint32_t i = tid; i < count; i += kPlanThreads) {
-      const Request r = request(i);
-      if (r.why == kCacheOk && r.shared >= 0) p.sharers[r.shared] = 0, p.last[r.shared] = -1, sharing = true;
-    }
-    __threadfence();  // the stores are in memory before the atomics on the same words
-  }
-  sharing = __syncthreads_or(sharing);
-  if (sharing && !few) {
-    for (uint32_t i = tid; i < count; i += kPlanThreads) {
-      const Request r = request(i);
-      if (r.why != kCacheOk || r.shared < 0) continue;
-      atomicAdd(&p.sharers[r.shared], 1);
-      atomicMax(&p.last[r.shared], static_cast<int32_t>(i));
-    }
+  // others copy it.  Then the pages that the request takes.
+  auto settle = [&](Request& r, uint32_t i, int32_t sharers, int32_t last) {
+    if (r.why != kCacheOk) return;
+    r.copy = r.holders > 1 && !(sharers == r.holders && last == static_cast<int32_t>(i));
+    r.need = r.at + (r.part + r.want + P - 1) / P - first_new(r);
+  };
+  auto needs = [](const Request& r) { return make_uint2(r.need, r.copy ? r.part : 0); };  // pages, rows to copy
+  uint2 total = make_uint2(0, 0), mine0 = make_uint2(0, 0);
+  if (tid < count) judge(mine);
+  if constexpr (kFew) {
+    pages[tid] = sharing(mine) ? mine.last : -1;
     __syncthreads();
-  }
-  auto copies_page = [&](uint32_t i, const Request& r) {
-    if (r.why != kCacheOk || r.shared < 0) return false;
     int32_t sharers = 0, last = -1;
-    if (few) {
+    if (sharing(mine)) {
       for (uint32_t j = 0; j < count; j += 4) {  // `pages` is padded with -1
         const int4 v = *reinterpret_cast<const int4*>(&pages[j]);
-        sharers += (v.x == r.shared) + (v.y == r.shared) + (v.z == r.shared) + (v.w == r.shared);
-        if (v.x == r.shared) last = j;
-        if (v.y == r.shared) last = j + 1;
-        if (v.z == r.shared) last = j + 2;
-        if (v.w == r.shared) last = j + 3;
+        const bool x = v.x == mine.last, y = v.y == mine.last, z = v.z == mine.last, w = v.w == mine.last;
+        sharers += x + y + z + w;
+        last = w ? j + 3 : z ? j + 2 : y ? j + 1 : x ? j : last;
       }
-    } else {
-      sharers = fresh_load(&p.sharers[r.shared]);
-      last = fresh_load(&p.last[r.shared]);
     }
-    return !(sharers == r.holders && last == static_cast<int32_t>(i));
-  };
-  auto needs = [&](const Request& r) {  // pages, rows to copy
-    if (r.why != kCacheOk) return make_uint2(0, 0);
-    return make_uint2(pages_of(r.have + r.want, P) - pages_of(r.have, P) + r.copy, r.copy ? r.have % P : 0);
-  };
-  uint2 total = make_uint2(0, 0), mine0 = make_uint2(0, 0);
-  for (uint32_t i0 = 0; i0 < count; i0 += kPlanThreads) {
-    const uint32_t i = i0 + tid;
-    Request r = no_request();
-    if (i < count) {
-      r = request(i);
-      r.copy = copies_page(i, r);
+    settle(mine, tid, sharers, last);
+    mine0 = scan(needs(mine), lds, &total);
+    reqs[tid] = mine;
+    if (status && tid < count && mine.why != kCacheOk) status[tid] = mine.why;
+  } else {
+    for (uint32_t i = tid; i < count; i += kPlanThreads) {
+      Request r = look_up(i);
+      judge(r);
       p.requests[i] = r;
-      if (status && r.why != kCacheOk) status[i] = r.why;
+      if (sharing(r)) p.sharers[r.last] = 0, p.last[r.last] = -1;
     }
-    uint2 sum;
-    const uint2 at = scan(needs(r), lds, &sum);
-    if (i0 == 0) mine0 = at, reqs[tid] = r;
-    total.x += sum.x;
-    total.y += sum.y;
+    __threadfence();  // the stores are in memory before the atomics on the same words
+    __syncthreads();
+    for (uint32_t i = tid; i < count; i += kPlanThreads) {
+      const Request r = p.requests[i];
+      if (!sharing(r)) continue;
+      atomicAdd(&p.sharers[r.last], 1);
+      atomicMax(&p.last[r.last], static_cast<int32_t>(i));
+    }
+    __syncthreads();
+    for (uint32_t b = 0; b < blocks; ++b) {
+      const uint32_t i = b * kPlanThreads + tid;
+      Request r = no_request();
+      if (i < count) {
+        r = p.requests[i];
+        settle(r, i, sharing(r) ? fresh_load(&p.sharers[r.last]) : 0, sharing(r) ? fresh_load(&p.last[r.last]) : 0);
+        p.requests[i] = r;
+        if (status && r.why != kCacheOk) status[i] = r.why;
+      }
+      uint2 sum;
+      scan(needs(r), lds, &sum);
+      total.x += sum.x;
+      total.y += sum.y;
+    }
   }
   // the lowest free pages, in order
   uint32_t found = 0;
@@ -361,52 +370,46 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
     found += sum.x;
   }
   __syncthreads();
-  if (found < total.x) {  // not enough: nobody is served
+  const bool short_of = found < total.x;  // not enough: nobody is served
+  if (tid == 0) *p.moves_n = short_of ? 0 : rows + total.y;
+  if (short_of) {
     for (uint32_t i = tid; i < count; i += kPlanThreads)
-      if (status && p.requests[i].why == kCacheOk) status[i] = kCacheNoPages;
-    if (tid == 0) *p.moves_n = 0;
+      if (status && (kFew ? mine.why : p.requests[i].why) == kCacheOk) status[i] = kCacheNoPages;
     return;
   }
-  if (tid == 0) *p.moves_n = rows + total.y;
-  // rows that no request names, or none that is served, stay where they are
-  if (!row0)
-    for (uint32_t r = count + tid; r < rows; r += kPlanThreads) p.moves[r].dst = nullptr;
-  else
-    for (uint32_t r = tid; r < rows; r += kPlanThreads)
-      if (astray || r < static_cast<uint32_t>(row0[0]) || r >= static_cast<uint32_t>(row0[count])) p.moves[r].dst = nullptr;
+  // input rows that no request names stay where they are
+  const uint32_t named0 = row0 && !astray ? row0[0] : 0;
+  const uint32_t named1 = astray ? 0 : row0 ? row0[count] : min(count, rows);
+  for (uint32_t r = tid; r < rows; r += kPlanThreads)
+    if (r < named0 || r >= named1) p.moves[r].dst = nullptr;
   if (astray) return;
   auto fresh = [&](uint32_t k) { return k < kPlanThreads ? pages[k] : p.fresh[k]; };
   uint2 done = make_uint2(0, 0);
-  for (uint32_t i0 = 0; i0 < count; i0 += kPlanThreads) {
-    const uint32_t n = min(count - i0, static_cast<uint32_t>(kPlanThreads));
-    uint2 at = mine0, sum;
-    if (i0 != 0 || count > kPlanThreads) {
+  for (uint32_t b = 0; b < blocks; ++b) {
+    const uint32_t i0 = b * kPlanThreads, n = min(count - i0, static_cast<uint32_t>(kPlanThreads));
+    uint2 at = mine0, sum = total;
+    if constexpr (!kFew) {
       __syncthreads();  // the block before is read out
-      Request r = no_request();
-      if (tid < n) r = p.requests[i0 + tid];
-      reqs[tid] = r;
-      at = scan(needs(r), lds, &sum);
-    } else {
-      sum = total;
+      mine = tid < n ? p.requests[i0 + tid] : no_request();
+      reqs[tid] = mine;
+      at = scan(needs(mine), lds, &sum);
     }
     page0[tid] = at.x;
     copy0[tid] = at.y;
-    if (tid < n && reqs[tid].why == kCacheOk) {
-      const Request r = reqs[tid];
-      c.lens[r.seq] = r.have + r.want;
+    if (tid < n && mine.why == kCacheOk) {
+      c.lens[mine.seq] = static_cast<int32_t>(mine.at * P + mine.part + mine.want);
       if (status) status[i0 + tid] = kCacheOk;
-      if (r.copy) atomicSub(&c.refs[r.shared], 1);
+      if (mine.copy) atomicSub(&c.refs[mine.last], 1);
     }
     __syncthreads();
     for (uint32_t k = tid; k < sum.x; k += kPlanThreads) {  // pages
       const uint32_t j = owner(page0, n, k);
-      const Request r = reqs[j];
       const int32_t page = fresh(done.x + k);
-      c.table[static_cast<size_t>(r.seq) * c.max_pages + (r.copy ? r.have / P : pages_of(r.have, P)) + (k - page0[j])] = page;
+      c.table[static_cast<size_t>(reqs[j].seq) * c.max_pages + first_new(reqs[j]) + (k - page0[j])] = page;
       c.refs[page] = 1;
     }
-    const uint32_t first = row0 ? reqs[0].first : i0, end = row0 ? row0[i0 + n] : min(i0 + n, rows);
-    for (uint32_t k = first + tid; k < end; k += kPlanThreads) {  // input rows
+    const uint32_t end = row0 ? row0[i0 + n] : min(i0 + n, rows);
+    for (uint32_t k = (row0 ? reqs[0].first : i0) + tid; k < end; k += kPlanThreads) {  // input rows
       uint32_t j = k - i0;
       if (row0) {  // the last request that starts at or before row k (empty ones before it start there too)
         uint32_t lo = 0, hi = n;
@@ -420,17 +423,15 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
       const Request r = reqs[j];
       uint32_t* dst = nullptr;
       if (r.why == kCacheOk) {
-        const int32_t pos = r.have + static_cast<int32_t>(k) - r.first, start = r.copy ? r.have / P : pages_of(r.have, P);
-        const int32_t page = pos / P < start ? r.last : fresh(done.x + page0[j] + pos / P - start);
-        if (valid_page(c, page)) dst = c.pool + (static_cast<size_t>(page) * P + pos % P) * c.row_words;  // else the caller's table had no page there
+        const uint32_t off = r.part + (k - r.first), ahead = off / P;
+        const int32_t page = r.at + ahead < first_new(r) ? r.last : fresh(done.x + page0[j] + r.at + ahead - first_new(r));
+        if (valid_page(c, page)) dst = c.pool + (static_cast<size_t>(page) * P + (off - ahead * P)) * c.row_words;  // else the caller's table had no page there
       }
       p.moves[k] = {rows_in + static_cast<size_t>(k) * c.row_words, dst};
     }
     for (uint32_t k = tid; k < sum.y; k += kPlanThreads) {  // copied rows
-      const uint32_t j = owner(copy0, n, k);
-      const Request r = reqs[j];
-      const uint32_t slot = k - copy0[j];
-      p.moves[rows + done.y + k] = {c.pool + (static_cast<size_t>(r.shared) * P + slot) * c.row_words,
+      const uint32_t j = owner(copy0, n, k), slot = k - copy0[j];
+      p.moves[rows + done.y + k] = {c.pool + (static_cast<size_t>(reqs[j].last) * P + slot) * c.row_words,
                                     c.pool + (static_cast<size_t>(fresh(done.x + page0[j])) * P + slot) * c.row_words};
     }
     done.x += sum.x;
@@ -592,7 +593,8 @@ hipError_t launch_cache_append(const Cache& c, const int32_t* seq, const int32_t
                                hipStream_t s) {
   Plan p;
   append_layout(c, count, rows, static_cast<uint8_t*>(workspace), &p);
-  cache_append_plan_kernel<<<1, kPlanThreads, 0, s>>>(c, seq, row0, count, rows_in, rows, status, p);
+  const auto plan = count <= kPlanThreads ? cache_append_plan_kernel<true> : cache_append_plan_kernel<false>;
+  plan<<<1, kPlanThreads, 0, s>>>(c, seq, row0, count, rows_in, rows, status, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   cache_move_kernel<<<move_blocks(append_moves(c, count, rows), c.row_words), kMoveThreads, 0, s>>>(
