@@ -48,7 +48,7 @@ constexpr uint32_t kFold = 1024;     // most inputs between reductions of the 64
 //     64: 1.97 ms with 4-bit u, 1.79 ms so).
 //   scales [limb][tile][sub-group][32 rows] of {sa, sb}: sa = 2^32 S / 16, sb = 2^48 S / 16 mod q_l
 //     (/ 8 with zero points), centred.  The 2^32 is what the closing reduction divides by.
-// A sub-group is what one set of i32 sums covers: 128 or 64 inputs that divide
+// A sub-group is what one set of i32 sums covers: 128, 96 or 64 inputs that divide
 // the group, else 32; a group that holds every input is cut freely.
 struct Shape {
   uint32_t tiles, steps, groups, sub_len, subs;
@@ -60,9 +60,9 @@ Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, bo
   s.tiles = (d_out + kPadRows - 1) / kPadRows * (kPadRows / 32);
   s.groups = (d_in + group - 1) / group;
   if (s.groups == 1)
-    s.sub_len = d_in <= 32 ? 32 : d_in <= 64 ? 64 : 128;
+    s.sub_len = d_in <= 32 ? 32 : d_in <= 64 ? 64 : d_in <= 96 ? 96 : 128;
   else
-    s.sub_len = group % 128 == 0 ? 128 : group % 64 == 0 ? 64 : 32;
+    s.sub_len = group % 128 == 0 ? 128 : group % 96 == 0 ? 96 : group % 64 == 0 ? 64 : 32;
   s.subs = (d_in + s.sub_len - 1) / s.sub_len;
   s.steps = s.subs * (s.sub_len / kStep);
   s.frag_bytes = static_cast<size_t>(s.tiles) * s.steps * 64 * (zeros ? 16 : 8);
@@ -387,7 +387,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
 // while the matrix cores work on this one's out of the other half of the LDS.
 constexpr int kDeepWaves = 12, kDeepTiles = 1;
 constexpr uint32_t kChunk = kDeepWaves;  // steps of a chunk: 16 inputs of one column a thread
-static_assert(kChunk % 4 == 0 && 2 * kChunk * kStep <= kFold, "whole sub-groups, and a reduction every other chunk");
+static_assert(kChunk % 3 == 0 && kChunk % 4 == 0 && 2 * kChunk * kStep <= kFold, "whole sub-groups, and a reduction every other chunk");
 template <int kSteps, bool kZeros>
 __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
     Tables tb, const void* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
@@ -438,7 +438,7 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
   // Few rows leave most of a whole strip's waves idle behind its one conversion; the chunked
   // kernel overlaps the two (2^14, 2 limbs, groups of 128, whole : chunked, us: 1024 -> 128 102 : 93, 256 -> 64
   // 37 : 31, 256 -> 256 43.0 : 42.7, 1024 -> 384 158 : 166, 768 -> 768 196 : 239).
-  if (sh.steps * kStep <= kFold && d_out > 256) {
+  if (d_in <= kFold && d_out > 256) {  // at most 33 steps of 4 KiB
     const uint32_t strip_bytes = sh.steps * kStepFrags * 16, waves = 2 * strip_bytes <= kLdsBytes ? 4 : 8;
     // Row splits only where the column strips alone leave CUs idle: each split converts the strip again.
     const uint32_t groups = sh.tiles / kWholeTiles, blocks = (groups + waves - 1) / waves;
@@ -490,6 +490,7 @@ hipError_t launch_mac_q4(const Tables& t, const void* w_q4, const uint32_t* ct_i
   switch (sh.sub_len) {
     case 32: return (zeros ? launch<1, true> : launch<1, false>)(t, sh, w_q4, ct_in, ct_out, d_out, d_in, limbs, s);
     case 64: return (zeros ? launch<2, true> : launch<2, false>)(t, sh, w_q4, ct_in, ct_out, d_out, d_in, limbs, s);
+    case 96: return (zeros ? launch<3, true> : launch<3, false>)(t, sh, w_q4, ct_in, ct_out, d_out, d_in, limbs, s);
     default: return (zeros ? launch<4, true> : launch<4, false>)(t, sh, w_q4, ct_in, ct_out, d_out, d_in, limbs, s);
   }
 }

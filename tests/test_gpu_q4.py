@@ -81,6 +81,15 @@ def test_output_counts(gpu_lib, d_out):
 
 
 @gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("d_in,group", [(70, 128), (96, 96), (513, 96), (1000, 192), (1024, 96), (1025, 96), (2500, 288)])
+def test_groups_of_three_steps(gpu_lib, d_in, group, zeros):
+    """Groups of 96 inputs and their multiples in a strip that stays whole (1024 inputs end inside
+    the last group, a step past them) and in chunks."""
+    check(gpu_lib, 10, 1, 300, d_in, group, zeros, 450 + d_in, rows=[0, 31, 64, 255, 299])
+
+
+@gpu
 @pytest.mark.parametrize("d_in,group", [(2048, 128), (2049, 64), (3072, 256), (4100, 32), (9000, 128), (2100, 2112)])
 @pytest.mark.parametrize("zeros", [False, True])
 def test_deep_contractions(gpu_lib, d_in, group, zeros):
