@@ -180,8 +180,8 @@ int ckks_linear_mac_scalar_noalloc(const ckks_ctx* ctx, const uint32_t* w_enc,
  * zero points.  The plaintext of a weight is (u - z) rint(scales * scale), rint
  * rounding half to even: the scale is rounded once and the small integer kept,
  * within 15/2 of the rounding of each product.  Encoded weights take 1/2 byte
- * (1 byte with zero points) and 8 limbs / group bytes a weight (groups below 128
- * that 64 does not divide: 8 limbs / 32), against 4 limbs bytes for
+ * (1 byte with zero points) and 8 limbs / s bytes a weight, s the largest of 128,
+ * 96, 64 and 32 that divides the group, against 4 limbs bytes for
  * ckks_linear_encode_scalar's, so layers stay resident (section 4.2) that did not.
  *
  * group is a positive multiple of 32 (the last group of a row may be shorter;

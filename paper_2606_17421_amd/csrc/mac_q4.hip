@@ -14,13 +14,16 @@
 // What bounds it: the vector unit.  Beside each 32-cycle v_mfma_i32_32x32x32_i8 run a shift-add
 // and a 64-bit multiply-add for every output of a sub-group and digit pair (4 vector
 // operations a matrix operation at groups of 128, 8 at 64, 16 at 32), the unpacking (1.5) and
-// the closing reduction (1.2 at 768 inputs); at about 4.3 cycles each, and 8.5 issue
-// cycles a matrix operation, they take longer than the matrix pipe, which is busy 49% of the
-// cycles at 768 -> 3072, and the chip holds 1.7 GHz under both (2.05 GHz and the same cycles
-// with zero residues).  Measured without effect there: contractions and combinations
-// interleaved by hand, fragments read ahead, three or four waves a SIMD with half the
-// rows, 64-byte stores after a transpose over lanes; int8 fragments instead of
-// 4-bit ones gave 4% for twice the memory.
+// the closing reduction (1.2 at 768 inputs); at about 4.3 cycles each (8.8 the multiply-add), and
+// 8.5 issue cycles a matrix operation, they take longer than the matrix pipe, which is busy 52% of
+// the cycles at 768 -> 3072 (groups of 128, N = 2^15, 6 limbs: 3.71 ms, 1.0e15 int8 products/s), and
+// the chip holds 1.7 GHz under both (2.05 GHz and the same cycles with zero residues).  Of a whole
+// strip's time the fill comes on top: at 2^14 and 4 limbs 768 -> 768 takes 368 us, 79 of them with the matrix
+// cores idle.  Measured without effect: contractions and combinations interleaved by hand, fragments
+// read ahead, three or four waves a SIMD with half the rows, 64-byte stores after a transpose over
+// lanes.  One combination for two sub-groups that share a scale (groups of 256 and more) gave 1-3%,
+// int8 fragments instead of 4-bit ones 4% for twice the memory; touching the next strip's lines before the
+// last rows cost 5%.
 #include <type_traits>
 
 #include "digits.hpp"
@@ -49,7 +52,7 @@ constexpr uint32_t kFold = 1024;     // most inputs between reductions of the 64
 //   scales [limb][tile][sub-group][32 rows] of {sa, sb}: sa = 2^32 S / 16, sb = 2^48 S / 16 mod q_l
 //     (/ 8 with zero points), centred.  The 2^32 is what the closing reduction divides by.
 // A sub-group is what one set of i32 sums covers: 128, 96 or 64 inputs that divide
-// the group, else 32; a group that holds every input is cut freely.
+// the group (768 -> 768 at 2^14, 4 limbs, groups of 96: 394 us, as 32 + 32 + 32 548), else 32; a group that holds every input is cut freely.
 struct Shape {
   uint32_t tiles, steps, groups, sub_len, subs;
   size_t frag_bytes, scale_bytes;
