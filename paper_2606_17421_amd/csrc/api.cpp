@@ -888,7 +888,7 @@ int check_cache(const ckks_ctx* ctx, const ckks_cache* k, ckks::Cache* out) {
     return fail(CKKS_E_INVALID_ARG, "bad cache sizes (pages=%u, page_rows=%u, row_cts=%u, seqs=%u, max_pages=%u)", k->pages,
                 k->page_rows, k->row_cts, k->seqs, k->max_pages);
   out->row_words = size_t(k->row_cts) * 2 * k->limbs * ctx->n;
-  if (out->row_words * k->page_rows > (size_t(1) << 60) / k->pages)
+  if (out->row_words > (size_t(1) << 60) / k->pages / k->page_rows)
     return fail(CKKS_E_INVALID_ARG, "cache pool too large");
   if (int rc = check_ptr(k->pool, "pool")) return rc;
   if (int rc = check_list(k->refs, "refs")) return rc;

@@ -369,6 +369,17 @@ def test_refusals(gpu_lib):
     assert c.refs.tolist() == [0] * 4 and c.lens.tolist() == [0] * 4
 
 
+@gpu
+def test_sizes_whose_product_passes_64_bits_are_refused(gpu_lib):
+    ck = gpu_lib
+    ctx = ctx_for(ck, 16, 2)
+    c = ck.Cache.empty(ctx, 1, 1, 1, 2, 1, 1)
+    c.struct.row_cts, c.struct.page_rows = 65536, 1 << 30      # 2^34 words a row, 2^64 a page
+    with pytest.raises(ck.CkksError) as e:
+        ck.ckks_cache_free(ctx, c, ints(ck, [0])[:0])
+    assert e.value.code == ck.CKKS_E_INVALID_ARG and "too large" in ck.ckks_last_error()
+
+
 def test_null_context_is_rejected_without_a_gpu():
     import ctypes
 
