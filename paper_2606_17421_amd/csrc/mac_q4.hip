@@ -345,15 +345,15 @@ __device__ __forceinline__ Place place_of(const Tables& tb, const void* frag, co
 }
 
 // Inputs that fit the LDS (d_in <= kFold): the workgroup converts its 32 columns once and its
-// waves walk the 64-row groups without further synchronisation.  Eight waves a CU, two a SIMD:
-// one workgroup, or two of four waves where both strips fit the LDS (640 inputs), so that one converts
-// while the other contracts (2^14, 2 limbs, groups of 128, one : two workgroups, us: 128 -> 768
-// 62 : 53, 384 -> 384 70 : 61, 512 -> 512 102 : 90, 384 -> 1536 210 : 200; four waves alone at 768 ->
-// 768 209 against 197).
-constexpr int kWholeTiles = 2;
+// waves walk groups of kTiles row tiles without further synchronisation.  Two tiles a wave leave
+// registers for two waves a SIMD: one workgroup of eight waves a CU, or two of four where both strips fit
+// the LDS (640 inputs), so that one converts while the other contracts (2^14, 2 limbs, groups of 128, one : two
+// workgroups, us: 384 -> 384 70 : 61, 512 -> 512 102 : 90, 384 -> 1536 210 : 200; four waves alone at 768 ->
+// 768 209 against 197).  One tile a wave leaves them for four waves a SIMD, and four strips of up to 320 inputs
+// fit: there the fill counts for more than the residues' second reading.
 constexpr uint32_t kLdsBytes = 160 << 10;
-template <int kSteps, bool kZeros, int kWaves>
-__global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
+template <int kSteps, bool kZeros, int kWaves, int kTiles>
+__global__ __launch_bounds__(kWaves * 64, kTiles == 1 ? 4 : 2) void mac_q4_whole_kernel(
     Tables tb, const void* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
     uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
     uint32_t tiles, uint32_t splits) {
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
                             &job);
   const Modulus q = modulus(tb.q[at.limb]);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t groups = tiles / kWholeTiles, each = (groups + splits - 1) / splits;
+  const uint32_t groups = tiles / kTiles, each = (groups + splits - 1) / splits;
   const uint32_t end = min(groups, (at.split + 1) * each);
   constexpr int kPasses = 4;
   for (uint32_t b0 = 0; b0 < 2 * steps; b0 += kPasses * kWaves * 2) {
@@ -372,16 +372,16 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void mac_q4_whole_kernel(
     place<kPasses>(b0, 2 * steps, x, lds);
   }
   __syncthreads();
-  Ahead<kSteps, kZeros, kWholeTiles> next;
+  Ahead<kSteps, kZeros, kTiles> next;
   uint32_t rg = at.split * each + wave;
   if (rg >= end) return;
-  next.load(job, rg * kWholeTiles, 0);
+  next.load(job, rg * kTiles, 0);
   for (; rg < end; rg += kWaves) {
-    int64_t acc[kWholeTiles][16];
-    clear<kWholeTiles>(acc);
+    int64_t acc[kTiles][16];
+    clear<kTiles>(acc);
     const uint32_t after = rg + kWaves < end ? rg + kWaves : rg;
-    contract<kSteps, kZeros, kWholeTiles>(job, rg * kWholeTiles, 0, subs, after * kWholeTiles, 0, lds, next, acc);
-    store<kWholeTiles>(job, rg * kWholeTiles, q, acc);
+    contract<kSteps, kZeros, kTiles>(job, rg * kTiles, 0, subs, after * kTiles, 0, lds, next, acc);
+    store<kTiles>(job, rg * kTiles, q, acc);
   }
 }
 
@@ -431,6 +431,93 @@ __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
   if (mine) store<kDeepTiles>(job, tile, q, acc);
 }
 
+// Few outputs: a lane has one column and kThinRows rows, and four-byte dot products take the matrix
+// instructions' place, on the same operands: a lane's digits of 16 inputs, and weights that are the
+// same for all lanes and so come into scalar registers.  No LDS and small workgroups, so that many loads
+// are in flight: it is bound by memory up to 8 outputs (2^16, 4 limbs, 1 -> 8 outputs, us, groups of 128: 1 input
+// 13, 64 inputs 30 -> 33, 1024 inputs 430 -> 450, the inputs at 5.0 TB/s; 150, 155, 860 with a
+// matrix tile of 32 mostly empty rows).  A workgroup is 64 columns: `blocks` waves of eight rows each, times
+// `slices` shares of the sub-groups where the columns alone are too few waves; their sums meet in LDS.
+constexpr int kThinRows = 8, kThinWaves = 8, kThinCols = 64;
+template <int kSteps, bool kZeros>
+__global__ __launch_bounds__(kThinWaves * 64, 4) void mac_q4_thin_kernel(
+    Tables tb, const Frag<kZeros>* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
+    uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
+    uint32_t tiles, uint32_t blocks, uint32_t slices) {
+  extern __shared__ uint32_t sums[];  // with slices: [waves][kThinRows][kThinCols]
+  constexpr uint32_t kSub = kSteps * kStep, kFoldSubs = kFold / kSub;
+  const uint32_t n = tb.n, strips = 2 * n / kThinCols, l = blockIdx.x / strips, col0 = (blockIdx.x - l * strips) * kThinCols;
+  const uint32_t row_words = 2 * limbs * n, lane = threadIdx.x & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = wave / blocks, block = wave - slice * blocks;
+  const uint32_t row0 = block * kThinRows, tile = row0 / 32, r32 = row0 % 32;
+  const size_t at = (static_cast<size_t>(col0 >> tb.log_n) * limbs + l) * n + (col0 & (n - 1));
+  const Modulus q = modulus(tb.q[l]);
+  const int32_t c32 = centred(tb.pow256[l * 8 + 4], q.q);
+  const uint32_t each = (subs + slices - 1) / slices, sub0 = slice * each, sub1 = min(subs, sub0 + each);
+  int64_t acc[kThinRows];
+#pragma unroll
+  for (int r = 0; r < kThinRows; ++r) acc[r] = 0;
+  for (uint32_t g = sub0; g < sub1; ++g) {
+    if (g != sub0 && (g - sub0) % kFoldSubs == 0) {  // the sum so far, reduced, goes on as a product
+#pragma unroll
+      for (int r = 0; r < kThinRows; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
+    }
+    int32_t m[kThinRows][4];
+#pragma unroll
+    for (int r = 0; r < kThinRows; ++r)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) m[r][d] = 0;
+#pragma unroll 1
+    for (uint32_t b = 0; b < 2 * kSteps; ++b) {
+      const uint32_t base = g * kSub + b * 16;
+      if (base >= d_in) break;
+      const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint32_t*>(ct_in) + at + static_cast<size_t>(base) * row_words, 0,
+          static_cast<int>(min(d_in - base, 16u) * row_words * 4), kRsrcWord3);
+      uint32_t x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, (i * row_words + lane) * 4, 0, 0);
+      v4i f[4];
+      to_fragments(x, f);
+      const Frag<kZeros>* w = frag + (static_cast<size_t>(tile) * steps + g * kSteps + b / 2) * 64 + 32 * (b & 1) + r32;
+#pragma unroll
+      for (int r = 0; r < kThinRows; ++r) {
+        const v4i wr = unpack(w[r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) m[r][d] = __builtin_amdgcn_sdot4(f[d][e], wr[e], m[r][d], false);
+      }
+    }
+    const int2* sg = scales + ((static_cast<size_t>(l) * tiles + tile) * subs + g) * 32 + r32;
+#pragma unroll
+    for (int r = 0; r < kThinRows; ++r) {
+      acc[r] += static_cast<int64_t>(sg[r].x) * (m[r][0] + (m[r][1] << 8));
+      acc[r] += static_cast<int64_t>(sg[r].y) * (m[r][2] + (m[r][3] << 8));
+    }
+  }
+  uint32_t y[kThinRows];
+#pragma unroll
+  for (int r = 0; r < kThinRows; ++r) y[r] = reduce(acc[r], q);
+  if (slices > 1) {
+    if (slice != 0) {
+#pragma unroll
+      for (int r = 0; r < kThinRows; ++r) sums[(wave * kThinRows + r) * kThinCols + lane] = y[r];
+    }
+    __syncthreads();
+    if (slice != 0) return;
+    for (uint32_t k = 1; k < slices; ++k)
+#pragma unroll
+      for (int r = 0; r < kThinRows; ++r) {
+        const uint32_t v = y[r] + sums[((k * blocks + block) * kThinRows + r) * kThinCols + lane];
+        y[r] = min(v, v - q.q);
+      }
+  }
+#pragma unroll
+  for (int r = 0; r < kThinRows; ++r)
+    if (row0 + r < d_out) ct_out[at + static_cast<size_t>(row0 + r) * row_words + lane] = y[r];
+}
+
 template <int kSteps, bool kZeros>
 hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out,
                   uint32_t d_out, uint32_t d_in, uint32_t limbs, hipStream_t s) {
@@ -438,15 +525,37 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
   const void* frag = base;
   const int2* scales = reinterpret_cast<const int2*>(base + sh.frag_bytes);
   const uint32_t strips = 2 * t.n / kCols * limbs;  // column tiles of every limb
-  // Few rows leave most of a whole strip's waves idle behind its one conversion; the chunked
-  // kernel overlaps the two (2^14, 2 limbs, groups of 128, whole : chunked, us: 1024 -> 128 102 : 93, 256 -> 64
-  // 37 : 31, 256 -> 256 43.0 : 42.7, 1024 -> 384 158 : 166, 768 -> 768 196 : 239).
-  if (d_in <= kFold && d_out > 256) {  // at most 33 steps of 4 KiB
-    const uint32_t strip_bytes = sh.steps * kStepFrags * 16, waves = 2 * strip_bytes <= kLdsBytes ? 4 : 8;
+  // Enough columns for four strips a CU.  Below that every call takes 10 to 20 us, and the forms made for many
+  // strips lose up to half of it (2^12, 3 limbs, 256 -> 1: 17.8 us one row tile a wave, 12.8 chunked).
+  const bool many = strips >= 4 * t.num_cus;
+  // Dot products against a matrix tile (2^16, 4 limbs, groups of 128, us): 1024 -> 8 450 : 856, 64 -> 16 53 : 57, 256 ->
+  // 16 183 : 162, 32 -> 32 62 : 60, 4 -> 32 43 : 61, 4 -> 64 83 : 76.
+  if (many && (d_out <= kThinRows || (d_out <= 32 && d_in * d_out <= 1024))) {
+    const uint32_t cols = strips / (kThinCols / kCols), blocks = (d_out + kThinRows - 1) / kThinRows, want = t.num_cus * 16;
+    uint32_t slices = 1;
+    while (cols * blocks * slices < want && 2 * slices * blocks <= kThinWaves && 2 * slices <= sh.subs) slices *= 2;
+    mac_q4_thin_kernel<kSteps, kZeros>
+        <<<cols, blocks * slices * 64, slices > 1 ? blocks * slices * kThinRows * kThinCols * 4 : 0, s>>>(
+            t, static_cast<const Frag<kZeros>*>(frag), scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs, sh.tiles,
+            blocks, slices);
+    return hipGetLastError();
+  }
+  // 2^16, 4 limbs, groups of 128, us, one tile a wave : two : chunked: 4 -> 64 76 : 93 : 181, 256 -> 64 214 : 241 :
+  // 339, 256 -> 512 785 : 808, 512 -> 128 481 : 491 : 623, 512 -> 200 646 : 607 : 782, 512 -> 1024 (2^13, 3 limbs) 128 : 127.
+  // Past 640 inputs one strip fills a CU, and with few outputs most of its waves idle behind the one conversion: the
+  // chunked kernel overlaps the two (2^14, 2 limbs, whole : chunked, 1024 -> 128 102 : 93, 1024 -> 384 158 : 166,
+  // 768 -> 768 196 : 239).
+  const size_t strip_bytes = size_t(sh.steps) * kStepFrags * 16;
+  const bool four = 4 * strip_bytes <= kLdsBytes, two = 2 * strip_bytes <= kLdsBytes;  // strips that fit a CU
+  const bool one_tile = many && (four || (two && d_out <= 128));
+  if (one_tile || (d_in <= kFold && (d_out > 256 || (many && two)))) {
+    const uint32_t row_tiles = one_tile ? 1 : 2, waves = two ? 4 : 8;
+    const auto k = row_tiles == 1 ? mac_q4_whole_kernel<kSteps, kZeros, 4, 1>
+                   : two          ? mac_q4_whole_kernel<kSteps, kZeros, 4, 2>
+                                  : mac_q4_whole_kernel<kSteps, kZeros, 8, 2>;
     // Row splits only where the column strips alone leave CUs idle: each split converts the strip again.
-    const uint32_t groups = sh.tiles / kWholeTiles, blocks = (groups + waves - 1) / waves;
+    const uint32_t groups = sh.tiles / row_tiles, blocks = (groups + waves - 1) / waves;
     const uint32_t want = (t.num_cus * (8 / waves) + strips - 1) / strips, splits = want < blocks ? want : blocks;
-    const auto k = waves == 4 ? mac_q4_whole_kernel<kSteps, kZeros, 4> : mac_q4_whole_kernel<kSteps, kZeros, 8>;
     k<<<strips * splits, waves * 64, strip_bytes, s>>>(t, frag, scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs,
                                                       sh.tiles, splits);
   } else {

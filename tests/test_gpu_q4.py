@@ -89,6 +89,37 @@ def test_groups_of_three_steps(gpu_lib, d_in, group, zeros):
     check(gpu_lib, 10, 1, 300, d_in, group, zeros, 450 + d_in, rows=[0, 31, 64, 255, 299])
 
 
+MANY = 16   # limbs of 2^10 that make enough columns for the kernels of wide batches
+
+
+def check_many(ck, d_out, d_in, group, zeros, seed):
+    ctx = ctx_for(ck, 10, MANY)
+    w4, scales, z = layer(seed, d_out, d_in, group, zeros)
+    ct = gen.uniform_residues(np.random.default_rng(seed + 1), (d_in, 2), ctx.moduli, ctx.n)
+    got = run(ck, ctx, w4, scales, z, ct, d_out, group, 2.0 ** 26)
+    cols = [0, 31, 32, 63, 64, 500, 1023]
+    rows = list(range(d_out)) if d_out <= 32 else [0, 31, 32, d_out // 2, d_out - 1]
+    want = OQ.mac(w4, scales, z, ct[..., cols], group, 2.0 ** 26, ctx.moduli, rows=rows).astype(np.uint32)
+    assert np.array_equal(got[rows][..., cols], want)
+    assert np.all(got < np.array(ctx.moduli, np.uint32)[None, None, :, None])
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 96, 128])
+@pytest.mark.parametrize("d_in,d_out", [(1, 1), (16, 8), (17, 9), (33, 31), (113, 9), (300, 3), (1024, 8), (1025, 1), (2500, 7)])
+def test_few_outputs_of_many_columns(gpu_lib, d_in, d_out, group, zeros):
+    check_many(gpu_lib, d_out, d_in, group, zeros, 460 + d_in)
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 96, 128])
+@pytest.mark.parametrize("d_in,d_out", [(1, 33), (40, 64), (320, 70), (321, 128), (200, 300), (500, 129), (640, 257), (641, 200)])
+def test_short_inputs_of_many_columns(gpu_lib, d_in, d_out, group, zeros):
+    check_many(gpu_lib, d_out, d_in, group, zeros, 480 + d_in)
+
+
 @gpu
 @pytest.mark.parametrize("d_in,group", [(2048, 128), (2049, 64), (3072, 256), (4100, 32), (9000, 128), (2100, 2112)])
 @pytest.mark.parametrize("zeros", [False, True])
@@ -111,15 +142,16 @@ def test_fewer_limbs_than_the_context(gpu_lib):
 @pytest.mark.parametrize("group,d_in", [(32, 1024), (64, 1024), (128, 2048), (256, 1024), (256, 1300), (1024, 1024)])
 @pytest.mark.parametrize("residue", [0x3F7F7F7F, 0x3F7F7F80, None])
 @pytest.mark.parametrize("u,z", [(0, None), (15, None), (0, 15), (15, 0)])
-def test_the_largest_sums(gpu_lib, u, z, residue, group, d_in):
+@pytest.mark.parametrize("limbs", [1, MANY])
+def test_the_largest_sums(gpu_lib, u, z, residue, group, d_in, limbs):
     """Every input at an end of the digits' range (None: q - 1), every weight at an end of its, and a
     scale of +-8 units, whose sixteenth is the largest centred residue; and scales of 2^61."""
     ck = gpu_lib
-    ctx = ctx_for(ck, 10, 1)
-    q = ctx.moduli[0]
+    ctx = ctx_for(ck, 10, limbs)
     groups = -(-d_in // group)
-    ct = np.full((d_in, 2, 1, ctx.n), q - 1 if residue is None else residue, np.uint32)
-    assert ct.max() < q
+    top = np.array(ctx.moduli, np.uint32)[None, None, :, None] - 1
+    ct = np.broadcast_to(top if residue is None else np.uint32(residue), (d_in, 2, limbs, ctx.n)).copy()
+    assert np.all(ct <= top)
     scales = np.empty((4, groups), np.float32)
     scales[0], scales[1], scales[2], scales[3] = 8, -8, 1.75 * 2.0 ** 61, -(2.0 ** 62)
     w4 = OQ.pack(np.full((4, d_in), u))
@@ -141,7 +173,7 @@ def test_zero_points_count_four_bits(gpu_lib):
 
 
 @gpu
-@pytest.mark.parametrize("d_out,d_in,group,zeros", [(70, 1100, 128, False), (600, 1030, 64, True)])
+@pytest.mark.parametrize("d_out,d_in,group,zeros", [(70, 1100, 128, False), (600, 1030, 64, True), (6, 1100, 96, True), (1200, 30, 32, False)])
 def test_offsets_past_32_bits(gpu_lib, d_out, d_in, group, zeros):
     """Rows of 4 MiB: the inputs (and the outputs) pass 2^32 bytes; checked on a sample of columns."""
     import torch
