@@ -435,7 +435,7 @@ __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
 // instructions' place, on the same operands: a lane's digits of 16 inputs, and weights that are the
 // same for all lanes and so come into scalar registers.  No LDS and small workgroups, so that many loads
 // are in flight: it is bound by memory up to 8 outputs (2^16, 4 limbs, 1 -> 8 outputs, us, groups of 128: 1 input
-// 13, 64 inputs 30 -> 33, 1024 inputs 430 -> 450, the inputs at 5.0 TB/s; 150, 155, 860 with a
+// 13 -> 15, 64 inputs 30 -> 33, 1024 inputs 430 -> 450, 4.8 to 5.0 TB/s; 150, 155, 860 with a
 // matrix tile of 32 mostly empty rows).  A workgroup is 64 columns: `blocks` waves of eight rows each, times
 // `slices` shares of the sub-groups where the columns alone are too few waves; their sums meet in LDS.
 constexpr int kThinRows = 8, kThinWaves = 8, kThinCols = 64;
@@ -541,13 +541,14 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
     return hipGetLastError();
   }
   // 2^16, 4 limbs, groups of 128, us, one tile a wave : two : chunked: 4 -> 64 76 : 93 : 181, 256 -> 64 214 : 241 :
-  // 339, 256 -> 512 785 : 808, 512 -> 128 481 : 491 : 623, 512 -> 200 646 : 607 : 782, 512 -> 1024 (2^13, 3 limbs) 128 : 127.
+  // 339, 256 -> 512 785 : 808, 512 -> 128 481 : 491 : 623, 512 -> 200 646 : 607 : 782; 2^14, 4 limbs, one tile : two, 128 ->
+  // 320 55 : 66, 256 -> 512 147 : 151, 256 -> 1024 255 : 239, 64 -> 2048 314 : 287.
   // Past 640 inputs one strip fills a CU, and with few outputs most of its waves idle behind the one conversion: the
   // chunked kernel overlaps the two (2^14, 2 limbs, whole : chunked, 1024 -> 128 102 : 93, 1024 -> 384 158 : 166,
   // 768 -> 768 196 : 239).
   const size_t strip_bytes = size_t(sh.steps) * kStepFrags * 16;
   const bool four = 4 * strip_bytes <= kLdsBytes, two = 2 * strip_bytes <= kLdsBytes;  // strips that fit a CU
-  const bool one_tile = many && (four || (two && d_out <= 128));
+  const bool one_tile = many && ((four && d_out <= 512) || (two && d_out <= 128));
   if (one_tile || (d_in <= kFold && (d_out > 256 || (many && two)))) {
     const uint32_t row_tiles = one_tile ? 1 : 2, waves = two ? 4 : 8;
     const auto k = row_tiles == 1 ? mac_q4_whole_kernel<kSteps, kZeros, 4, 1>
