@@ -431,40 +431,41 @@ __global__ __launch_bounds__(kDeepWaves * 64, 1) void mac_q4_deep_kernel(
   if (mine) store<kDeepTiles>(job, tile, q, acc);
 }
 
-// Few outputs: a lane has one column and kThinRows rows, and four-byte dot products take the matrix
+// Few outputs: a lane has one column and kRows rows, and four-byte dot products take the matrix
 // instructions' place, on the same operands: a lane's digits of 16 inputs, and weights that are the
 // same for all lanes and so come into scalar registers.  No LDS and small workgroups, so that many loads
 // are in flight: it is bound by memory up to 8 outputs (2^16, 4 limbs, 1 -> 8 outputs, us, groups of 128: 1 input
 // 13 -> 15, 64 inputs 30 -> 33, 1024 inputs 430 -> 450, 4.8 to 5.0 TB/s; 150, 155, 860 with a
-// matrix tile of 32 mostly empty rows).  A workgroup is 64 columns: `blocks` waves of eight rows each, times
-// `slices` shares of the sub-groups where the columns alone are too few waves; their sums meet in LDS.
-constexpr int kThinRows = 8, kThinWaves = 8, kThinCols = 64;
-template <int kSteps, bool kZeros>
-__global__ __launch_bounds__(kThinWaves * 64, 4) void mac_q4_thin_kernel(
+// matrix tile of 32 mostly empty rows), by the dot products and the digits above.  Sixteen rows a lane for more
+// outputs share the digits (1024 -> 16: 600 us, 748 with eight).  A workgroup is 64 columns: `blocks` waves of kRows
+// rows each, times `slices` shares of the sub-groups where the columns alone are too few waves; their sums meet in LDS.
+constexpr int kThinWaves = 8, kThinCols = 64;
+template <int kSteps, bool kZeros, int kRows>
+__global__ __launch_bounds__(kThinWaves * 64, kRows == 8 ? 4 : 2) void mac_q4_thin_kernel(
     Tables tb, const Frag<kZeros>* __restrict__ frag, const int2* __restrict__ scales, const uint32_t* __restrict__ ct_in,
     uint32_t* __restrict__ ct_out, uint32_t d_out, uint32_t d_in, uint32_t limbs, uint32_t steps, uint32_t subs,
     uint32_t tiles, uint32_t blocks, uint32_t slices) {
-  extern __shared__ uint32_t sums[];  // with slices: [waves][kThinRows][kThinCols]
+  extern __shared__ uint32_t sums[];  // with slices: [waves][kRows][kThinCols]
   constexpr uint32_t kSub = kSteps * kStep, kFoldSubs = kFold / kSub;
   const uint32_t n = tb.n, strips = 2 * n / kThinCols, l = blockIdx.x / strips, col0 = (blockIdx.x - l * strips) * kThinCols;
   const uint32_t row_words = 2 * limbs * n, lane = threadIdx.x & 63;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = wave / blocks, block = wave - slice * blocks;
-  const uint32_t row0 = block * kThinRows, tile = row0 / 32, r32 = row0 % 32;
+  const uint32_t row0 = block * kRows, tile = row0 / 32, r32 = row0 % 32;
   const size_t at = (static_cast<size_t>(col0 >> tb.log_n) * limbs + l) * n + (col0 & (n - 1));
   const Modulus q = modulus(tb.q[l]);
   const int32_t c32 = centred(tb.pow256[l * 8 + 4], q.q);
   const uint32_t each = (subs + slices - 1) / slices, sub0 = slice * each, sub1 = min(subs, sub0 + each);
-  int64_t acc[kThinRows];
+  int64_t acc[kRows];
 #pragma unroll
-  for (int r = 0; r < kThinRows; ++r) acc[r] = 0;
+  for (int r = 0; r < kRows; ++r) acc[r] = 0;
   for (uint32_t g = sub0; g < sub1; ++g) {
     if (g != sub0 && (g - sub0) % kFoldSubs == 0) {  // the sum so far, reduced, goes on as a product
 #pragma unroll
-      for (int r = 0; r < kThinRows; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
+      for (int r = 0; r < kRows; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
     }
-    int32_t m[kThinRows][4];
+    int32_t m[kRows][4];
 #pragma unroll
-    for (int r = 0; r < kThinRows; ++r)
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
       for (int d = 0; d < 4; ++d) m[r][d] = 0;
 #pragma unroll 1
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 4) void mac_q4_thin_kernel(
       to_fragments(x, f);
       const Frag<kZeros>* w = frag + (static_cast<size_t>(tile) * steps + g * kSteps + b / 2) * 64 + 32 * (b & 1) + r32;
 #pragma unroll
-      for (int r = 0; r < kThinRows; ++r) {
+      for (int r = 0; r < kRows; ++r) {
         const v4i wr = unpack(w[r]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -491,30 +492,30 @@ __global__ __launch_bounds__(kThinWaves * 64, 4) void mac_q4_thin_kernel(
     }
     const int2* sg = scales + ((static_cast<size_t>(l) * tiles + tile) * subs + g) * 32 + r32;
 #pragma unroll
-    for (int r = 0; r < kThinRows; ++r) {
+    for (int r = 0; r < kRows; ++r) {
       acc[r] += static_cast<int64_t>(sg[r].x) * (m[r][0] + (m[r][1] << 8));
       acc[r] += static_cast<int64_t>(sg[r].y) * (m[r][2] + (m[r][3] << 8));
     }
   }
-  uint32_t y[kThinRows];
+  uint32_t y[kRows];
 #pragma unroll
-  for (int r = 0; r < kThinRows; ++r) y[r] = reduce(acc[r], q);
+  for (int r = 0; r < kRows; ++r) y[r] = reduce(acc[r], q);
   if (slices > 1) {
     if (slice != 0) {
 #pragma unroll
-      for (int r = 0; r < kThinRows; ++r) sums[(wave * kThinRows + r) * kThinCols + lane] = y[r];
+      for (int r = 0; r < kRows; ++r) sums[(wave * kRows + r) * kThinCols + lane] = y[r];
     }
     __syncthreads();
     if (slice != 0) return;
     for (uint32_t k = 1; k < slices; ++k)
 #pragma unroll
-      for (int r = 0; r < kThinRows; ++r) {
-        const uint32_t v = y[r] + sums[((k * blocks + block) * kThinRows + r) * kThinCols + lane];
+      for (int r = 0; r < kRows; ++r) {
+        const uint32_t v = y[r] + sums[((k * blocks + block) * kRows + r) * kThinCols + lane];
         y[r] = min(v, v - q.q);
       }
   }
 #pragma unroll
-  for (int r = 0; r < kThinRows; ++r)
+  for (int r = 0; r < kRows; ++r)
     if (row0 + r < d_out) ct_out[at + static_cast<size_t>(row0 + r) * row_words + lane] = y[r];
 }
 
@@ -528,16 +529,18 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
   // Enough columns for four strips a CU.  Below that every call takes 10 to 20 us, and the forms made for many
   // strips lose up to half of it (2^12, 3 limbs, 256 -> 1: 17.8 us one row tile a wave, 12.8 chunked).
   const bool many = strips >= 4 * t.num_cus;
-  // Dot products against a matrix tile (2^16, 4 limbs, groups of 128, us): 1024 -> 8 450 : 856, 64 -> 16 53 : 57, 256 ->
-  // 16 183 : 162, 32 -> 32 62 : 60, 4 -> 32 43 : 61, 4 -> 64 83 : 76.
-  if (many && (d_out <= kThinRows || (d_out <= 32 && d_in * d_out <= 1024))) {
-    const uint32_t cols = strips / (kThinCols / kCols), blocks = (d_out + kThinRows - 1) / kThinRows, want = t.num_cus * 16;
+  // Dot products against the matrix forms, us, groups of 128: 2^16, 4 limbs, 1024 -> 8 450 : 856, 64 -> 16 44 : 57, 256 ->
+  // 16 156 : 163, 1024 -> 16 600 : 875, 16 -> 32 35 : 52, 64 -> 32 77 : 66; 2^14, 4 limbs, 64 -> 16 15 : 17, 256 -> 16 47 :
+  // 28, 512 -> 16 89 : 61, 1024 -> 16 181 : 175 (groups of 32 196 : 261), 32 -> 32 16 : 18, 64 -> 32 25 : 17.
+  if (many && (d_out <= 8 || (d_out <= 16 && (d_in <= 64 || d_in > 640)) || (d_out <= 32 && d_in <= 32))) {
+    const uint32_t rows = d_out <= 8 ? 8 : 16, cols = strips / (kThinCols / kCols), blocks = (d_out + rows - 1) / rows;
+    const uint32_t want = t.num_cus * 16;
     uint32_t slices = 1;
     while (cols * blocks * slices < want && 2 * slices * blocks <= kThinWaves && 2 * slices <= sh.subs) slices *= 2;
-    mac_q4_thin_kernel<kSteps, kZeros>
-        <<<cols, blocks * slices * 64, slices > 1 ? blocks * slices * kThinRows * kThinCols * 4 : 0, s>>>(
-            t, static_cast<const Frag<kZeros>*>(frag), scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs, sh.tiles,
-            blocks, slices);
+    const auto k = rows == 8 ? mac_q4_thin_kernel<kSteps, kZeros, 8> : mac_q4_thin_kernel<kSteps, kZeros, 16>;
+    k<<<cols, blocks * slices * 64, slices > 1 ? blocks * slices * rows * kThinCols * 4 : 0, s>>>(
+        t, static_cast<const Frag<kZeros>*>(frag), scales, ct_in, ct_out, d_out, d_in, limbs, sh.steps, sh.subs, sh.tiles,
+        blocks, slices);
     return hipGetLastError();
   }
   // 2^16, 4 limbs, groups of 128, us, one tile a wave : two : chunked: 4 -> 64 76 : 93 : 181, 256 -> 64 214 : 241 :

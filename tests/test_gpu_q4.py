@@ -107,7 +107,7 @@ def check_many(ck, d_out, d_in, group, zeros, seed):
 @gpu
 @pytest.mark.parametrize("zeros", [False, True])
 @pytest.mark.parametrize("group", [32, 64, 96, 128])
-@pytest.mark.parametrize("d_in,d_out", [(1, 1), (16, 8), (17, 9), (33, 31), (113, 9), (300, 3), (1024, 8), (1025, 1), (2500, 7)])
+@pytest.mark.parametrize("d_in,d_out", [(1, 1), (16, 8), (17, 9), (31, 31), (64, 16), (300, 3), (700, 13), (1025, 1), (2500, 16)])
 def test_few_outputs_of_many_columns(gpu_lib, d_in, d_out, group, zeros):
     check_many(gpu_lib, d_out, d_in, group, zeros, 460 + d_in)
 
@@ -115,7 +115,7 @@ def test_few_outputs_of_many_columns(gpu_lib, d_in, d_out, group, zeros):
 @gpu
 @pytest.mark.parametrize("zeros", [False, True])
 @pytest.mark.parametrize("group", [32, 64, 96, 128])
-@pytest.mark.parametrize("d_in,d_out", [(1, 33), (40, 64), (320, 70), (321, 128), (200, 300), (500, 129), (640, 257), (641, 200)])
+@pytest.mark.parametrize("d_in,d_out", [(1, 33), (40, 64), (33, 31), (65, 9), (320, 70), (321, 128), (200, 300), (500, 129), (640, 257), (641, 200)])
 def test_short_inputs_of_many_columns(gpu_lib, d_in, d_out, group, zeros):
     check_many(gpu_lib, d_out, d_in, group, zeros, 480 + d_in)
 
