@@ -406,8 +406,8 @@ int ckks_cache_init(const ckks_ctx* ctx, const ckks_cache* cache, void* stream);
  * request i appends input rows row0[i] .. row0[i+1] - 1, or row i where row0 is
  * NULL.  Requests get the free pages with the lowest numbers, in request order.
  * A partly filled last page that other sequences hold too is copied first (its
- * filled rows); where every holder appends in this call the last request
- * keeps it in place.  If the free pages do not suffice for all requests that
+ * filled rows); where every holder appends in this call the request with the most
+ * rows on the page, of those the last, keeps it in place.  If the free pages do not suffice for all requests that
  * could be served, none is (CKKS_CACHE_NO_PAGES).
  *   row0  [count + 1], ascending, at most `rows` (else every request is bad); or NULL.
  *   rows_in  device uint32 [rows][row_cts][2][limbs][N]; must not overlap the cache.

@@ -79,20 +79,31 @@ class Cache:
             else:
                 status.append(OK)
         before = [a.copy() for a in (self.pool, self.refs, self.table, self.lens)]
+        keepers = self._keepers(seq, [range(*span) if st == OK else () for span, st in zip(spans, status)])
         try:
-            for s, span, st in zip(seq, spans, status):
+            for i, (s, span, st) in enumerate(zip(seq, spans, status)):
                 if st == OK:
                     for r in range(*span):
-                        self._append_row(s, rows[r])
+                        self._append_row(s, rows[r], i in keepers)
         except IndexError:  # no free page left: the call leaves the cache as it was
             self.pool, self.refs, self.table, self.lens = before
             status = [NO_PAGES if st == OK else st for st in status]
         return status
 
-    def _append_row(self, s: int, row) -> None:
+    def _keepers(self, seq, new_rows) -> set:
+        """Requests that write their last page in place though others hold it: where all of its holders
+        append, the one with the most rows on it, of those the last."""
+        writers = {}
+        for i, (s, r) in enumerate(zip(seq, new_rows)):
+            if len(r) and self.lens[s] % self.page_rows:
+                page = int(self.table[s, self.lens[s] // self.page_rows])
+                writers.setdefault(page, []).append((int(self.lens[s] % self.page_rows), i))
+        return {max(w)[1] for page, w in writers.items() if len(w) == self.refs[page]}
+
+    def _append_row(self, s: int, row, keeps: bool) -> None:
         at, slot = divmod(int(self.lens[s]), self.page_rows)
         page = self.table[s, at] if slot else -1
-        if page < 0 or self.refs[page] > 1:
+        if page < 0 or (self.refs[page] > 1 and not keeps):
             fresh = np.flatnonzero(self.refs == 0)[0]
             if page >= 0:
                 self.pool[fresh, :slot] = self.pool[page, :slot]

@@ -41,6 +41,11 @@ struct Request {
   uint32_t need;    // pages from the free ones, the copy's among them
 };
 __device__ __forceinline__ Request no_request() { return {kCacheBadRequest, 0, 0, 0, 0, 0, -1, 0, 0, 0}; }
+// Of the requests that write one shared page the highest rank has the most rows on it, and is the
+// last of those.
+__device__ __forceinline__ unsigned long long rank(uint32_t part, uint32_t i) {
+  return static_cast<unsigned long long>(part) << 32 | i;
+}
 // The first position of the sequence's table that gets a page.
 __device__ __forceinline__ uint32_t first_new(const Request& r) { return r.at + (r.part != 0 && !r.copy); }
 
@@ -52,7 +57,7 @@ struct Plan {
   int32_t* movers;    // compact: pages that move
   int32_t* to;        // compact: [pages] new page, -1 where it stays
   int32_t* sharers;   // append: [pages] requests that would write a shared last page
-  int32_t* last;      // append: [pages] the highest of them
+  unsigned long long* keeper;  // append: [pages] the highest rank (rank()) among them
   Request* requests;  // append: [count]
 };
 
@@ -70,14 +75,14 @@ size_t append_layout(const Cache& c, uint32_t count, uint32_t rows, uint8_t* bas
   size_t at = 0;
   const size_t o_n = take(at, 4), o_m = take(at, append_moves(c, count, rows) * sizeof(Move));
   const size_t o_f = take(at, size_t(c.pages) * 4), o_s = take(at, size_t(c.pages) * 4);
-  const size_t o_l = take(at, size_t(c.pages) * 4), o_r = take(at, size_t(count) * sizeof(Request));
+  const size_t o_k = take(at, size_t(c.pages) * 8), o_r = take(at, size_t(count) * sizeof(Request));
   if (p) {
     *p = Plan{};
     p->moves_n = reinterpret_cast<uint32_t*>(base + o_n);
     p->moves = reinterpret_cast<Move*>(base + o_m);
     p->fresh = reinterpret_cast<int32_t*>(base + o_f);
     p->sharers = reinterpret_cast<int32_t*>(base + o_s);
-    p->last = reinterpret_cast<int32_t*>(base + o_l);
+    p->keeper = reinterpret_cast<unsigned long long*>(base + o_k);
     p->requests = reinterpret_cast<Request*>(base + o_r);
   }
   return at;
@@ -111,7 +116,8 @@ __device__ __forceinline__ int32_t held_rows(const Cache& c, int32_t s) {
   return n < 0 ? 0 : n < most ? n : static_cast<int32_t>(most);
 }
 
-__device__ __forceinline__ int32_t fresh_load(const int32_t* p) {
+template <class T>
+__device__ __forceinline__ T fresh_load(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -254,6 +260,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
   __shared__ Request reqs[kPlanThreads];
   __shared__ uint32_t page0[kPlanThreads], copy0[kPlanThreads];
   __shared__ __align__(16) int32_t pages[kPlanThreads];  // shared pages of the requests, then the first free pages
+  __shared__ __align__(16) uint32_t parts[kPlanThreads];  // rows on the shared pages
   const uint32_t tid = threadIdx.x, P = c.page_rows;
   const uint32_t blocks = kFew ? 1 : (count + kPlanThreads - 1) / kPlanThreads;  // of requests
   const int32_t holders0 = tid < c.pages ? c.refs[tid] : 1;  // of the first pages, looked at further down
@@ -299,11 +306,12 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
       r.why = kCacheOk;
   };
   auto sharing = [](const Request& r) { return r.why == kCacheOk && r.holders > 1; };
-  // Where every holder of a shared page is in the call, the last of them keeps it; the
-  // others copy it.  Then the pages that the request takes.
-  auto settle = [&](Request& r, uint32_t i, int32_t sharers, int32_t last) {
+  // Where every holder of a shared page is in the call, the one of the highest rank keeps it; the
+  // others copy it.  None of them copies a row that the keeper writes: it has as many rows or more
+  // on the page, and writes past them (the moves run in no order).  Then the pages that the request takes.
+  auto settle = [&](Request& r, uint32_t i, int32_t sharers, unsigned long long keeper) {
     if (r.why != kCacheOk) return;
-    r.copy = r.holders > 1 && !(sharers == r.holders && last == static_cast<int32_t>(i));
+    r.copy = r.holders > 1 && !(sharers == r.holders && keeper == rank(r.part, i));
     r.need = r.at + (r.part + r.want + P - 1) / P - first_new(r);
   };
   auto needs = [](const Request& r) { return make_uint2(r.need, r.copy ? r.part : 0); };  // pages, rows to copy
@@ -311,17 +319,27 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
   if (tid < count) judge(mine);
   if constexpr (kFew) {
     pages[tid] = sharing(mine) ? mine.last : -1;
+    parts[tid] = mine.part;
     __syncthreads();
-    int32_t sharers = 0, last = -1;
+    int32_t sharers = 0;
+    uint32_t most = 0, keeper = 0;
     if (sharing(mine)) {
+      auto meet = [&](int32_t page, uint32_t part, uint32_t j) {
+        const bool same = page == mine.last, ahead = same && part >= most;
+        sharers += same;
+        most = ahead ? part : most;
+        keeper = ahead ? j : keeper;
+      };
       for (uint32_t j = 0; j < count; j += 4) {  // `pages` is padded with -1
         const int4 v = *reinterpret_cast<const int4*>(&pages[j]);
-        const bool x = v.x == mine.last, y = v.y == mine.last, z = v.z == mine.last, w = v.w == mine.last;
-        sharers += x + y + z + w;
-        last = w ? j + 3 : z ? j + 2 : y ? j + 1 : x ? j : last;
+        const uint4 n = *reinterpret_cast<const uint4*>(&parts[j]);
+        meet(v.x, n.x, j);
+        meet(v.y, n.y, j + 1);
+        meet(v.z, n.z, j + 2);
+        meet(v.w, n.w, j + 3);
       }
     }
-    settle(mine, tid, sharers, last);
+    settle(mine, tid, sharers, rank(most, keeper));
     mine0 = scan(needs(mine), lds, &total);
     reqs[tid] = mine;
     if (status && tid < count && mine.why != kCacheOk) status[tid] = mine.why;
@@ -330,7 +348,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
       Request r = look_up(i);
       judge(r);
       p.requests[i] = r;
-      if (sharing(r)) p.sharers[r.last] = 0, p.last[r.last] = -1;
+      if (sharing(r)) p.sharers[r.last] = 0, p.keeper[r.last] = 0;
     }
     __threadfence();  // the stores are in memory before the atomics on the same words
     __syncthreads();
@@ -338,7 +356,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
       const Request r = p.requests[i];
       if (!sharing(r)) continue;
       atomicAdd(&p.sharers[r.last], 1);
-      atomicMax(&p.last[r.last], static_cast<int32_t>(i));
+      atomicMax(&p.keeper[r.last], rank(r.part, i));
     }
     __syncthreads();
     for (uint32_t b = 0; b < blocks; ++b) {
@@ -346,7 +364,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_append_plan_kernel(
       Request r = no_request();
       if (i < count) {
         r = p.requests[i];
-        settle(r, i, sharing(r) ? fresh_load(&p.sharers[r.last]) : 0, sharing(r) ? fresh_load(&p.last[r.last]) : 0);
+        settle(r, i, sharing(r) ? fresh_load(&p.sharers[r.last]) : 0, sharing(r) ? fresh_load(&p.keeper[r.last]) : 0);
         p.requests[i] = r;
         if (status && r.why != kCacheOk) status[i] = r.why;
       }

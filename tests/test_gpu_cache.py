@@ -8,6 +8,7 @@ import pytest
 
 from oracle import cache as OC
 from oracle import rlwe as OR
+from tests import cache_drafts
 from workloads import gen
 
 gpu = pytest.mark.gpu
@@ -378,6 +379,50 @@ def test_sizes_whose_product_passes_64_bits_are_refused(gpu_lib):
     with pytest.raises(ck.CkksError) as e:
         ck.ckks_cache_free(ctx, c, ints(ck, [0])[:0])
     assert e.value.code == ck.CKKS_E_INVALID_ARG and "too large" in ck.ckks_last_error()
+
+
+@gpu
+@pytest.mark.parametrize("crowd", [0, 1100])
+@pytest.mark.parametrize("order", [[0, 1, 2], [0, 2, 1], [2, 1, 0], [1, 0, 2]])
+def test_holders_of_unlike_lengths(gpu_lib, order, crowd):
+    """Holders of 5, 1 and 3 rows on one page append in one call, alone and among more requests than one
+    workgroup has threads: the longest keeps the page, and the others copy rows that nobody writes."""
+    rng = np.random.default_rng(20)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 10 + crowd, 6, 1, 1, 3 + crowd, 3)
+    p.append([0], some_rows(rng, 11, 1, 1, 1024), [0, 11])
+    p.fork([0, 0], [1, 2])
+    p.free([1, 2], [7, 9])
+    page, before = p.ref.table[0, 1], p.ref.table.copy()
+    who = order[:2] + list(range(3, 3 + crowd)) + order[2:]
+    counts = [3] * 2 + [1] * crowd + [2]
+    row0 = np.concatenate([[0], np.cumsum(counts)])
+    assert set(p.append(who, some_rows(rng, int(row0[-1]), 1, 1, 1024), row0)) == {0}
+    assert p.ref.table[0, 1] == page and p.ref.refs[page] == 1
+    assert not cache_drafts.clashes([11, 7, 9] + [0] * crowd, before, p.ref.table, 6, who, counts)
+    p.same()
+    p.gather([0] * 14 + [1] * 10 + [2] * 12, list(range(14)) + list(range(10)) + list(range(12)))
+
+
+@gpu
+@pytest.mark.parametrize("page_rows", [3, 4, 5, 8])
+def test_drafts(gpu_lib, page_rows):
+    """Speculative decoding's fork, cut back and append together; every array compared after each call."""
+    rng, data = np.random.default_rng(30 + page_rows), np.random.default_rng(50 + page_rows)
+    p = Pair(gpu_lib, ctx_for(gpu_lib, 10, 3), 40, page_rows, 1, 1, cache_drafts.SEQS, 6)
+    kept = unlike = 0
+    for name, *args in cache_drafts.calls(rng, 60, page_rows):
+        if name == "append":
+            seq, counts = args
+            k, u = cache_drafts.shared_last_pages(p.ref.lens, p.ref.table, p.ref.refs, page_rows, seq, counts)
+            kept, unlike = kept + k, unlike + u
+            row0 = np.concatenate([[0], np.cumsum(counts)])
+            p.append(seq, some_rows(data, int(row0[-1]), 1, 1, 1024), row0)
+        elif args and not args[0]:
+            continue                                   # nobody is cut back
+        else:
+            getattr(p, name)(*args)
+        p.same()
+    assert kept >= 10 and unlike >= 5
 
 
 def test_null_context_is_rejected_without_a_gpu():

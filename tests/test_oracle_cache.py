@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import cache as OC
+from tests import cache_drafts
 
 
 def rows_of(c, s):
@@ -74,3 +75,51 @@ def test_a_row_that_is_not_there_gathers_as_zeros():
     c = OC.Cache(2, 2, (1,), 2, 2)
     c.append([0], np.array([[7]], np.uint32))
     assert c.gather([0, 0, 0, 1, -1, 2], [0, 1, -1, 0, 0, 0])[:, 0].tolist() == [7, 0, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("order", [[0, 1, 2], [0, 2, 1], [2, 1, 0], [1, 0, 2]])
+def test_the_longest_of_all_holders_keeps_a_shared_page(order):
+    """Holders of 3, 1 and 2 rows on one page: none of the rows that the others copy is written in the call."""
+    c = OC.Cache(8, 4, (1,), 3, 2)
+    c.append([0], np.array([[10], [11], [12]], np.uint32), [0, 3])
+    c.fork([0, 0], [1, 2])
+    c.free([1, 2], [1, 2])
+    page, before = c.table[0, 0], c.table.copy()
+    assert c.append(order, np.array([[100 + s] for s in order], np.uint32)) == [OC.OK] * 3
+    assert c.table[0, 0] == page and c.refs[page] == 1
+    assert [rows_of(c, s) for s in range(3)] == [[10, 11, 12, 100], [10, 101], [10, 11, 102]]
+    assert not cache_drafts.clashes([3, 1, 2], before, c.table, 4, order, [1] * 3)
+
+
+@pytest.mark.parametrize("page_rows", [3, 4, 5, 8])
+def test_drafts_against_lists(page_rows):
+    rng = np.random.default_rng(30 + page_rows)
+    c = OC.Cache(40, page_rows, (1,), cache_drafts.SEQS, 6)
+    lists = [[] for _ in range(cache_drafts.SEQS)]
+    fresh, kept, unlike = 1, 0, 0
+    for name, *args in cache_drafts.calls(rng, 60, page_rows):
+        if name == "append":
+            seq, counts = args
+            row0 = np.concatenate([[0], np.cumsum(counts)])
+            rows = np.arange(fresh, fresh + row0[-1], dtype=np.uint32)[:, None]
+            fresh += int(row0[-1])
+            lens, table = c.lens.copy(), c.table.copy()
+            k, u = cache_drafts.shared_last_pages(lens, table, c.refs, page_rows, seq, counts)
+            kept, unlike = kept + k, unlike + u
+            assert c.append(seq, rows, row0) == [OC.OK] * len(seq)
+            assert not cache_drafts.clashes(lens, table, c.table, page_rows, seq, counts)
+            for i, s in enumerate(seq):
+                lists[s] += rows[row0[i]:row0[i + 1], 0].tolist()
+        elif name == "fork":
+            assert c.fork(*args) == [OC.OK] * len(args[0])
+            for s, d in zip(*args):
+                lists[d] = list(lists[s])
+        elif name == "free":
+            assert c.free(*args) == [OC.OK] * len(args[0])
+            for i, s in enumerate(args[0]):
+                lists[s] = lists[s][: args[1][i] if args[1] else 0]
+        else:
+            c.compact()
+        check_holders(c)
+        assert [rows_of(c, s) for s in range(cache_drafts.SEQS)] == lists
+    assert kept >= 10 and unlike >= 5
