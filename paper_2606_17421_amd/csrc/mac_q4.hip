@@ -61,7 +61,7 @@ struct Shape {
 Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t group, uint32_t limbs, bool zeros) {
   Shape s;
   s.tiles = (d_out + kPadRows - 1) / kPadRows * (kPadRows / 32);
-  s.groups = (d_in + group - 1) / group;
+  s.groups = (d_in - 1) / group + 1;  // a group may end past 2^32
   if (s.groups == 1)
     s.sub_len = d_in <= 32 ? 32 : d_in <= 64 ? 64 : d_in <= 96 ? 96 : 128;
   else

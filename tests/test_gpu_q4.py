@@ -306,3 +306,16 @@ def test_null_context_is_rejected_without_a_gpu():
     assert lib.ckks_linear_mac_q4(None, None, None, None, 1, 1, 32, 1, 0, None) == ck.CKKS_E_INVALID_ARG
     assert lib.ckks_linear_encode_q4(None, None, None, None, 1, 1, 32, 1, 1.0, None, None) == ck.CKKS_E_INVALID_ARG
     assert lib.ckks_q4_weight_bytes(None, 1, 1, 32, 1, 0) == ctypes.c_size_t(-1).value
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("d_in,group", [(64, 0xFFFFFFE0), (33, 0xFFFFFFE0), (200, 0xFFFFFF80), (1100, 0xFFFFFFE0), (70, 1 << 31)])
+def test_groups_far_longer_than_the_layer(gpu_lib, d_in, group, zeros):
+    """A group that ends past 2^32 inputs is one scale and zero point a row, as one of the layer's length is."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    for kind in (False, True):
+        assert ck.ckks_q4_weight_bytes(ctx, 5, d_in, group, 2, kind) == \
+            ck.ckks_q4_weight_bytes(ctx, 5, d_in, -(-d_in // 32) * 32, 2, kind)
+    check(ck, 10, 2, 5, d_in, group, zeros, 570 + d_in)
