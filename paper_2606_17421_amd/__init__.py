@@ -124,7 +124,10 @@ def _stream(stream):
     if stream is None:
         # the current device's current stream, without the Stream object that
         # torch.cuda.current_stream() builds (2.5 us a call, as long as a launch)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        try:
+            return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        except AttributeError:      # not part of torch's public interface
+            stream = torch.cuda.current_stream()
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
