@@ -179,10 +179,16 @@ int ckks_linear_mac_scalar_noalloc(const ckks_ctx* ctx, const uint32_t* w_enc,
  * w[j][i] = scales[j][i / group] (u[j][i] - z[j][i / group]), z = 8 without
  * zero points.  The plaintext of a weight is (u - z) rint(scales * scale), rint
  * rounding half to even: the scale is rounded once and the small integer kept,
- * within 15/2 of the rounding of each product.  Encoded weights take 1/2 byte
- * (1 byte with zero points) and 8 limbs / s bytes a weight, s the largest of 128,
- * 96, 64 and 32 that divides the group, against 4 limbs bytes for
- * ckks_linear_encode_scalar's, so layers stay resident (section 4.2) that did not.
+ * within 15/2 of the unrounded product and within 8 of its rounding (4 of both
+ * without zero points).
+ *
+ * Encoded weights take 1/2 byte (1 byte with zero points) a weight and 8 limbs
+ * bytes a row and s inputs, with rows padded to a multiple of 64 and inputs to a multiple
+ * of s: the largest of 128, 96, 64 and 32 that divides the group; where one group holds
+ * every input, the smallest of 32, 64, 96 and 128 that holds them, or 128.  Against the
+ * 4 limbs bytes a weight of ckks_linear_encode_scalar that is, from four limbs on, an
+ * eighth or less for layers of many outputs; a layer of few outputs pays for the padding
+ * (1 x 128 at two limbs: 5120 bytes against 1024).
  *
  * group is a positive multiple of 32 (the last group of a row may be shorter;
  * one scale a row: d_in rounded up to a multiple of 32). */

@@ -319,3 +319,19 @@ def test_groups_far_longer_than_the_layer(gpu_lib, d_in, group, zeros):
         assert ck.ckks_q4_weight_bytes(ctx, 5, d_in, group, 2, kind) == \
             ck.ckks_q4_weight_bytes(ctx, 5, d_in, -(-d_in // 32) * 32, 2, kind)
     check(ck, 10, 2, 5, d_in, group, zeros, 570 + d_in)
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("limbs", [1, 2])
+def test_weight_bytes_are_as_declared(gpu_lib, limbs, zeros):
+    """The header's formula: padded rows times padded inputs, and a pair of scales a row and s inputs."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    assert ck.ckks_q4_weight_bytes(ctx, 1, 128, 128, 2) == 5120
+    for d_out, d_in, group, s in [(1, 128, 128, 128), (64, 768, 128, 128), (65, 769, 96, 96), (100, 200, 192, 96), (7, 300, 320, 128),
+                                  (7, 33, 320, 64), (7, 70, 320, 96), (7, 5, 32, 32), (513, 1021, 32, 32), (3, 500, 320, 64),
+                                  (3, 900, 160, 32)]:
+        rows, inputs = -(-d_out // 64) * 64, -(-d_in // s) * s
+        want = rows * inputs // (1 if zeros else 2) + 8 * limbs * rows * (inputs // s)
+        assert ck.ckks_q4_weight_bytes(ctx, d_out, d_in, group, limbs, zeros) == want, (d_out, d_in, group)

@@ -49,3 +49,18 @@ def test_scales_beyond_a_prime():
     p = q4.plaintexts(q4.pack([[15]]), np.array([[1.0]], np.float32), None, 1, 32, 2.0 ** 62)
     assert p[0, 0] == 7 << 62
     assert q4.residues(p, qs)[0, 0, 0] == (7 << 62) % qs[0]
+
+
+@pytest.mark.parametrize("zeros,from_product,from_rounding", [(True, 7.5, 8), (False, 4, 4)])
+def test_distance_to_the_rounded_products(zeros, from_product, from_rounding):
+    """The scale is rounded before the product: at most half a unit times the small integer, and a
+    rounding more; scaled scales of halves reach both."""
+    u = np.arange(16).reshape(16, 1)
+    far = [0.0, 0.0]
+    for z in range(16) if zeros else (8,):
+        for s in (0.5, 1.5, 2.49, 0.25, 1000.5):
+            p = q4.plaintexts(q4.pack(u), np.full((16, 1), s, np.float32), np.full((16, 1), z, np.uint8) if zeros else None,
+                              1, 32, 1.0).astype(float)
+            product = (u - z) * np.float64(np.float32(s))
+            far = [max(far[0], abs(p - product).max()), max(far[1], abs(p - np.rint(product)).max())]
+    assert far == [from_product, from_rounding]
