@@ -335,3 +335,39 @@ def test_weight_bytes_are_as_declared(gpu_lib, limbs, zeros):
         rows, inputs = -(-d_out // 64) * 64, -(-d_in // s) * s
         want = rows * inputs // (1 if zeros else 2) + 8 * limbs * rows * (inputs // s)
         assert ck.ckks_q4_weight_bytes(ctx, d_out, d_in, group, limbs, zeros) == want, (d_out, d_in, group)
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 96, 128])
+@pytest.mark.parametrize("d_out", [7, 16])
+def test_few_outputs_of_deep_layers_in_one_slice(gpu_lib, d_out, group, zeros):
+    """Columns enough that one wave goes through all inputs, so that it reduces its sums twice on the
+    way: random layers and the largest sums, checked on a sample of columns."""
+    import torch
+    ck = gpu_lib
+    limbs, d_in = 8, 2100
+    ctx = ctx_for(ck, 14, limbs)
+    w4, scales, z = layer(580 + group, d_out, d_in, group, zeros)
+    g = torch.Generator(device="cuda").manual_seed(group)
+    ct = torch.empty((d_in, 2, limbs, ctx.n), dtype=torch.int32, device="cuda")
+    for l, q in enumerate(ctx.moduli):
+        ct[:, :, l] = torch.randint(0, q, (d_in, 2, ctx.n), generator=g, device="cuda", dtype=torch.int32)
+    out = ck.empty_u32((d_out, 2, limbs, ctx.n))
+    cols = torch.tensor([0, 1, 63, 64, 9000, 16383], device="cuda")
+
+    def compare(w4, scales, z, scale):
+        enc = encode(ck, ctx, w4, scales, z, d_out, d_in, group, limbs, scale)
+        out.fill_(-1)
+        ck.ckks_linear_mac_q4(ctx, enc, ct, out, d_out, d_in, group, limbs, zeros)
+        got = out[..., cols].cpu().numpy().view(np.uint32)
+        part = ct[..., cols].cpu().numpy().view(np.uint32)
+        assert np.array_equal(got, OQ.mac(w4, scales, z, part, group, scale, ctx.moduli).astype(np.uint32))
+    compare(w4, scales, z, 2.0 ** 26)
+    ends = np.full_like(scales, 8)
+    ends[1::2] = -8
+    for residue in (0x3F7F7F7F, 0x3F7F7F80):
+        assert residue < min(ctx.moduli)
+        ct.fill_(residue)
+        for u in (0, 15):
+            compare(OQ.pack(np.full((d_out, d_in), u)), ends, np.full_like(z, 15 - u) if zeros else None, 1.0)
