@@ -11,15 +11,17 @@
 // integers: T = a + 2^16 b with a and b from two digits each, and the sum over g of
 // (S mod q) a + (2^16 S mod q) b is reduced once an output.
 //
-// What bounds it: the vector unit.  Beside each 32-cycle v_mfma_i32_32x32x32_i8 run a shift-add
-// and a 64-bit multiply-add for every output of a sub-group and digit pair (4 vector
+// What bounds the large layers: issue, for four fifths of the cycles.  Beside each 32-cycle v_mfma_i32_32x32x32_i8
+// run a shift-add and a 64-bit multiply-add for every output of a sub-group and digit pair (4 vector
 // operations a matrix operation at groups of 128, 8 at 64, 16 at 32), the unpacking (1.5) and
 // the closing reduction (1.2 at 768 inputs); at about 4.3 cycles each (8.8 the multiply-add), and
 // 8.5 issue cycles a matrix operation, they take longer than the matrix pipe, which is busy 52% of
-// the cycles at 768 -> 3072 (groups of 128, N = 2^15, 6 limbs: 3.71 ms, 1.0e15 int8 products/s), and
-// the chip holds 1.7 GHz under both (2.05 GHz and the same cycles with zero residues).  Of a whole
-// strip's time the fill comes on top: at 2^14 and 4 limbs 768 -> 768 takes 368 us, 79 of them with the matrix
-// cores idle.  Measured without effect: contractions and combinations interleaved by hand, fragments
+// the cycles at 768 -> 3072 (groups of 128, N = 2^15, 6 limbs: 3.70 to 3.78 ms, 1.0e15 int8 products/s), and
+// the chip holds 1.7 GHz under both (2.05 GHz and the same cycles with zero residues).  The other fifth is
+// waiting: for a row group's stores (contract()) and for the fill of a strip, at 2^14 and 4 limbs 79 of the 370 us of
+// 768 -> 768, with the matrix cores idle.  At a few hundred inputs and outputs of wide batches these two
+// weigh most: 256 -> 512 at 2^16 and 4 limbs takes 734 us, more than its products at the large layers' rate (277) and
+// its bytes (340) one after the other.  Measured without effect: contractions and combinations interleaved by hand, fragments
 // read ahead, three or four waves a SIMD with half the rows, 64-byte stores after a transpose over
 // lanes.  One combination for two sub-groups that share a scale (groups of 256 and more) gave 1-3%,
 // int8 fragments instead of 4-bit ones 4% for twice the memory; touching the next strip's lines before the
@@ -36,11 +38,12 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256;        // encode kernels
 constexpr uint32_t kStep = 32;       // inputs of one matrix-core step
 constexpr uint32_t kCols = 32;       // columns of a workgroup
-constexpr uint32_t kPadRows = 64;    // output rows are padded to this
+constexpr uint32_t kPadRows = 64;    // output rows are padded to this: two tiles a wave (one-tile waves contract the padding's zeros)
 constexpr int kStepFrags = 4 * 64;   // 16-byte residue fragments of a step: four digits, 64 lanes
 constexpr uint32_t kFold = 1024;     // most inputs between reductions of the 64-bit sums
 
-// Encoded weights:
+// Encoded weights (written once a layer by two short kernels, the launches of which are most of their time: 8 to 9 us for
+// 768 -> 768 and smaller, 17 us for 1024 -> 6144 at 8 limbs, whose bytes take 2):
 //   fragments [tile][step][64 lanes] of row tile*32 + lane%32 and inputs step*32 + 16
 //     (lane/32) + i, i < 16; rows are padded to kPadRows, steps to whole sub-groups.
 //     Without zero points 8 bytes: v = u - 8 in four bits, two's complement.  Word d holds i =
@@ -220,9 +223,11 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
-// A wave's next weights and scales: of one sub-group of kTiles row tiles, loaded a sub-group
-// ahead and across row groups and chunks (768 -> 3072, groups of 128: 3.78 -> 3.69 ms against a fresh start
-// a row group; 3072 -> 768 1.53 -> 1.45 ms).
+// A wave's next weights and scales: of one sub-group of kTiles row tiles, asked for before the sub-group ahead of it
+// is combined, and across row groups and chunks (768 -> 3072, groups of 128: 3.78 -> 3.69 ms against a
+// fresh start a row group; 3072 -> 768 1.53 -> 1.45 ms).  The source asks first thing, but the compiler places the
+// loads behind 27 of the 32 matrix operations of a sub-group of 128 and two row tiles (7 of 8 of the chunked kernel's at
+// 64), so what covers them is the combination.
 template <int kSteps, bool kZeros, int kTiles>
 struct Ahead {
   Frag<kZeros> raw[kSteps][kTiles];
@@ -286,8 +291,9 @@ __device__ __forceinline__ void contract(const Job& job, uint32_t tile0, uint32_
       }
     }
   };
-  // The shortest sub-groups' first one stands before the loop: its weights came before the last outputs'
-  // stores, and the loop's wait would cover those too (768 -> 3072, groups of 32: 6.40 -> 6.17 ms; longer
+  // Loads and stores share one counter, which the loop waits down to zero: the first sub-group of a row
+  // group waits for the last outputs' stores too.  For the shortest sub-groups it stands before the loop, with a wait
+  // of its own for weights that came before those stores (768 -> 3072, groups of 32: 6.40 -> 6.17 ms; longer
   // sub-groups lose more to registers: groups of 128 3.69 -> 4.02 ms).
   uint32_t g = 0;
   if constexpr (kSteps == 1) body(g++);
@@ -350,7 +356,8 @@ __device__ __forceinline__ Place place_of(const Tables& tb, const void* frag, co
 // the LDS (640 inputs), so that one converts while the other contracts (2^14, 2 limbs, groups of 128, one : two
 // workgroups, us: 384 -> 384 70 : 61, 512 -> 512 102 : 90, 384 -> 1536 210 : 200; four waves alone at 768 ->
 // 768 209 against 197).  One tile a wave leaves them for four waves a SIMD, and four strips of up to 320 inputs
-// fit: there the fill counts for more than the residues' second reading.
+// fit: there the fill counts for more than the residues' second reading.  Three instances with zero points spill
+// one register: both of two tiles in groups of 128, and one tile in groups of 96.
 constexpr uint32_t kLdsBytes = 160 << 10;
 template <int kSteps, bool kZeros, int kWaves, int kTiles>
 __global__ __launch_bounds__(kWaves * 64, kTiles == 1 ? 4 : 2) void mac_q4_whole_kernel(
@@ -531,7 +538,8 @@ hipError_t launch(const Tables& t, const Shape& sh, const void* w_q4, const uint
   const bool many = strips >= 4 * t.num_cus;
   // Dot products against the matrix forms, us, groups of 128: 2^16, 4 limbs, 1024 -> 8 450 : 856, 64 -> 16 44 : 57, 256 ->
   // 16 156 : 163, 1024 -> 16 600 : 875, 16 -> 32 35 : 52, 64 -> 32 77 : 66; 2^14, 4 limbs, 64 -> 16 15 : 17, 256 -> 16 47 :
-  // 28, 512 -> 16 89 : 61, 1024 -> 16 181 : 175 (groups of 32 196 : 261), 32 -> 32 16 : 18, 64 -> 32 25 : 17.
+  // 28, 512 -> 16 89 : 61, 1024 -> 16 181 : 175 (groups of 32 196 : 261), 32 -> 32 16 : 18, 64 -> 32 25 : 17.  From 65 to
+  // 640 inputs the two rings differ for 9 to 16 outputs: the matrix form loses 4% at 2^16 and wins 40% at 2^14.
   if (many && (d_out <= 8 || (d_out <= 16 && (d_in <= 64 || d_in > 640)) || (d_out <= 32 && d_in <= 32))) {
     const uint32_t rows = d_out <= 8 ? 8 : 16, cols = strips / (kThinCols / kCols), blocks = (d_out + rows - 1) / rows;
     const uint32_t want = t.num_cus * 16;
