@@ -33,23 +33,23 @@ LARGEST = 448.0         # of e4m3
 def listed():
     return [
         # The smallest layer, 16 features in a ring of 2^10: launch and latency.
-        dict(name="fp8-16x16-n10", kind="fp8", log_n=10, limbs=2, log_scale=34, d_in=16, d_out=16, block_rows=128),
+        dict(name="fp8-16x16-n10", kind="fp8", log_n=10, limbs=2, log_scale=30, d_in=16, d_out=16, block_rows=128),
         # A router's scores: one output an expert.
-        dict(name="fp8-1024x16-n13", kind="fp8", log_n=13, limbs=3, log_scale=35, d_in=1024, d_out=16, block_rows=128),
+        dict(name="fp8-1024x16-n13", kind="fp8", log_n=13, limbs=3, log_scale=31, d_in=1024, d_out=16, block_rows=128),
         # Odd sizes: one tensor-parallel share of a layer with a scale for each output.
-        dict(name="fp8-513x1021-n13-rows", kind="fp8", log_n=13, limbs=3, log_scale=36, d_in=513, d_out=1021, block_rows=1),
+        dict(name="fp8-513x1021-n13-rows", kind="fp8", log_n=13, limbs=3, log_scale=32, d_in=513, d_out=1021, block_rows=1),
         # A down projection: deep contraction, few outputs.
-        dict(name="fp8-2048x768-n14", kind="fp8", log_n=14, limbs=4, log_scale=35, d_in=2048, d_out=768, block_rows=128),
+        dict(name="fp8-2048x768-n14", kind="fp8", log_n=14, limbs=4, log_scale=31, d_in=2048, d_out=768, block_rows=128),
         # An up projection in a large ring: the largest layer.
-        dict(name="fp8-1024x2048-n15", kind="fp8", log_n=15, limbs=4, log_scale=35, d_in=1024, d_out=2048, block_rows=128),
+        dict(name="fp8-1024x2048-n15", kind="fp8", log_n=15, limbs=4, log_scale=31, d_in=1024, d_out=2048, block_rows=128),
         # A few small experts: the latency of a call.
-        dict(name="experts-4-32x32-n10", kind="experts", log_n=10, limbs=2, log_scale=34, experts=4, count=5, padded=0,
+        dict(name="experts-4-32x32-n10", kind="experts", log_n=10, limbs=2, log_scale=30, experts=4, count=5, padded=0,
              bundles=3, d_in=32, d_out=32, block_rows=128),
         # Odd sizes, a scale for each output, and room that the step does not fill.
-        dict(name="experts-8-200x333-n11-rows", kind="experts", log_n=11, limbs=2, log_scale=36, experts=8, count=13,
+        dict(name="experts-8-200x333-n11-rows", kind="experts", log_n=11, limbs=2, log_scale=32, experts=8, count=13,
              padded=3, bundles=6, d_in=200, d_out=333, block_rows=1),
         # Two experts for each of ten bundles, of sixteen fine-grained experts.
-        dict(name="experts-16-1024x384-n12", kind="experts", log_n=12, limbs=3, log_scale=35, experts=16, count=20,
+        dict(name="experts-16-1024x384-n12", kind="experts", log_n=12, limbs=3, log_scale=31, experts=16, count=20,
              padded=0, bundles=10, d_in=1024, d_out=384, block_rows=128),
         # Two experts' outputs for each of two bundles in a small ring: latency.
         dict(name="combine-2x16-n10", kind="combine", log_n=10, limbs=2, count=4, bundles=2, top=2, features=16),
@@ -72,7 +72,7 @@ def _draw_once(rng):
         c.update(bundles=_spread(rng, 1, 64), top=rng.randint(1, 8), features=_spread(rng, 1, 2048))
         c["count"] = max(1, round(c["bundles"] * c["top"] * rng.uniform(0.4, 1.2)))
         return c
-    c.update(log_scale=rng.randint(30, 40), d_in=_spread(rng, 1, 4096), d_out=_spread(rng, 1, 4096),
+    c.update(log_scale=rng.randint(26, 36), d_in=_spread(rng, 1, 4096), d_out=_spread(rng, 1, 4096),
              block_rows=rng.choice([1, 64, 128, 128, 128]))
     if kind == "experts":
         c.update(experts=_spread(rng, 1, 64), count=_spread(rng, 1, 64), padded=rng.choice([0, 0, 1, 3]),
@@ -246,10 +246,10 @@ def run(state):
 
 
 def _plaintexts(st):
-    """512 times the weights, whole numbers, times the rounded scales: residues [many][L][d_out][d_in]."""
+    """64 times the weights, rounded to whole numbers, times the rounded scales: residues [many][L][d_out][d_in]."""
     c, q = st["case"], st["q"]
-    v = (st["w8"].to(torch.float32) * 512).to(torch.int64)
-    s = torch.round(st["scales"].double() * (2.0 ** c["log_scale"] / 512)).to(torch.int64)
+    v = torch.round(st["w8"].to(torch.float32) * 64).to(torch.int64)
+    s = torch.round(st["scales"].double() * (2.0 ** c["log_scale"] / 64)).to(torch.int64)
     row = torch.arange(c["d_out"], device="cuda") // c["block_rows"]
     col = torch.arange(c["d_in"], device="cuda") // BLOCK
     s = s[:, row][:, :, col]
@@ -334,9 +334,12 @@ def exact(case, seed):
 
 
 def _e4m3(code):
-    """512 times the number that a code stands for: a sign, four bits of exponent and three of mantissa."""
+    """64 times the number that a code stands for (a sign, four bits of exponent, three of mantissa, the least step
+    2^-9), rounded half to even."""
     sign, exponent, mantissa = code >> 7, code >> 3 & 15, code & 7
-    size = mantissa if exponent == 0 else (8 + mantissa) << (exponent - 1)
+    eighths = mantissa if exponent == 0 else (8 + mantissa) << (exponent - 1)
+    size, rest = divmod(eighths, 8)
+    size += rest > 4 or (rest == 4 and size % 2 == 1)
     return -size if sign else size
 
 
@@ -344,7 +347,7 @@ def _exact_layer(case, codes, scales, x, q):
     out = np.zeros((case["d_out"],) + x.shape[1:], dtype=np.int64)
     for j in range(case["d_out"]):
         for i in range(case["d_in"]):
-            s = float(scales[j // case["block_rows"], i // BLOCK]) * 2.0 ** case["log_scale"] / 512
+            s = float(scales[j // case["block_rows"], i // BLOCK]) * 2.0 ** case["log_scale"] / 64
             weight = _e4m3(int(codes[j, i])) * int(np.rint(s))
             weight = np.array([weight % int(v) for v in q], dtype=np.int64)
             out[j] = (out[j] + weight[None, :, None] * x[i]) % q[None, :, None]
