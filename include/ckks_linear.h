@@ -32,7 +32,7 @@
  * stream), so device-side faults surface at the caller's next synchronisation.
  * ckks_last_error() returns a thread-local description of the last failure.
  * Device pointers must be 16-byte aligned unless stated (int32 lists of a cache
- * and 4-bit weights: the element).  Entry points taking a context are
+ * or of requests, 4-bit and 8-bit weights: the element).  Entry points taking a context are
  * safe to call concurrently on different streams; outputs must not alias
  * inputs unless stated.
  */
@@ -222,6 +222,87 @@ int ckks_linear_encode_q4(const ckks_ctx* ctx, const uint8_t* w4, const float* s
  * d_in == 0 writes zeros. */
 int ckks_linear_mac_q4(const ckks_ctx* ctx, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
                        uint32_t d_in, uint32_t group, uint32_t limbs, int zeros, void* stream);
+
+/* ---- Layers over 8-bit floating-point weights, and experts ------------------
+ *
+ * A layer whose weights are e4m3 numbers f (a sign, four bits of exponent with bias 7,
+ * three of mantissa; no infinities, the codes 0x7f and 0xff are NaN) with one scale
+ * for every block of 128 consecutive inputs and block_rows consecutive outputs:
+ * w[j][i] = scales[j / block_rows][i / 128] f[j][i].  The plaintext of a weight is
+ * rint(64 f) rint(scales * scale / 64), rint rounding half to even: the block's scale
+ * is rounded once, and f to a multiple of 2^-6, which is exact for |f| >= 1/8 and
+ * within 2^-7 below (2^-16 of the largest e4m3 number, 448).  The rounded scale is off by at most
+ * 32 / (|scales| scale) relative to itself, so `scale` should be large against 1 / |scales|.
+ *
+ * Encoded weights take 2 bytes a weight and 12 limbs bytes a row and 128 inputs, with rows and inputs
+ * padded to multiples of 32, against the 4 limbs bytes a weight of ckks_linear_encode_scalar. */
+
+/* Bytes of the encoded weights ((size_t)-1 for an invalid request; 0 for an
+ * empty layer); a multiple of 128. */
+size_t ckks_fp8_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in, uint32_t limbs);
+
+/* Encode 8-bit weights for `limbs` limbs.
+ *   w8      device uint8 [d_out][d_in], e4m3 codes; any alignment.
+ *   scales  device fp32 [ceil(d_out / block_rows)][ceil(d_in / 128)], 4-byte aligned;
+ *           |scales * scale / 64| < 2^63.
+ *   block_rows  1 or more: 128 for square blocks, 1 for a scale for each output and 128 inputs.
+ *   w_fp8   device, ckks_fp8_weight_bytes bytes, in a layout of the library's own; must not
+ *           overlap the inputs.
+ *   bad     device int32 [1], 4-byte aligned, or NULL: the number of weights that are NaN and of scales that are no
+ *           finite number.  Such weights, and the weights of such scales, count as zero.
+ * Run once per layer. */
+int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                           uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream);
+
+/* ct x pt MAC with 8-bit weights:  ct_out[j][c][l][k] = sum_i rint(64 f[j][i])
+ * rint(scales * scale / 64) ct_in[i][c][l][k] mod q_l, as ckks_linear_mac_scalar over
+ * the same plaintexts.
+ *   w_fp8   ckks_linear_encode_fp8's output for the same d_out, d_in and limbs.
+ *   ct_in   device uint32 [d_in][2][limbs][N];  ct_out [d_out][2][limbs][N], which
+ *           must not overlap ct_in or w_fp8 (CKKS_E_INVALID_ARG).
+ * d_out <= 524280 and d_in <= 2^24.  No workspace.  d_out == 0 is a no-op;
+ * d_in == 0 writes zeros. */
+int ckks_linear_mac_fp8(const ckks_ctx* ctx, const void* w_fp8, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
+                        uint32_t d_in, uint32_t limbs, void* stream);
+
+/* Status of a request of ckks_experts_mac_fp8. */
+enum ckks_expert_status {
+  CKKS_EXPERT_OK = 0,
+  CKKS_EXPERT_BAD_REQUEST = 1 /* an expert or a bundle out of range */
+};
+
+/* Experts' layers in one call: request r is ckks_linear_mac_fp8 of expert[r]'s weights over bundle[r] of
+ * the inputs.  An expert may have any number of requests, none included, and a bundle may be
+ * named by several (tokens that go to two experts); requests of one expert next to each other share its
+ * weights in the caches.  The lists are read on the device, so a call can be captured with room for the
+ * most requests: one that names no expert (-1) or no bundle leaves its outputs as they were and says
+ * so in `status`.
+ *   w_fp8   device [experts]: ckks_linear_encode_fp8's outputs for the same d_out, d_in and limbs,
+ *           ckks_fp8_weight_bytes apart.
+ *   expert  device int32 [count].   bundle  device int32 [count], or NULL (request r has bundle r).
+ *   ct_in   device uint32 [bundles][d_in][2][limbs][N].
+ *   ct_out  device uint32 [count][d_out][2][limbs][N].
+ *   status  device int32 [count] (ckks_expert_status), or NULL.
+ * ct_out and status must not overlap each other or the inputs (CKKS_E_INVALID_ARG).
+ * experts, count and bundles <= 65536.  count == 0 is a no-op; with d_out == 0 only the status is written;
+ * d_in == 0 writes zeros for good requests. */
+int ckks_experts_mac_fp8(const ckks_ctx* ctx, const void* w_fp8, uint32_t experts, const int32_t* expert,
+                         const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
+                         uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, void* stream);
+
+/* Gated sums of requests' outputs:  ct_out[t][j][c][l][k] = sum_i gates[r][l][k] ct_in[r][j][c][l][k] mod q_l
+ * over the requests r = terms[t][i], i < top: the sum of a bundle's experts, each weighted in
+ * every slot by its gate for the token there.  A term outside 0 .. count - 1 (-1) adds nothing, and a
+ * bundle without terms gets zeros; a request that is named twice counts twice.
+ *   gates   device uint32 [count][limbs][N], NTT form (ckks_linear_encode_poly of the slots' gates).
+ *   ct_in   device uint32 [count][features][2][limbs][N], ckks_experts_mac_fp8's outputs (rescaled or not).
+ *   terms   device int32 [bundles][top].
+ *   ct_out  device uint32 [bundles][features][2][limbs][N]; must not overlap the inputs (CKKS_E_INVALID_ARG).
+ * count, bundles and top <= 65536, features <= 524280.  bundles == 0 or features == 0 is a no-op; top == 0 or
+ * count == 0 writes zeros. */
+int ckks_experts_combine(const ckks_ctx* ctx, const uint32_t* gates, const uint32_t* ct_in, uint32_t count,
+                         const int32_t* terms, uint32_t bundles, uint32_t top, uint32_t* ct_out, uint32_t features,
+                         uint32_t limbs, void* stream);
 
 /* ct x pt MAC with full-polynomial NTT-form weights (the fallback-encode
  * path of section 4.2): slot-wise

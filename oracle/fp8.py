@@ -1,0 +1,61 @@
+"""Layers over 8-bit floating-point weights and gated sums of their outputs (CPU
+oracle; test infrastructure only).
+
+A weight is scales[j // block_rows, i // 128] f[j, i] with f an e4m3 number.  Its
+plaintext is the integer rint(64 f) rint(scales * scale / 64), both rounded half to
+even, so the layer is the scalar-weight MAC (section 3.2) over those integers mod
+each prime.  Python integers throughout: scaled scales may be as large as 2^63.
+
+Parity: pinned (tests/test_oracle_fp8.py) by the numbers of e4m3 written out, by a
+tiny case, and by the scalar encode where both round alike.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from .linear import mac_scalar
+
+BLOCK = 128
+
+
+def numbers(codes) -> np.ndarray:
+    """e4m3 codes -> float64: (-1)^s 2^(e - 7) (1 + m / 8), or (-1)^s 2^-6 m / 8 where e = 0; NaN for e = 15, m = 7."""
+    c = np.asarray(codes, np.uint8).astype(np.int64)
+    e, m = c >> 3 & 15, c & 7
+    f = np.where(e == 0, m / 8 * 2.0 ** -6, (1 + m / 8) * 2.0 ** (e - 7.0))
+    f = np.where((e == 15) & (m == 7), np.nan, f)
+    return np.where(c >> 7, -f, f)
+
+
+def plaintexts(codes, scales, block_rows: int, scale: float) -> np.ndarray:
+    """The integers rint(64 f) rint(scales * scale / 64), as Python integers (object array d_out x d_in); NaN weights
+    and scales that are no finite number are zero."""
+    f = numbers(codes)
+    v = np.rint(64 * np.nan_to_num(f, nan=0.0)).astype(np.int64)
+    s = np.asarray(scales, np.float32).astype(np.float64)
+    s = np.rint(np.where(np.isfinite(s), s, 0.0) * (scale / 64))
+    s = np.vectorize(int, otypes=[object])(s) if s.size else s.astype(object)
+    row, col = np.arange(v.shape[0]) // block_rows, np.arange(v.shape[1]) // BLOCK
+    return v.astype(object) * s[row][:, col]
+
+
+def residues(p, qs) -> np.ndarray:
+    """Integers (d_out, d_in) -> uint64 (d_out, d_in, L)."""
+    return np.stack([(p % int(q)).astype(np.uint64) for q in qs], axis=-1)
+
+
+def mac(codes, scales, ct, block_rows: int, scale: float, qs, rows=None) -> np.ndarray:
+    """ct (d_in, 2, L, N) residues -> (len(rows), 2, L, N)."""
+    return mac_scalar(residues(plaintexts(codes, scales, block_rows, scale), qs), ct, qs, rows=rows)
+
+
+def combine(gates, y, terms, qs) -> np.ndarray:
+    """gates (count, L, N), y (count, features, 2, L, N), terms (bundles, top) -> (bundles, features, 2, L, N)."""
+    gates, y = np.asarray(gates).astype(np.uint64), np.asarray(y).astype(np.uint64)
+    q = np.array(qs, np.uint64)[:, None]
+    out = np.zeros((len(terms),) + y.shape[1:], np.uint64)
+    for t, row in enumerate(terms):
+        for r in row:
+            if 0 <= r < len(y):
+                out[t] = (out[t] + gates[r] * y[r] % q) % q
+    return out

@@ -40,6 +40,9 @@ CKKS_OP_RESCALE = 2
 CKKS_OP_ENCODE_POLY = 3
 CKKS_OP_ROTATE = 4
 
+CKKS_EXPERT_OK = 0
+CKKS_EXPERT_BAD_REQUEST = 1
+
 CKKS_CACHE_OK = 0
 CKKS_CACHE_BAD_REQUEST = 1
 CKKS_CACHE_TABLE_FULL = 2
@@ -77,6 +80,11 @@ _SIGS = {
     "ckks_q4_weight_bytes": (_sz, [_vp, _u32, _u32, _u32, _u32, _i32]),
     "ckks_linear_encode_q4": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _dbl, _vp, _vp]),
     "ckks_linear_mac_q4": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _i32, _vp]),
+    "ckks_fp8_weight_bytes": (_sz, [_vp, _u32, _u32, _u32]),
+    "ckks_linear_encode_fp8": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _u32, _dbl, _vp, _vp, _vp]),
+    "ckks_linear_mac_fp8": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
+    "ckks_experts_mac_fp8": (_i32, [_vp, _vp, _u32, _vp, _vp, _u32, _vp, _u32, _vp, _u32, _u32, _u32, _vp, _vp]),
+    "ckks_experts_combine": (_i32, [_vp, _vp, _vp, _u32, _vp, _u32, _u32, _vp, _u32, _u32, _vp]),
     "ckks_linear_mac_poly": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "ckks_rescale": (_i32, [_vp, _vp, _vp, _u32, _u32, _vp, _sz, _vp]),
     "ckks_encrypt": (_i32, [_vp, _vp, _vp, _vp, _vp, _u32, _u32, _vp, _vp]),
@@ -382,6 +390,73 @@ def ckks_linear_mac_q4(ctx: Context, w_q4, ct_in, ct_out, d_out: int, d_in: int,
         ctx.handle, _ptr(w_q4, "w_q4", need, w_q4.element_size() if w_q4 is not None else 1),
         _ptr(ct_in, "ct_in", d_in * ct_words * 4, 4), _ptr(ct_out, "ct_out", d_out * ct_words * 4, 4),
         d_out, d_in, group, limbs, int(zeros), _stream(stream)), "ckks_linear_mac_q4")
+
+
+def ckks_fp8_weight_bytes(ctx: Context, d_out: int, d_in: int, limbs: int) -> int:
+    v = _lib.ckks_fp8_weight_bytes(ctx.handle, d_out, d_in, limbs)
+    if v == ctypes.c_size_t(-1).value:
+        raise ValueError("invalid 8-bit weight request")
+    return int(v)
+
+
+def _words(t) -> int:
+    return t.element_size() if t is not None else 1
+
+
+def ckks_linear_encode_fp8(ctx: Context, w8, scales, d_out: int, d_in: int, block_rows: int, limbs: int, scale: float,
+                           w_fp8, bad=None, stream=None) -> None:
+    """w8: e4m3 weights, as torch.float8_e4m3fn or their codes as uint8; scales float32; bad int32 [1] or None."""
+    need = ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs)
+    if block_rows < 1:
+        raise ValueError("block_rows must be positive")
+    if w8 is not None and w8.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise ValueError(f"w8 must be float8_e4m3fn or its codes as uint8 (got {w8.dtype})")
+    if scales is not None and scales.dtype != torch.float32:
+        raise ValueError(f"scales must be float32 (got {scales.dtype})")
+    blocks = -(-d_out // block_rows) * -(-d_in // 128)
+    _check(_lib.ckks_linear_encode_fp8(
+        ctx.handle, _ptr(w8, "w8", d_out * d_in, 1), _ptr(scales, "scales", blocks * 4, 4), d_out, d_in, block_rows, limbs,
+        float(scale), _ptr(w_fp8, "w_fp8", need, _words(w_fp8)), _ptr(bad, "bad", 4, 4, True), _stream(stream)),
+        "ckks_linear_encode_fp8")
+
+
+def ckks_linear_mac_fp8(ctx: Context, w_fp8, ct_in, ct_out, d_out: int, d_in: int, limbs: int, stream=None) -> None:
+    ct_words = 2 * limbs * ctx.n if d_out else 0
+    need = ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs)
+    _check(_lib.ckks_linear_mac_fp8(
+        ctx.handle, _ptr(w_fp8, "w_fp8", need, _words(w_fp8)), _ptr(ct_in, "ct_in", d_in * ct_words * 4, 4),
+        _ptr(ct_out, "ct_out", d_out * ct_words * 4, 4), d_out, d_in, limbs, _stream(stream)), "ckks_linear_mac_fp8")
+
+
+def ckks_experts_mac_fp8(ctx: Context, w_fp8, expert, bundle, ct_in, ct_out, d_out: int, d_in: int, limbs: int, status=None,
+                         stream=None) -> None:
+    """w_fp8 [experts][bytes of one]; expert int32 [count]; bundle int32 [count], or None (a request's own number);
+    ct_in [bundles][d_in][2][limbs][N]; ct_out [count][d_out][2][limbs][N]."""
+    experts, bundles, count = w_fp8.shape[0], ct_in.shape[0], expert.numel()
+    ct_words = 2 * limbs * ctx.n if d_out else 0
+    need = ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs)
+    if need and w_fp8.numel() * _words(w_fp8) != experts * need:
+        raise ValueError(f"w_fp8 must be [{experts}][{need} bytes] (got {tuple(w_fp8.shape)})")
+    if expert.dtype != torch.int32 or (bundle is not None and bundle.dtype != torch.int32):
+        raise ValueError("expert and bundle must be int32")
+    _check(_lib.ckks_experts_mac_fp8(
+        ctx.handle, _ptr(w_fp8, "w_fp8", experts * need, _words(w_fp8)), experts, _ptr(expert, "expert", count * 4, 4),
+        _ptr(bundle, "bundle", count * 4, 4, True), count, _ptr(ct_in, "ct_in", bundles * d_in * ct_words * 4, 4), bundles,
+        _ptr(ct_out, "ct_out", count * d_out * ct_words * 4, 4), d_out, d_in, limbs, _ptr(status, "status", count * 4, 4, True),
+        _stream(stream)), "ckks_experts_mac_fp8")
+
+
+def ckks_experts_combine(ctx: Context, gates, ct_in, terms, ct_out, features: int, limbs: int, stream=None) -> None:
+    """gates [count][limbs][N]; ct_in [count][features][2][limbs][N]; terms int32 [bundles][top];
+    ct_out [bundles][features][2][limbs][N]."""
+    count, (bundles, top) = gates.shape[0], terms.shape
+    if terms.dtype != torch.int32:
+        raise ValueError(f"terms must be int32 (got {terms.dtype})")
+    words = limbs * ctx.n * 4
+    _check(_lib.ckks_experts_combine(
+        ctx.handle, _ptr(gates, "gates", count * words, 4), _ptr(ct_in, "ct_in", count * features * 2 * words, 4), count,
+        _ptr(terms, "terms", bundles * top * 4, 4), bundles, top, _ptr(ct_out, "ct_out", bundles * features * 2 * words, 4),
+        features, limbs, _stream(stream)), "ckks_experts_combine")
 
 
 class Cache:

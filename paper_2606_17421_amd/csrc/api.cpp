@@ -16,6 +16,8 @@
 static_assert(CKKS_CACHE_OK == ckks::kCacheOk && CKKS_CACHE_BAD_REQUEST == ckks::kCacheBadRequest &&
                   CKKS_CACHE_TABLE_FULL == ckks::kCacheTableFull && CKKS_CACHE_NO_PAGES == ckks::kCacheNoPages,
               "request status in the header and the kernels");
+static_assert(CKKS_EXPERT_OK == ckks::kExpertOk && CKKS_EXPERT_BAD_REQUEST == ckks::kExpertBadRequest,
+              "request status in the header and the kernels");
 static_assert(CKKS_NOALLOC_SCRATCH_BYTES == ckks::kNoAllocScratchBytes, "scratch size in the header and the library");
 
 struct ckks_ctx {
@@ -868,8 +870,6 @@ int ckks_linear_mac_q4(const ckks_ctx* ctx, const void* w_q4, const uint32_t* ct
   return e == hipSuccess ? ok() : hip_fail(e, "mac_q4 launch");
 }
 
-// ---- paged cache ------------------------------------------------------------
-
 namespace {
 
 struct Span {
@@ -877,6 +877,145 @@ struct Span {
   size_t bytes;
   const char* name;
 };
+
+bool clash(const Span& a, const Span& b) { return a.p && b.p && a.bytes && b.bytes && overlaps(a.p, a.bytes, b.p, b.bytes); }
+
+// Nothing that a call writes shares bytes with another output or an input.
+int check_writes(std::initializer_list<Span> writes, std::initializer_list<Span> reads) {
+  auto told = [](const Span& a, const Span& b) { return fail(CKKS_E_INVALID_ARG, "%s overlaps %s", a.name, b.name); };
+  for (auto w = writes.begin(); w != writes.end(); ++w) {
+    for (auto v = w + 1; v != writes.end(); ++v)
+      if (clash(*w, *v)) return told(*w, *v);
+    for (const Span& r : reads)
+      if (clash(*w, r)) return told(*w, r);
+  }
+  return CKKS_OK;
+}
+
+}  // namespace
+
+// ---- layers over 8-bit weights, and experts ----------------------------------
+
+size_t ckks_fp8_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in, uint32_t limbs) {
+  if (!ctx || limbs < 1 || limbs > ctx->L || check_mac_shapes(d_out, d_in) != CKKS_OK) return static_cast<size_t>(-1);
+  return ckks::fp8_weight_bytes(d_out, d_in, limbs);
+}
+
+int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                           uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(d_out, d_in)) return rc;
+  if (block_rows == 0) return fail(CKKS_E_INVALID_ARG, "block_rows must be positive");
+  if (!(scale > 0.0) || !std::isfinite(scale)) return fail(CKKS_E_INVALID_ARG, "scale must be finite and > 0");
+  if (bad)
+    if (int rc = check_list(bad, "bad")) return rc;
+  DeviceGuard guard(ctx->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d_out == 0 || d_in == 0) {  // nothing is bad in an empty layer
+    hipError_t e = bad ? ckks::launch_zero(reinterpret_cast<uint32_t*>(bad), 1, s) : hipSuccess;
+    return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
+  }
+  if (!w8) return fail(CKKS_E_INVALID_ARG, "w8 is null");
+  if (int rc = check_list(scales, "scales")) return rc;
+  if (int rc = check_ptr(w_fp8, "w_fp8")) return rc;
+  const size_t scale_count = ((size_t(d_out) - 1) / block_rows + 1) * ((size_t(d_in) + 127) / 128);
+  if (int rc = check_writes({{w_fp8, ckks::fp8_weight_bytes(d_out, d_in, limbs), "w_fp8"}, {bad, 4, "bad"}},
+                            {{w8, size_t(d_out) * d_in, "w8"}, {scales, scale_count * 4, "scales"}}))
+    return rc;
+  hipError_t e = ckks::launch_encode_fp8(ctx->t, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad, s);
+  return e == hipSuccess ? ok() : hip_fail(e, "encode_fp8 launch");
+}
+
+int ckks_linear_mac_fp8(const ckks_ctx* ctx, const void* w_fp8, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
+                        uint32_t d_in, uint32_t limbs, void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(d_out, d_in)) return rc;
+  if (d_out == 0) return ok();
+  if (int rc = check_ptr(ct_out, "ct_out")) return rc;
+  const size_t ct_row = size_t(2) * limbs * ctx->n * 4;
+  DeviceGuard guard(ctx->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d_in == 0) {
+    hipError_t e = ckks::launch_zero(ct_out, d_out * ct_row / 4, s);
+    return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
+  }
+  if (int rc = check_ptr(w_fp8, "w_fp8")) return rc;
+  if (int rc = check_ptr(ct_in, "ct_in")) return rc;
+  if (int rc = check_writes({{ct_out, d_out * ct_row, "ct_out"}},
+                            {{ct_in, d_in * ct_row, "ct_in"}, {w_fp8, ckks::fp8_weight_bytes(d_out, d_in, limbs), "w_fp8"}}))
+    return rc;
+  hipError_t e = ckks::launch_mac_fp8(ctx->t, w_fp8, 1, nullptr, nullptr, 1, ct_in, 1, ct_out, d_out, d_in, limbs, nullptr, s);
+  return e == hipSuccess ? ok() : hip_fail(e, "mac_fp8 launch");
+}
+
+int ckks_experts_mac_fp8(const ckks_ctx* ctx, const void* w_fp8, uint32_t experts, const int32_t* expert,
+                         const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
+                         uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(d_out, d_in)) return rc;
+  if (experts > ckks::kMaxRequests || count > ckks::kMaxRequests || bundles > ckks::kMaxRequests)
+    return fail(CKKS_E_INVALID_ARG, "experts=%u, count=%u or bundles=%u over %u", experts, count, bundles, ckks::kMaxRequests);
+  if (count == 0) return ok();
+  if (int rc = check_list(expert, "expert")) return rc;
+  if (bundle)
+    if (int rc = check_list(bundle, "bundle")) return rc;
+  if (status)
+    if (int rc = check_list(status, "status")) return rc;
+  const size_t ct_row = size_t(2) * limbs * ctx->n * 4, w_b = ckks::fp8_weight_bytes(d_out, d_in, limbs);
+  const bool reads = d_out != 0 && d_in != 0 && experts != 0 && bundles != 0;
+  if (d_out != 0)
+    if (int rc = check_ptr(ct_out, "ct_out")) return rc;
+  if (reads) {
+    if (int rc = check_ptr(w_fp8, "w_fp8")) return rc;
+    if (int rc = check_ptr(ct_in, "ct_in")) return rc;
+  }
+  if (int rc = check_writes({{ct_out, size_t(count) * d_out * ct_row, "ct_out"}, {status, size_t(count) * 4, "status"}},
+                            {{ct_in, reads ? size_t(bundles) * d_in * ct_row : 0, "ct_in"},
+                             {w_fp8, reads ? experts * w_b : 0, "w_fp8"},
+                             {expert, size_t(count) * 4, "expert"},
+                             {bundle, size_t(count) * 4, "bundle"}}))
+    return rc;
+  DeviceGuard guard(ctx->device);
+  hipError_t e = ckks::launch_mac_fp8(ctx->t, w_fp8, experts, expert, bundle, count, ct_in, bundles, ct_out, d_out, d_in,
+                                      limbs, status, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ok() : hip_fail(e, "experts_mac_fp8 launch");
+}
+
+int ckks_experts_combine(const ckks_ctx* ctx, const uint32_t* gates, const uint32_t* ct_in, uint32_t count,
+                         const int32_t* terms, uint32_t bundles, uint32_t top, uint32_t* ct_out, uint32_t features,
+                         uint32_t limbs, void* stream) {
+  if (int rc = check_ctx(ctx)) return rc;
+  if (int rc = check_limbs(ctx, limbs, 1)) return rc;
+  if (int rc = check_mac_shapes(features, 1)) return rc;
+  if (count > ckks::kMaxRequests || bundles > ckks::kMaxRequests || top > ckks::kMaxRequests)
+    return fail(CKKS_E_INVALID_ARG, "count=%u, bundles=%u or top=%u over %u", count, bundles, top, ckks::kMaxRequests);
+  if (bundles == 0 || features == 0) return ok();
+  if (int rc = check_ptr(ct_out, "ct_out")) return rc;
+  const size_t ct_row = size_t(2) * limbs * ctx->n * 4;
+  DeviceGuard guard(ctx->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (top == 0 || count == 0) {
+    hipError_t e = ckks::launch_zero(ct_out, size_t(bundles) * features * (ct_row / 4), s);
+    return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
+  }
+  if (int rc = check_ptr(gates, "gates")) return rc;
+  if (int rc = check_ptr(ct_in, "ct_in")) return rc;
+  if (int rc = check_list(terms, "terms")) return rc;
+  if (int rc = check_writes({{ct_out, size_t(bundles) * features * ct_row, "ct_out"}},
+                            {{gates, count * ct_row / 2, "gates"},
+                             {ct_in, size_t(count) * features * ct_row, "ct_in"},
+                             {terms, size_t(bundles) * top * 4, "terms"}}))
+    return rc;
+  hipError_t e = ckks::launch_combine(ctx->t, gates, ct_in, count, terms, bundles, top, ct_out, features, limbs, s);
+  return e == hipSuccess ? ok() : hip_fail(e, "experts_combine launch");
+}
+
+// ---- paged cache ------------------------------------------------------------
+
+namespace {
 
 // The cache as the kernels see it, or why it is no cache.
 int check_cache(const ckks_ctx* ctx, const ckks_cache* k, ckks::Cache* out) {
@@ -914,7 +1053,6 @@ int check_apart(const ckks::Cache& c, std::initializer_list<Span> writes, std::i
                       {c.refs, size_t(c.pages) * 4, "refs"},
                       {c.table, size_t(c.seqs) * c.max_pages * 4, "table"},
                       {c.lens, size_t(c.seqs) * 4, "lens"}};
-  auto clash = [](const Span& a, const Span& b) { return a.p && b.p && a.bytes && b.bytes && overlaps(a.p, a.bytes, b.p, b.bytes); };
   auto told = [](const Span& a, const Span& b) { return fail(CKKS_E_INVALID_ARG, "%s overlaps %s", a.name, b.name); };
   for (size_t i = 0; i < 4; ++i) {
     for (size_t j = i + 1; j < 4; ++j)
@@ -924,13 +1062,7 @@ int check_apart(const ckks::Cache& c, std::initializer_list<Span> writes, std::i
     for (const Span& r : reads)
       if (clash(r, own[i])) return told(r, own[i]);
   }
-  for (auto w = writes.begin(); w != writes.end(); ++w) {
-    for (auto v = w + 1; v != writes.end(); ++v)
-      if (clash(*w, *v)) return told(*w, *v);
-    for (const Span& r : reads)
-      if (clash(*w, r)) return told(*w, r);
-  }
-  return CKKS_OK;
+  return check_writes(writes, reads);
 }
 
 int check_count(uint32_t count) {

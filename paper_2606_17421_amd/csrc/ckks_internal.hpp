@@ -192,6 +192,23 @@ hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* sca
 hipError_t launch_mac_q4(const Tables& t, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
                          uint32_t d_in, uint32_t group, uint32_t limbs, bool zeros, hipStream_t s);
 
+// MAC over e4m3 weights with a scale for each block of 128 inputs and block_rows
+// outputs (mac_fp8.hip): count requests (expert, bundle); one layer is expert 0 of one
+// and bundle 0 of one, with null lists.
+constexpr int32_t kExpertOk = 0, kExpertBadRequest = 1;
+constexpr uint32_t kMaxRequests = 65536;
+size_t fp8_weight_bytes(uint32_t d_out, uint32_t d_in, uint32_t limbs);
+hipError_t launch_encode_fp8(const Tables& t, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, hipStream_t s);
+hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, const int32_t* expert,
+                          const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
+                          uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, hipStream_t s);
+
+// Gated sums of requests' outputs (combine.hip).
+hipError_t launch_combine(const Tables& t, const uint32_t* gates, const uint32_t* ct_in, uint32_t count,
+                          const int32_t* terms, uint32_t bundles, uint32_t top, uint32_t* ct_out, uint32_t features,
+                          uint32_t limbs, hipStream_t s);
+
 size_t rescale_workspace_bytes(const Tables& t, uint32_t count, uint32_t limbs);
 hipError_t launch_rescale(const Tables& t, const uint32_t* ct_in, uint32_t* ct_out, uint32_t count,
                           uint32_t limbs, void* workspace, hipStream_t s);

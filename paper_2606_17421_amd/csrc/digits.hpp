@@ -1,5 +1,5 @@
-// Balanced base-256 digits of residues as int8 matrix-core operands, shared by
-// the MACs that contract them.
+// Balanced base-256 digits of residues as int8 matrix-core operands, and the
+// constants of a closing reduction, shared by the MACs that contract them.
 #pragma once
 
 #include "ckks_internal.hpp"
@@ -7,6 +7,7 @@
 namespace ckks {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 constexpr uint32_t kBias = 0x80808080u;
 constexpr int kRsrcWord3 = 0x00020000;  // buffer resource word 3: 32-bit raw data, range-checked
@@ -37,6 +38,22 @@ __device__ __forceinline__ void to_fragments(const uint32_t (&x)[16], v4i (&f)[4
 #pragma unroll
     for (int b = 0; b < 4; ++b) f[b][g] = static_cast<int>(o[b] ^ kBias);
   }
+}
+
+// The residue nearest to zero.
+__device__ __forceinline__ int32_t centred(uint32_t r, uint32_t q) {
+  return r > (q >> 1) ? static_cast<int32_t>(r - q) : static_cast<int32_t>(r);
+}
+
+// A prime and its inverse for Montgomery's reduction.
+struct Modulus {
+  uint32_t q, qinv;  // qinv = 1 / q mod 2^32
+};
+__device__ __forceinline__ Modulus modulus(uint32_t q) {
+  uint32_t v = q;  // right mod 2^3 for odd q; each step doubles the bits
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v *= 2u - q * v;
+  return {q, v};
 }
 
 }  // namespace ckks

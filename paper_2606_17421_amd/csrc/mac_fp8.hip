@@ -1,0 +1,311 @@
+// ct x pt MAC over 8-bit floating-point (e4m3) weights with one scale per block of
+// 128 inputs and some outputs on the gfx950 matrix cores, exact over the plaintexts:
+// one layer, or requests that each name an expert's layer and a bundle of inputs.
+//
+// Per limb l, with f the weights, v = rint(64 f) and S = rint(scale Delta / 64) of a block,
+//     out[j][col] = sum_b S[j][b] T[j][b][col] mod q_l,
+//     T[j][b][col] = sum over the 128 inputs of v[j][i] x[i][col].
+// |v| <= 64 * 448 = 28672 is two balanced base-256 digits, the same for every limb, against the
+// residues' four: eight int8 products a modular MAC.  Every step of e4m3 (2^-9) would take three
+// digits and twelve; what the rounding to 64ths costs is 2^-7 at most of a weight below 1/8, 2^-16 of the largest one.
+// T = a + 2^16 b + 2^32 c with a and b from two digit sums each and c from one; a block's scale enters
+// in 64-bit integers, and the sum over the blocks is reduced once an output.
+#include "digits.hpp"
+
+namespace ckks {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kStep = 32;        // inputs of one matrix-core step
+constexpr uint32_t kBlock = 128;      // inputs that share a scale
+constexpr uint32_t kBlockSteps = kBlock / kStep;
+constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 64-bit sums
+constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
+constexpr int kDigits = 2;            // of a weight
+
+// Encoded weights (written once a layer):
+//   fragments [tile][step][digit][64 lanes] of 16 bytes: digit of row tile*32 + lane%32 and inputs
+//     step*32 + 16 (lane/32) + i, i < 16; rows are padded to 32, inputs to 32.
+//   scales [limb][tile][block][3][32 rows]: 2^32 S, 2^48 S and 2^64 S mod q_l, centred.  The
+//     2^32 is what the closing reduction divides by.
+struct Shape {
+  uint32_t tiles, steps, blocks;
+  size_t frag_bytes, scale_bytes;
+};
+
+Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t limbs) {
+  Shape s;
+  s.tiles = (d_out + 31) / 32;
+  s.steps = (d_in + kStep - 1) / kStep;
+  s.blocks = (d_in + kBlock - 1) / kBlock;
+  s.frag_bytes = static_cast<size_t>(s.tiles) * s.steps * kDigits * 64 * 16;
+  s.scale_bytes = static_cast<size_t>(limbs) * s.tiles * s.blocks * 3 * 32 * 4;
+  return s;
+}
+
+// rint(64 f) of an e4m3 code, half to even.  A code is a sign, four bits of exponent and three of
+// mantissa; 512 f is a whole number.  NaN (all of exponent and mantissa set) counts as 0.
+__device__ __forceinline__ int32_t units_of(uint32_t code, bool* nan) {
+  const uint32_t e = code >> 3 & 15, m = code & 7;
+  const uint32_t u = e == 0 ? m : (8 + m) << (e - 1);  // 512 |f|
+  const int32_t v = static_cast<int32_t>((u + 3 + (u >> 3 & 1)) >> 3);
+  *nan = (code & 0x7f) == 0x7f;
+  return *nan ? 0 : code & 0x80 ? -v : v;
+}
+
+__global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __restrict__ w8, uint32_t d_out, uint32_t d_in,
+                                                            uint32_t steps, size_t lanes, int32_t* bad,
+                                                            v4i* __restrict__ frag) {
+  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;
+  if (idx >= lanes) return;
+  const uint32_t lane = idx & 63;
+  const uint32_t step = static_cast<uint32_t>((idx >> 6) % steps), tile = static_cast<uint32_t>((idx >> 6) / steps);
+  const uint32_t row = tile * 32 + (lane & 31), k0 = step * kStep + 16 * (lane >> 5);
+  const uint8_t* w = w8 + static_cast<size_t>(row) * d_in;
+  v4i f[kDigits];
+  int32_t nans = 0;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    uint32_t lo = 0, hi = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = k0 + 4 * d + e;
+      bool nan = false;
+      const int32_t v = row < d_out && k < d_in ? units_of(w[k], &nan) : 0;
+      nans += nan;
+      const uint32_t b = (static_cast<uint32_t>(v) + 0x8080u) ^ 0x8080u;  // its low two bytes, as int8, are the digits
+      lo |= (b & 0xffu) << (8 * e);
+      hi |= (b >> 8 & 0xffu) << (8 * e);
+    }
+    f[0][d] = static_cast<int>(lo);
+    f[1][d] = static_cast<int>(hi);
+  }
+  if (bad && nans) atomicAdd(bad, nans);
+#pragma unroll
+  for (int d = 0; d < kDigits; ++d) frag[((idx >> 6) * kDigits + d) * 64 + lane] = f[d];
+}
+
+__global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const float* __restrict__ scales, uint32_t d_out,
+                                                             uint32_t block_rows, uint32_t blocks, uint32_t tiles,
+                                                             size_t total, double scale, int32_t* bad,
+                                                             int32_t* __restrict__ out) {
+  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][block][32]
+  if (idx >= total) return;
+  const uint32_t block = static_cast<uint32_t>((idx >> 5) % blocks);
+  const size_t lt = (idx >> 5) / blocks;
+  const uint32_t l = static_cast<uint32_t>(lt / tiles);
+  const uint32_t row = static_cast<uint32_t>(lt % tiles) * 32 + (idx & 31);
+  const uint32_t q = tb.q[l];
+  uint32_t r = 0;
+  if (row < d_out) {
+    const float s = scales[static_cast<size_t>(row / block_rows) * blocks + block];
+    const bool fine = isfinite(s);
+    if (fine) r = reduce_f64_int(rint(static_cast<double>(s) * scale), q, tb.q_recip[l]);
+    if (bad && !fine && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
+  }
+#pragma unroll
+  for (int d = 0; d < 3; ++d) {
+    r = static_cast<uint32_t>((static_cast<uint64_t>(r) << (d == 0 ? 32 : 16)) % q);
+    out[((idx >> 5) * 3 + d) * 32 + (idx & 31)] = centred(r, q);
+  }
+}
+
+// A layer, or a layer for each expert, and what it is applied to.
+struct Layers {
+  const uint8_t* w;       // [experts]: fragments, then scales
+  size_t w_bytes;         // of one expert
+  const uint32_t* ct_in;  // [bundles][d_in][2][limbs][N]
+  uint32_t* ct_out;       // [requests][d_out][2][limbs][N]
+  const int32_t* expert;  // [requests], or null: expert 0
+  const int32_t* bundle;  // [requests], or null: the request's own number
+  int32_t* status;        // [requests], or null
+  uint32_t experts, bundles, d_out, d_in, limbs;
+  Shape sh;
+};
+
+// Where a workgroup finds its part of a request.
+struct Job {
+  const v4i* frag;
+  const int32_t* scales;   // the limb's
+  const uint32_t* src;     // input 0's word of column 0 of the workgroup
+  uint32_t* dst;           // output 0's
+  uint32_t row_bytes, d_out, d_in, steps, blocks, limb, split;
+};
+
+__device__ __forceinline__ bool named(const Layers& a, uint32_t request, uint32_t* expert, uint32_t* bundle) {
+  *expert = a.expert ? static_cast<uint32_t>(a.expert[request]) : 0;
+  *bundle = a.bundle ? static_cast<uint32_t>(a.bundle[request]) : request;
+  return *expert < a.experts && *bundle < a.bundles;
+}
+
+// The status of requests for layers without outputs.
+__global__ __launch_bounds__(kThreads) void experts_status_kernel(Layers a, uint32_t count) {
+  const uint32_t r = blockIdx.x * kThreads + threadIdx.x;
+  uint32_t e, b;
+  if (r < count) a.status[r] = named(a, r, &e, &b) ? kExpertOk : kExpertBadRequest;
+}
+
+// The workgroup's request, limb, `cols` columns and share of the row tiles; false where the request names no
+// expert or no bundle.  Consecutive workgroup ids alternate XCDs: each XCD takes a contiguous range of
+// (request, limb, column strip, row split), so that workgroups which share columns or weights meet in one L2.
+__device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, Job* job) {
+  const uint32_t G = gridDim.x;
+  uint32_t lid = blockIdx.x;
+  if ((G & 7u) == 0) lid = (lid & 7u) * (G >> 3) + (lid >> 3);
+  const uint32_t n = tb.n, strips = 2 * n / cols, per = strips * a.limbs * splits;
+  const uint32_t r = lid / per, in = lid - r * per;
+  const uint32_t split = in % splits, lc = in / splits, l = lc / strips, col0 = (lc - l * strips) * cols;
+  uint32_t e, b;
+  const bool good = named(a, r, &e, &b);
+  if (a.status && in == 0 && threadIdx.x == 0) a.status[r] = good ? kExpertOk : kExpertBadRequest;
+  if (!good) return false;
+  const uint8_t* w = a.w + e * a.w_bytes;
+  const size_t at = (static_cast<size_t>(col0 >> tb.log_n) * a.limbs + l) * n + (col0 & (n - 1));
+  const size_t row_words = static_cast<size_t>(2) * a.limbs * n;
+  *job = {reinterpret_cast<const v4i*>(w),
+          reinterpret_cast<const int32_t*>(w + a.sh.frag_bytes) + static_cast<size_t>(l) * a.sh.tiles * a.sh.blocks * 96,
+          a.ct_in + b * row_words * a.d_in + at,
+          a.ct_out + r * row_words * a.d_out + at,
+          static_cast<uint32_t>(row_words * 4), a.d_out, a.d_in, a.sh.steps, a.sh.blocks, l, split};
+  return true;
+}
+
+// T / 2^32 mod q in [0, q) for |T| <= 1.88 q 2^32 (Montgomery's reduction): with m = T / q mod 2^32 the
+// difference T - m q is a multiple of 2^32 whose quotient is hi(T) - hi(m q).  h = hi(T) is taken to [0,
+// 2q) first (for h < 0 the sum h + 2q is below 2^31 and h itself, unsigned, above; for h >= 0 h is the smaller), the
+// difference lies in (-q, 2q), and two conditional corrections finish.  The bound holds over kFoldBlocks
+// blocks: per block |a| <= 128 (128 * 128 + 256 (128 * 128 + 112 * 128)) < 1.010e9, |b| <= 128 (128 * 128 + 112 *
+// 128 + 256 (128 * 64 + 112 * 128)) < 0.742e9, |c| <= 128 * 112 * 64 < 0.001e9 times centred scales of at
+// most q / 2 is 0.877e9 q, eight of them and a sum carried over from earlier blocks, at most q q / 2 < 0.537e9 q, are
+// 7.56e9 q < 1.77 q 2^32 (and below 2^63).
+__device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
+  const uint32_t h = static_cast<uint32_t>(t >> 32);
+  const uint32_t k = static_cast<uint32_t>(t) * m.qinv;
+  const uint32_t s = min(h, h + 2 * m.q) - __umulhi(k, m.q);
+  const uint32_t u = min(s, s + m.q);
+  return min(u, u - m.q);
+}
+
+// The digit sums of a step.
+__device__ __forceinline__ void contract(const v4i (&x)[4], const v4i (&w)[kDigits], v16i (&m)[kPairs]) {
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[b], w[d], m[b + d], 0, 0, 0);
+}
+
+// A block's digit sums, times its scales, onto the 64-bit sums.
+__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const int32_t* scales, int64_t (&acc)[16]) {
+  const uint32_t row = threadIdx.x & 31;
+  const int64_t sa = scales[row], sb = scales[32 + row], sc = scales[64 + row];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    acc[r] += sa * (m[0][r] + (m[1][r] << 8));
+    acc[r] += sb * (m[2][r] + (m[3][r] << 8));
+    acc[r] += sc * m[4][r];
+  }
+}
+
+// A row tile's outputs; rows past d_out are out of range.
+__device__ __forceinline__ void store(const Job& job, uint32_t tile, const Modulus& q, const int64_t (&acc)[16]) {
+  const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
+  const uint32_t rows = min(job.d_out - row0, 32u);
+  const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(job.dst + static_cast<size_t>(row0) * (job.row_bytes >> 2), 0,
+                                                       static_cast<int>(rows * job.row_bytes), kRsrcWord3);
+#pragma unroll
+  for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
+    v4i u;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(reduce(acc[4 * r4 + r], q));
+    __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * job.row_bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
+  }
+}
+
+// A wave has 32 columns and one row tile, and its residues go from memory to registers to the matrix cores: a
+// lane's digits of 16 inputs of one column are its operand, so there is no LDS and nothing to wait for
+// but the loads.
+constexpr uint32_t kThinCols = kThreads / 64 * 32;
+__global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, Layers a) {
+  Job job;
+  if (!place_of(tb, a, kThinCols, a.sh.tiles, &job)) return;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  job.src += wave * 32;
+  job.dst += wave * 32;
+  const Modulus q = modulus(tb.q[job.limb]);
+  const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
+  int64_t acc[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0;
+  for (uint32_t g = 0; g < job.blocks; ++g) {
+    if (g != 0 && g % kFoldBlocks == 0) {  // the sum so far, reduced, goes on as a product
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
+    }
+    v16i m[kPairs];
+#pragma unroll
+    for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
+    const uint32_t end = min(job.steps, (g + 1) * kBlockSteps);
+    for (uint32_t s = g * kBlockSteps; s < end; ++s) {
+      const uint32_t base = s * kStep;
+      // inputs past d_in read as zero through the buffer range check
+      const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint32_t*>(job.src) + static_cast<size_t>(base) * (job.row_bytes >> 2), 0,
+          static_cast<int>(min(job.d_in - base, kStep) * job.row_bytes), kRsrcWord3);
+      uint32_t x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * job.row_bytes + (lane & 31) * 4, 0, 0);
+      const v4i* wp = job.frag + (static_cast<size_t>(job.split) * job.steps + s) * kDigits * 64 + lane;
+      const v4i w[kDigits] = {wp[0], wp[64]};
+      v4i f[4];
+      to_fragments(x, f);
+      contract(f, w, m);
+    }
+    combine(m, job.scales + (static_cast<size_t>(job.split) * job.blocks + g) * 96, acc);
+  }
+  store(job, job.split, q, acc);
+}
+
+}  // namespace
+
+size_t fp8_weight_bytes(uint32_t d_out, uint32_t d_in, uint32_t limbs) {
+  if (d_out == 0 || d_in == 0) return 0;
+  const Shape s = shape_of(d_out, d_in, limbs);
+  return s.frag_bytes + s.scale_bytes;
+}
+
+hipError_t launch_encode_fp8(const Tables& t, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, hipStream_t s) {
+  const Shape sh = shape_of(d_out, d_in, limbs);
+  uint8_t* base = static_cast<uint8_t*>(w_fp8);
+  if (bad)
+    if (hipError_t e = launch_zero(reinterpret_cast<uint32_t*>(bad), 1, s); e != hipSuccess) return e;
+  const size_t lanes = static_cast<size_t>(sh.tiles) * sh.steps * 64;
+  if (lanes / kThreads > 0x7FFFFFFFu) return hipErrorInvalidConfiguration;
+  fp8_frag_kernel<<<static_cast<uint32_t>((lanes + kThreads - 1) / kThreads), kThreads, 0, s>>>(
+      w8, d_out, d_in, sh.steps, lanes, bad, reinterpret_cast<v4i*>(base));
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const size_t total = static_cast<size_t>(limbs) * sh.tiles * sh.blocks * 32;
+  fp8_scale_kernel<<<static_cast<uint32_t>((total + kThreads - 1) / kThreads), kThreads, 0, s>>>(
+      t, scales, d_out, block_rows, sh.blocks, sh.tiles, total, scale / 64, bad,
+      reinterpret_cast<int32_t*>(base + sh.frag_bytes));
+  return hipGetLastError();
+}
+
+hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, const int32_t* expert,
+                          const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
+                          uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, hipStream_t s) {
+  Layers a{static_cast<const uint8_t*>(w_fp8), fp8_weight_bytes(d_out, d_in, limbs), ct_in, ct_out, expert, bundle, status,
+           experts, bundles, d_out, d_in, limbs, shape_of(d_out, d_in, limbs)};
+  if (d_out == 0) {
+    if (!status) return hipSuccess;
+    experts_status_kernel<<<(count + kThreads - 1) / kThreads, kThreads, 0, s>>>(a, count);
+    return hipGetLastError();
+  }
+  const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols) * a.sh.tiles;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
+  mac_fp8_thin_kernel<<<static_cast<uint32_t>(grid), kThreads, 0, s>>>(t, a);
+  return hipGetLastError();
+}
+
+}  // namespace ckks

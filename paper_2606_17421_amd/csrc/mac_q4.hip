@@ -33,8 +33,6 @@
 namespace ckks {
 namespace {
 
-typedef int v16i __attribute__((ext_vector_type(16)));
-
 constexpr int kThreads = 256;        // encode kernels
 constexpr uint32_t kStep = 32;       // inputs of one matrix-core step
 constexpr uint32_t kCols = 32;       // columns of a workgroup
@@ -117,10 +115,6 @@ __global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __rest
     }
     frag[idx] = make_uint2(word[0], word[1]);
   }
-}
-
-__device__ __forceinline__ int32_t centred(uint32_t r, uint32_t q) {
-  return r > (q >> 1) ? static_cast<int32_t>(r - q) : static_cast<int32_t>(r);
 }
 
 __global__ __launch_bounds__(kThreads) void q4_scale_kernel(Tables tb, const float* __restrict__ scales,
@@ -207,15 +201,6 @@ __device__ __forceinline__ void place(uint32_t b0, uint32_t blocks, const uint32
 // inputs: |16 v| <= 128 times digit pairs of at most 128 * 257 and 128 + 64 * 256,
 // times centred scales of at most q / 2, is 0.754 q 2^32, and a sum carried over
 // from earlier inputs adds q q / 2 < 0.125 q 2^32.
-struct Modulus {
-  uint32_t q, qinv;  // qinv = 1 / q mod 2^32
-};
-__device__ __forceinline__ Modulus modulus(uint32_t q) {
-  uint32_t v = q;  // right mod 2^3 for odd q; each step doubles the bits
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v *= 2u - q * v;
-  return {q, v};
-}
 __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   const uint32_t k = static_cast<uint32_t>(t) * m.qinv;
   const uint32_t s = static_cast<uint32_t>(t >> 32) - __umulhi(k, m.q);
