@@ -22,6 +22,8 @@ constexpr uint32_t kBlockSteps = kBlock / kStep;
 constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 64-bit sums
 constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
 constexpr int kDigits = 2;            // of a weight
+constexpr int kWaves = 8;             // of a workgroup of the chunked kernel
+constexpr int kStepFrags = 4 * 64;    // 16-byte residue fragments of a step: four digits, 64 lanes
 
 // Encoded weights (written once a layer):
 //   fragments [tile][step][digit][64 lanes] of 16 bytes: digit of row tile*32 + lane%32 and inputs
@@ -145,15 +147,12 @@ __global__ __launch_bounds__(kThreads) void experts_status_kernel(Layers a, uint
   if (r < count) a.status[r] = named(a, r, &e, &b) ? kExpertOk : kExpertBadRequest;
 }
 
-// The workgroup's request, limb, `cols` columns and share of the row tiles; false where the request names no
-// expert or no bundle.  Consecutive workgroup ids alternate XCDs: each XCD takes a contiguous range of
-// (request, limb, column strip, row split), so that workgroups which share columns or weights meet in one L2.
-__device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, Job* job) {
-  const uint32_t G = gridDim.x;
-  uint32_t lid = blockIdx.x;
-  if ((G & 7u) == 0) lid = (lid & 7u) * (G >> 3) + (lid >> 3);
+// Request, limb, `cols` columns and share of the row tiles of a workgroup's job; false where the request names no
+// expert or no bundle.  Jobs are numbered by request, limb, column strip and row split, so that neighbours share
+// columns or weights.
+__device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, uint32_t id, Job* job) {
   const uint32_t n = tb.n, strips = 2 * n / cols, per = strips * a.limbs * splits;
-  const uint32_t r = lid / per, in = lid - r * per;
+  const uint32_t r = id / per, in = id - r * per;
   const uint32_t split = in % splits, lc = in / splits, l = lc / strips, col0 = (lc - l * strips) * cols;
   uint32_t e, b;
   const bool good = named(a, r, &e, &b);
@@ -169,6 +168,54 @@ __device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint
           static_cast<uint32_t>(row_words * 4), a.d_out, a.d_in, a.sh.steps, a.sh.blocks, l, split};
   return true;
 }
+
+// Consecutive workgroup ids alternate XCDs; the workgroups of one XCD take a contiguous range of `jobs`, next to each
+// other at any time: `first`, then every `stride`-th below `end`.
+struct Range {
+  uint32_t first, stride, end;
+};
+__device__ __forceinline__ Range range_of(uint32_t jobs) {
+  const uint32_t G = gridDim.x, id = blockIdx.x;
+  if (G < 8) return {id, G, jobs};
+  const uint32_t xcd = id & 7, each = jobs / 8, rest = jobs % 8;  // the first `rest` XCDs take one more
+  const uint32_t begin = xcd * each + min(xcd, rest);
+  return {begin + (id >> 3), (G - xcd + 7) / 8, begin + each + (xcd < rest)};
+}
+
+// The residues of a chunk in registers: 16 consecutive inputs of one column a lane and pass.  Unit u of a chunk is step
+// u / kColWaves of columns 32 (u % kColWaves) and on; a wave takes every 8th.  Inputs past d_in read as zero through
+// the buffer range check.
+template <int kColWaves, int kPasses>
+struct Chunk {
+  uint32_t x[kPasses][16];
+  __device__ __forceinline__ void fetch(const Job& job, uint32_t step0) {
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const uint32_t u = wave + p * kWaves, base = (step0 + u / kColWaves) * kStep;
+      const uint32_t rows = base < job.d_in ? min(job.d_in - base, kStep) : 0;
+      const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint32_t*>(job.src) + u % kColWaves * 32 + (rows ? static_cast<size_t>(base) * (job.row_bytes >> 2) : 0),
+          0, static_cast<int>(rows * job.row_bytes), kRsrcWord3);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[p][i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * job.row_bytes + (lane & 31) * 4, 0, 0);
+    }
+  }
+  // As digit fragments [column tile][step] in LDS.
+  __device__ __forceinline__ void place(v4i* lds) const {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr uint32_t kSteps = kWaves * kPasses / kColWaves;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const uint32_t u = wave + p * kWaves;
+      v4i f[4];
+      to_fragments(x[p], f);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) lds[(u % kColWaves * kSteps + u / kColWaves) * kStepFrags + d * 64 + lane] = f[d];
+    }
+  }
+};
 
 // T / 2^32 mod q in [0, q) for |T| <= 1.88 q 2^32 (Montgomery's reduction): with m = T / q mod 2^32 the
 // difference T - m q is a multiple of 2^32 whose quotient is hi(T) - hi(m q).  h = hi(T) is taken to [0,
@@ -186,23 +233,81 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
-// The digit sums of a step.
-__device__ __forceinline__ void contract(const v4i (&x)[4], const v4i (&w)[kDigits], v16i (&m)[kPairs]) {
-#pragma unroll
-  for (int b = 0; b < 4; ++b)
-#pragma unroll
-    for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[b], w[d], m[b + d], 0, 0, 0);
-}
-
 // A block's digit sums, times its scales, onto the 64-bit sums.
-__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const int32_t* scales, int64_t (&acc)[16]) {
-  const uint32_t row = threadIdx.x & 31;
-  const int64_t sa = scales[row], sb = scales[32 + row], sc = scales[64 + row];
+__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const int32_t (&sc)[3], int64_t (&acc)[16]) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    acc[r] += sa * (m[0][r] + (m[1][r] << 8));
-    acc[r] += sb * (m[2][r] + (m[3][r] << 8));
-    acc[r] += sc * m[4][r];
+    acc[r] += static_cast<int64_t>(sc[0]) * (m[0][r] + (m[1][r] << 8));
+    acc[r] += static_cast<int64_t>(sc[1]) * (m[2][r] + (m[3][r] << 8));
+    acc[r] += static_cast<int64_t>(sc[2]) * m[4][r];
+  }
+}
+
+__device__ __forceinline__ void clear(int64_t (&acc)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0;
+}
+
+// The sum so far, reduced, goes on as a product.
+__device__ __forceinline__ void fold(const Modulus& q, int32_t c32, int64_t (&acc)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
+}
+
+// A row tile's next weights and scales: of one block, asked for while the block ahead of it is contracted.
+// Steps past the layer's last are the last one again.
+struct Ahead {
+  v4i w[kBlockSteps][kDigits];
+  int32_t sc[3];
+  __device__ __forceinline__ void load(const Job& job, uint32_t tile, uint32_t block) {
+    const uint32_t lane = threadIdx.x & 63;
+    const v4i* p = job.frag + static_cast<size_t>(tile) * job.steps * (kDigits * 64) + lane;
+#pragma unroll
+    for (uint32_t s = 0; s < kBlockSteps; ++s) {
+      const v4i* at = p + static_cast<size_t>(min(block * kBlockSteps + s, job.steps - 1)) * (kDigits * 64);
+#pragma unroll
+      for (int d = 0; d < kDigits; ++d) w[s][d] = at[d * 64];
+    }
+    const int32_t* c = job.scales + (static_cast<size_t>(tile) * job.blocks + block) * 96 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32];
+  }
+};
+
+// A block of kSteps steps whose residues are at `f`: its digit sums, and onto the 64-bit sums.
+template <uint32_t kSteps>
+__device__ __forceinline__ void block_of(const Ahead& a, const v4i* f, int64_t (&acc)[16]) {
+  v16i m[kPairs];
+#pragma unroll
+  for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
+#pragma unroll
+  for (uint32_t s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const v4i x = f[s * kStepFrags + b * 64];
+#pragma unroll
+      for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, a.w[s][d], m[b + d], 0, 0, 0);
+    }
+  combine(m, a.sc, acc);
+}
+
+// Blocks g0 .. g0 + blocks - 1 of the layer, whose residues are at `lds`.  `next` holds the first one's weights, and
+// is left with those of block `after` of row tile `then` of another job.
+__device__ __forceinline__ void contract(const Job& job, uint32_t tile, uint32_t g0, uint32_t blocks, const Job& other,
+                                         uint32_t then, uint32_t after, const v4i* lds, Ahead& next, int64_t (&acc)[16]) {
+  const v4i* f = lds + (threadIdx.x & 63);
+  for (uint32_t g = 0; g < blocks; ++g, f += kBlockSteps * kStepFrags) {
+    const Ahead now = next;
+    if (g + 1 < blocks)
+      next.load(job, tile, g0 + g + 1);
+    else
+      next.load(other, then, after);
+    switch (min(job.steps - (g0 + g) * kBlockSteps, kBlockSteps)) {
+      case 1: block_of<1>(now, f, acc); break;
+      case 2: block_of<2>(now, f, acc); break;
+      case 3: block_of<3>(now, f, acc); break;
+      default: block_of<4>(now, f, acc); break;
+    }
   }
 }
 
@@ -227,20 +332,16 @@ __device__ __forceinline__ void store(const Job& job, uint32_t tile, const Modul
 constexpr uint32_t kThinCols = kThreads / 64 * 32;
 __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, Layers a) {
   Job job;
-  if (!place_of(tb, a, kThinCols, a.sh.tiles, &job)) return;
+  if (!place_of(tb, a, kThinCols, 1, range_of(gridDim.x).first, &job)) return;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   job.src += wave * 32;
   job.dst += wave * 32;
   const Modulus q = modulus(tb.q[job.limb]);
   const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
   int64_t acc[16];
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0;
+  clear(acc);
   for (uint32_t g = 0; g < job.blocks; ++g) {
-    if (g != 0 && g % kFoldBlocks == 0) {  // the sum so far, reduced, goes on as a product
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
-    }
+    if (g != 0 && g % kFoldBlocks == 0) fold(q, c32, acc);
     v16i m[kPairs];
 #pragma unroll
     for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
@@ -259,11 +360,100 @@ __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, La
       const v4i w[kDigits] = {wp[0], wp[64]};
       v4i f[4];
       to_fragments(x, f);
-      contract(f, w, m);
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[b], w[d], m[b + d], 0, 0, 0);
     }
-    combine(m, job.scales + (static_cast<size_t>(job.split) * job.blocks + g) * 96, acc);
+    const int32_t* c = job.scales + (static_cast<size_t>(job.split) * job.blocks + g) * 96 + (lane & 31);
+    const int32_t sc[3] = {c[0], c[32], c[64]};
+    combine(m, sc, acc);
   }
   store(job, job.split, q, acc);
+}
+
+// A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
+// jobs and their chunks of inputs without a pause: the next chunk's residues, of this job or the next, are in
+// flight in registers while the matrix cores work on this one's out of the other half of the LDS.
+template <int kColWaves, int kPasses>
+__global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
+  constexpr uint32_t kCols = kColWaves * 32, kChunk = kWaves * kPasses / kColWaves, kChunkBlocks = kChunk / kBlockSteps;
+  static_assert(kChunk % kBlockSteps == 0 && kFoldBlocks % kChunkBlocks == 0, "whole blocks, and reductions between chunks");
+  __shared__ v4i lds[2][kColWaves * kChunk * kStepFrags];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
+  const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits;
+  const Range range = range_of(jobs);
+  uint32_t id = range.first;
+  // the next job from id on that names an expert and a bundle
+  auto seek = [&](Job* job) {
+    for (; id < range.end; id += range.stride)
+      if (place_of(tb, a, kCols, splits, id, job)) {
+        id += range.stride;
+        return true;
+      }
+    return false;
+  };
+  Job job;
+  if (!seek(&job)) return;
+  Chunk<kColWaves, kPasses> chunk;
+  Ahead next;
+  chunk.fetch(job, 0);
+  next.load(job, min(job.split * each + row_wave, tiles - 1), 0);
+  chunk.place(lds[0]);
+  __syncthreads();
+  uint32_t buf = 0;
+  for (bool going = true; going;) {
+    const Modulus q = modulus(tb.q[job.limb]);
+    const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
+    const uint32_t tile = job.split * each + row_wave;
+    const bool mine = row_wave < each && tile < tiles;
+    int64_t acc[16];
+    clear(acc);
+    Job after = job;
+    for (uint32_t g0 = 0; g0 < job.blocks; g0 += kChunkBlocks, buf ^= 1) {
+      const bool last = g0 + kChunkBlocks >= job.blocks;
+      if (last) going = seek(&after);
+      const uint32_t g1 = last ? 0 : g0 + kChunkBlocks;  // where the next chunk begins
+      if (!last || going) chunk.fetch(after, g1 * kBlockSteps);
+      if (mine && g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+      if (mine)
+        contract(job, tile, g0, min(kChunkBlocks, job.blocks - g0), after, min(after.split * each + row_wave, tiles - 1), g1,
+                 lds[buf] + col_wave * kChunk * kStepFrags, next, acc);
+      else if (last)
+        next.load(after, min(after.split * each + row_wave, tiles - 1), 0);
+      if (last && mine) {
+        job.dst += col_wave * 32;
+        store(job, tile, q, acc);
+      }
+      if (!last || going) chunk.place(lds[buf ^ 1]);
+      __syncthreads();
+    }
+    job = after;
+  }
+}
+
+// Zeros, for layers without inputs.
+__global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layers a, uint32_t count) {
+  const size_t words = static_cast<size_t>(a.d_out) * 2 * a.limbs * tb.n;
+  for (uint32_t r = blockIdx.y; r < count; r += gridDim.y) {
+    uint32_t e, b;
+    const bool good = named(a, r, &e, &b);
+    if (a.status && blockIdx.x == 0 && threadIdx.x == 0) a.status[r] = good ? kExpertOk : kExpertBadRequest;
+    if (!good) continue;
+    for (size_t i = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x; i < words; i += static_cast<size_t>(gridDim.x) * kThreads)
+      a.ct_out[r * words + i] = 0;
+  }
+}
+
+template <int kColWaves, int kPasses>
+hipError_t launch_chunked(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
+  constexpr uint32_t kRowWaves = kWaves / kColWaves;
+  const uint32_t splits = (a.sh.tiles + kRowWaves - 1) / kRowWaves;
+  const uint64_t jobs = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / (32 * kColWaves)) * splits;
+  if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
+  const uint32_t grid = jobs < t.num_cus ? static_cast<uint32_t>(jobs) : t.num_cus;
+  mac_fp8_kernel<kColWaves, kPasses><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -302,7 +492,15 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
     experts_status_kernel<<<(count + kThreads - 1) / kThreads, kThreads, 0, s>>>(a, count);
     return hipGetLastError();
   }
-  const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols) * a.sh.tiles;
+  if (d_in == 0) {
+    experts_zero_kernel<<<dim3(64, count < 1024 ? count : 1024), kThreads, 0, s>>>(t, a, count);
+    return hipGetLastError();
+  }
+  if (a.sh.tiles > 1) {
+    const uint32_t four = (a.sh.tiles + 3) / 4 * 4, eight = (a.sh.tiles + 7) / 8 * 8;
+    return four < eight ? launch_chunked<2, 1>(t, a, count, s) : launch_chunked<1, 1>(t, a, count, s);
+  }
+  const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols);
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   mac_fp8_thin_kernel<<<static_cast<uint32_t>(grid), kThreads, 0, s>>>(t, a);
   return hipGetLastError();
