@@ -254,61 +254,64 @@ __device__ __forceinline__ void fold(const Modulus& q, int32_t c32, int64_t (&ac
   for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
 }
 
-// A row tile's next weights and scales: of one block, asked for while the block ahead of it is contracted.
-// Steps past the layer's last are the last one again.
-struct Ahead {
+// A wave's weights and scales of one block.  They are loaded again, for the block that comes next, as soon as they are
+// used, so that a block's contraction covers the loads; steps past the layer's last read as zero through the
+// buffer range check.
+struct Weights {
   v4i w[kBlockSteps][kDigits];
   int32_t sc[3];
-  __device__ __forceinline__ void load(const Job& job, uint32_t tile, uint32_t block) {
-    const uint32_t lane = threadIdx.x & 63;
-    const v4i* p = job.frag + static_cast<size_t>(tile) * job.steps * (kDigits * 64) + lane;
+  __device__ __forceinline__ void load_step(const rsrc_t& rs, uint32_t block, uint32_t s) {
+    const uint32_t at = (block * kBlockSteps + s) * (kDigits * 1024) + (threadIdx.x & 63) * 16;
 #pragma unroll
-    for (uint32_t s = 0; s < kBlockSteps; ++s) {
-      const v4i* at = p + static_cast<size_t>(min(block * kBlockSteps + s, job.steps - 1)) * (kDigits * 64);
+    for (int d = 0; d < kDigits; ++d) w[s][d] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(rs, at + d * 1024, 0, 0);
+  }
+  __device__ __forceinline__ void load_scales(const int32_t* tile_scales, uint32_t block) {
+    const int32_t* c = tile_scales + static_cast<size_t>(block) * 96;
 #pragma unroll
-      for (int d = 0; d < kDigits; ++d) w[s][d] = at[d * 64];
-    }
-    const int32_t* c = job.scales + (static_cast<size_t>(tile) * job.blocks + block) * 96 + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32];
+    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32 + (threadIdx.x & 31)];
   }
 };
 
-// A block of kSteps steps whose residues are at `f`: its digit sums, and onto the 64-bit sums.
-template <uint32_t kSteps>
-__device__ __forceinline__ void block_of(const Ahead& a, const v4i* f, int64_t (&acc)[16]) {
+// Where a wave finds a row tile's weights.
+struct Source {
+  rsrc_t frag;
+  const int32_t* scales;
+};
+__device__ __forceinline__ Source source_of(const Job& job, uint32_t tile) {
+  return {__builtin_amdgcn_make_buffer_rsrc(const_cast<v4i*>(job.frag) + static_cast<size_t>(tile) * job.steps * (kDigits * 64), 0,
+                                            static_cast<int>(job.steps * kDigits * 1024), kRsrcWord3),
+          job.scales + static_cast<size_t>(tile) * job.blocks * 96};
+}
+
+// Residue digits of a step, from LDS.
+__device__ __forceinline__ void read(const v4i* f, v4i (&x)[4]) {
+#pragma unroll
+  for (int b = 0; b < 4; ++b) x[b] = f[b * 64];
+}
+
+// One block of `steps` steps whose residues are at `f` (the first step's already in x[0]): its digit sums, and onto the
+// 64-bit sums.  A step's residues are read while the step before is contracted, those at `f_next` during
+// the last one; the weights of block `after` of `next` take the place of those used.
+__device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i* f_next, const Source& next, uint32_t after,
+                                         Weights& w, v4i (&x)[2][4], int64_t (&acc)[16]) {
   v16i m[kPairs];
 #pragma unroll
   for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
 #pragma unroll
-  for (uint32_t s = 0; s < kSteps; ++s)
+  for (uint32_t s = 0; s < kBlockSteps; ++s) {
+    if (s == 0 || s < steps) {
+      read(s + 1 < kBlockSteps ? f + (s + 1) * kStepFrags : f_next, x[(s + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const v4i x = f[s * kStepFrags + b * 64];
+      for (int d = 0; d < kDigits; ++d)
 #pragma unroll
-      for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, a.w[s][d], m[b + d], 0, 0, 0);
+        for (int b = 0; b < 4; ++b) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s & 1][b], w.w[s][d], m[b + d], 0, 0, 0);
     }
-  combine(m, a.sc, acc);
-}
-
-// Blocks g0 .. g0 + blocks - 1 of the layer, whose residues are at `lds`.  `next` holds the first one's weights, and
-// is left with those of block `after` of row tile `then` of another job.
-__device__ __forceinline__ void contract(const Job& job, uint32_t tile, uint32_t g0, uint32_t blocks, const Job& other,
-                                         uint32_t then, uint32_t after, const v4i* lds, Ahead& next, int64_t (&acc)[16]) {
-  const v4i* f = lds + (threadIdx.x & 63);
-  for (uint32_t g = 0; g < blocks; ++g, f += kBlockSteps * kStepFrags) {
-    const Ahead now = next;
-    if (g + 1 < blocks)
-      next.load(job, tile, g0 + g + 1);
-    else
-      next.load(other, then, after);
-    switch (min(job.steps - (g0 + g) * kBlockSteps, kBlockSteps)) {
-      case 1: block_of<1>(now, f, acc); break;
-      case 2: block_of<2>(now, f, acc); break;
-      case 3: block_of<3>(now, f, acc); break;
-      default: block_of<4>(now, f, acc); break;
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    w.load_step(next.frag, after, s);
   }
+  combine(m, w.sc, acc);
+  w.load_scales(next.scales, after);
 }
 
 // A row tile's outputs; rows past d_out are out of range.
@@ -396,9 +399,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
   Job job;
   if (!seek(&job)) return;
   Chunk<kColWaves, kPasses> chunk;
-  Ahead next;
+  Weights w;
+  // waves without a row tile in a job's last split contract the last tile again, which costs no time of the others
+  auto source = [&](const Job& j) { return source_of(j, min(j.split * each + row_wave, tiles - 1)); };
+  const bool works = row_wave < each;
   chunk.fetch(job, 0);
-  next.load(job, min(job.split * each + row_wave, tiles - 1), 0);
+  Source src = source(job);
+#pragma unroll
+  for (uint32_t s = 0; s < kBlockSteps; ++s) w.load_step(src.frag, 0, s);
+  w.load_scales(src.scales, 0);
   chunk.place(lds[0]);
   __syncthreads();
   uint32_t buf = 0;
@@ -406,22 +415,32 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
     const Modulus q = modulus(tb.q[job.limb]);
     const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
     const uint32_t tile = job.split * each + row_wave;
-    const bool mine = row_wave < each && tile < tiles;
     int64_t acc[16];
     clear(acc);
     Job after = job;
     for (uint32_t g0 = 0; g0 < job.blocks; g0 += kChunkBlocks, buf ^= 1) {
       const bool last = g0 + kChunkBlocks >= job.blocks;
-      if (last) going = seek(&after);
+      if (last) {
+        going = seek(&after);
+        src = source(after);
+      }
       const uint32_t g1 = last ? 0 : g0 + kChunkBlocks;  // where the next chunk begins
       if (!last || going) chunk.fetch(after, g1 * kBlockSteps);
-      if (mine && g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
-      if (mine)
-        contract(job, tile, g0, min(kChunkBlocks, job.blocks - g0), after, min(after.split * each + row_wave, tiles - 1), g1,
-                 lds[buf] + col_wave * kChunk * kStepFrags, next, acc);
-      else if (last)
-        next.load(after, min(after.split * each + row_wave, tiles - 1), 0);
-      if (last && mine) {
+      if (works) {
+        if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+        const v4i* f = lds[buf] + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
+        const uint32_t blocks = min(kChunkBlocks, job.blocks - g0);
+        const Source here = source(job);
+        v4i x[2][4];
+        read(f, x[0]);
+        for (uint32_t g = 0; g < blocks; ++g) {
+          const bool more = g + 1 < blocks;
+          const v4i* f_next = more ? f + kBlockSteps * kStepFrags : f;
+          contract(f, job.steps - (g0 + g) * kBlockSteps, f_next, more ? here : src, more ? g0 + g + 1 : g1, w, x, acc);
+          f = f_next;
+        }
+      }
+      if (last && works && tile < tiles) {
         job.dst += col_wave * 32;
         store(job, tile, q, acc);
       }
