@@ -23,6 +23,7 @@ constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 6
 constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
 constexpr int kDigits = 2;            // of a weight
 constexpr int kWaves = 8;             // of a workgroup of the chunked kernel
+constexpr uint32_t kChunk = 8;         // steps that are in LDS at a time, and the next as many
 constexpr int kStepFrags = 4 * 64;    // 16-byte residue fragments of a step: four digits, 64 lanes
 
 // Encoded weights (written once a layer):
@@ -131,8 +132,10 @@ struct Job {
   const int32_t* scales;   // the limb's
   const uint32_t* src;     // input 0's word of column 0 of the workgroup
   uint32_t* dst;           // output 0's
-  uint32_t row_bytes, d_out, d_in, steps, blocks, limb, split;
+  uint32_t limb, split;
 };
+
+__device__ __forceinline__ uint32_t row_bytes(const Tables& tb, const Layers& a) { return 8u * a.limbs * tb.n; }
 
 __device__ __forceinline__ bool named(const Layers& a, uint32_t request, uint32_t* expert, uint32_t* bundle) {
   *expert = a.expert ? static_cast<uint32_t>(a.expert[request]) : 0;
@@ -164,8 +167,7 @@ __device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint
   *job = {reinterpret_cast<const v4i*>(w),
           reinterpret_cast<const int32_t*>(w + a.sh.frag_bytes) + static_cast<size_t>(l) * a.sh.tiles * a.sh.blocks * 96,
           a.ct_in + b * row_words * a.d_in + at,
-          a.ct_out + r * row_words * a.d_out + at,
-          static_cast<uint32_t>(row_words * 4), a.d_out, a.d_in, a.sh.steps, a.sh.blocks, l, split};
+          a.ct_out + r * row_words * a.d_out + at, l, split};
   return true;
 }
 
@@ -182,38 +184,30 @@ __device__ __forceinline__ Range range_of(uint32_t jobs) {
   return {begin + (id >> 3), (G - xcd + 7) / 8, begin + each + (xcd < rest)};
 }
 
-// The residues of a chunk in registers: 16 consecutive inputs of one column a lane and pass.  Unit u of a chunk is step
-// u / kColWaves of columns 32 (u % kColWaves) and on; a wave takes every 8th.  Inputs past d_in read as zero through
+// Residues on their way to LDS: 16 consecutive inputs of one column a lane.  Unit u of a chunk is step u / kColWaves of
+// columns 32 (u % kColWaves) and on; a wave takes every 8th, one a pass.  Inputs past d_in read as zero through
 // the buffer range check.
-template <int kColWaves, int kPasses>
-struct Chunk {
-  uint32_t x[kPasses][16];
-  __device__ __forceinline__ void fetch(const Job& job, uint32_t step0) {
+template <int kColWaves>
+struct Stage {
+  uint32_t x[16];
+  __device__ __forceinline__ void fetch(const Tables& tb, const Layers& a, const Job& job, uint32_t step0, int pass) {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t bytes = row_bytes(tb, a), u = wave + pass * kWaves, base = (step0 + u / kColWaves) * kStep;
+    const uint32_t rows = base < a.d_in ? min(a.d_in - base, kStep) : 0;
+    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint32_t*>(job.src) + u % kColWaves * 32 + (rows ? static_cast<size_t>(base) * (bytes >> 2) : 0),
+        0, static_cast<int>(rows * bytes), kRsrcWord3);
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const uint32_t u = wave + p * kWaves, base = (step0 + u / kColWaves) * kStep;
-      const uint32_t rows = base < job.d_in ? min(job.d_in - base, kStep) : 0;
-      const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint32_t*>(job.src) + u % kColWaves * 32 + (rows ? static_cast<size_t>(base) * (job.row_bytes >> 2) : 0),
-          0, static_cast<int>(rows * job.row_bytes), kRsrcWord3);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        x[p][i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * job.row_bytes + (lane & 31) * 4, 0, 0);
-    }
+    for (int i = 0; i < 16; ++i)
+      x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * bytes + (lane & 31) * 4, 0, 0);
   }
   // As digit fragments [column tile][step] in LDS.
-  __device__ __forceinline__ void place(v4i* lds) const {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr uint32_t kSteps = kWaves * kPasses / kColWaves;
+  __device__ __forceinline__ void place(v4i* lds, int pass) const {
+    const uint32_t lane = threadIdx.x & 63, u = (threadIdx.x >> 6) + pass * kWaves;
+    v4i f[4];
+    to_fragments(x, f);
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const uint32_t u = wave + p * kWaves;
-      v4i f[4];
-      to_fragments(x[p], f);
-#pragma unroll
-      for (int d = 0; d < 4; ++d) lds[(u % kColWaves * kSteps + u / kColWaves) * kStepFrags + d * 64 + lane] = f[d];
-    }
+    for (int d = 0; d < 4; ++d) lds[(u % kColWaves * kChunk + u / kColWaves) * kStepFrags + d * 64 + lane] = f[d];
   }
 };
 
@@ -254,34 +248,35 @@ __device__ __forceinline__ void fold(const Modulus& q, int32_t c32, int64_t (&ac
   for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
 }
 
-// A wave's weights and scales of one block.  They are loaded again, for the block that comes next, as soon as they are
-// used, so that a block's contraction covers the loads; steps past the layer's last read as zero through the
-// buffer range check.
-struct Weights {
-  v4i w[kBlockSteps][kDigits];
-  int32_t sc[3];
-  __device__ __forceinline__ void load_step(const rsrc_t& rs, uint32_t block, uint32_t s) {
-    const uint32_t at = (block * kBlockSteps + s) * (kDigits * 1024) + (threadIdx.x & 63) * 16;
-#pragma unroll
-    for (int d = 0; d < kDigits; ++d) w[s][d] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(rs, at + d * 1024, 0, 0);
-  }
-  __device__ __forceinline__ void load_scales(const int32_t* tile_scales, uint32_t block) {
-    const int32_t* c = tile_scales + static_cast<size_t>(block) * 96;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32 + (threadIdx.x & 31)];
-  }
-};
-
 // Where a wave finds a row tile's weights.
 struct Source {
   rsrc_t frag;
   const int32_t* scales;
 };
-__device__ __forceinline__ Source source_of(const Job& job, uint32_t tile) {
-  return {__builtin_amdgcn_make_buffer_rsrc(const_cast<v4i*>(job.frag) + static_cast<size_t>(tile) * job.steps * (kDigits * 64), 0,
-                                            static_cast<int>(job.steps * kDigits * 1024), kRsrcWord3),
-          job.scales + static_cast<size_t>(tile) * job.blocks * 96};
+__device__ __forceinline__ Source source_of(const Layers& a, const Job& job, uint32_t tile) {
+  return {__builtin_amdgcn_make_buffer_rsrc(const_cast<v4i*>(job.frag) + static_cast<size_t>(tile) * a.sh.steps * (kDigits * 64), 0,
+                                            static_cast<int>(a.sh.steps * kDigits * 1024), kRsrcWord3),
+          job.scales + static_cast<size_t>(tile) * a.sh.blocks * 96};
 }
+
+// A wave's weights and scales of one block.  They are loaded again, for the block after the next, as soon as they are
+// used, so that two blocks' contractions cover the loads (and the residues' before them, since a wave's loads are
+// waited for in order); steps past the layer's last read as zero through the
+// buffer range check.
+struct Weights {
+  v4i w[kBlockSteps][kDigits];
+  int32_t sc[3];
+  __device__ __forceinline__ void load_step(const Source& src, uint32_t block, uint32_t s) {
+    const uint32_t at = (block * kBlockSteps + s) * (kDigits * 1024) + (threadIdx.x & 63) * 16;
+#pragma unroll
+    for (int d = 0; d < kDigits; ++d) w[s][d] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(src.frag, at + d * 1024, 0, 0);
+  }
+  __device__ __forceinline__ void load_scales(const Source& src, uint32_t block, uint32_t blocks) {
+    const int32_t* c = src.scales + static_cast<size_t>(min(block, blocks - 1)) * 96;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32 + (threadIdx.x & 31)];
+  }
+};
 
 // Residue digits of a step, from LDS.
 __device__ __forceinline__ void read(const v4i* f, v4i (&x)[4]) {
@@ -289,43 +284,47 @@ __device__ __forceinline__ void read(const v4i* f, v4i (&x)[4]) {
   for (int b = 0; b < 4; ++b) x[b] = f[b * 64];
 }
 
-// One block of `steps` steps whose residues are at `f` (the first step's already in x[0]): its digit sums, and onto the
-// 64-bit sums.  A step's residues are read while the step before is contracted, those at `f_next` during
-// the last one; the weights of block `after` of `next` take the place of those used.
+// One block of `steps` steps, none included, whose residues are at `f` (the first step's already in x): its digit sums,
+// and onto the 64-bit sums.  A digit of the next step's residues is read as soon as this step's is used, those at
+// `f_next` during the last one; the weights of block `after` of `next` take the place of those used.
 __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i* f_next, const Source& next, uint32_t after,
-                                         Weights& w, v4i (&x)[2][4], int64_t (&acc)[16]) {
+                                         uint32_t blocks, Weights& w, v4i (&x)[4], int64_t (&acc)[16]) {
   v16i m[kPairs];
 #pragma unroll
-  for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
-#pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s) {
-    if (s == 0 || s < steps) {
-      read(s + 1 < kBlockSteps ? f + (s + 1) * kStepFrags : f_next, x[(s + 1) & 1]);
-      __builtin_amdgcn_sched_barrier(0);
+    if (s < steps) {
+      const v4i* ahead = s + 1 < kBlockSteps ? f + (s + 1) * kStepFrags : f_next;
 #pragma unroll
-      for (int d = 0; d < kDigits; ++d)
+      for (int b = 0; b < 4; ++b) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s & 1][b], w.w[s][d], m[b + d], 0, 0, 0);
+        for (int d = kDigits - 1; d >= 0; --d) {
+          const bool first = s == 0 && (b == 0 || d == 1);  // of sum b + d
+          m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[b], w.w[s][d], first ? v16i{} : m[b + d], 0, 0, 0);
+        }
+        x[b] = ahead[b * 64];
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+    w.load_step(next, after, s);
     __builtin_amdgcn_sched_barrier(0);
-    w.load_step(next.frag, after, s);
   }
-  combine(m, w.sc, acc);
-  w.load_scales(next.scales, after);
+  if (steps != 0) combine(m, w.sc, acc);
+  w.load_scales(next, after, blocks);
 }
 
 // A row tile's outputs; rows past d_out are out of range.
-__device__ __forceinline__ void store(const Job& job, uint32_t tile, const Modulus& q, const int64_t (&acc)[16]) {
+__device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile, const Modulus& q,
+                                      const int64_t (&acc)[16]) {
   const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
-  const uint32_t rows = min(job.d_out - row0, 32u);
-  const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(job.dst + static_cast<size_t>(row0) * (job.row_bytes >> 2), 0,
-                                                       static_cast<int>(rows * job.row_bytes), kRsrcWord3);
+  const uint32_t rows = min(d_out - row0, 32u);
+  const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(dst + static_cast<size_t>(row0) * (bytes >> 2), 0,
+                                                       static_cast<int>(rows * bytes), kRsrcWord3);
 #pragma unroll
   for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
     v4i u;
 #pragma unroll
     for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(reduce(acc[4 * r4 + r], q));
-    __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * job.row_bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
   }
 }
 
@@ -339,27 +338,28 @@ __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, La
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   job.src += wave * 32;
   job.dst += wave * 32;
+  const uint32_t bytes = row_bytes(tb, a);
   const Modulus q = modulus(tb.q[job.limb]);
   const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
   int64_t acc[16];
   clear(acc);
-  for (uint32_t g = 0; g < job.blocks; ++g) {
+  for (uint32_t g = 0; g < a.sh.blocks; ++g) {
     if (g != 0 && g % kFoldBlocks == 0) fold(q, c32, acc);
     v16i m[kPairs];
 #pragma unroll
     for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
-    const uint32_t end = min(job.steps, (g + 1) * kBlockSteps);
+    const uint32_t end = min(a.sh.steps, (g + 1) * kBlockSteps);
     for (uint32_t s = g * kBlockSteps; s < end; ++s) {
       const uint32_t base = s * kStep;
       // inputs past d_in read as zero through the buffer range check
       const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint32_t*>(job.src) + static_cast<size_t>(base) * (job.row_bytes >> 2), 0,
-          static_cast<int>(min(job.d_in - base, kStep) * job.row_bytes), kRsrcWord3);
+          const_cast<uint32_t*>(job.src) + static_cast<size_t>(base) * (bytes >> 2), 0,
+          static_cast<int>(min(a.d_in - base, kStep) * bytes), kRsrcWord3);
       uint32_t x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * job.row_bytes + (lane & 31) * 4, 0, 0);
-      const v4i* wp = job.frag + (static_cast<size_t>(job.split) * job.steps + s) * kDigits * 64 + lane;
+        x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * bytes + (lane & 31) * 4, 0, 0);
+      const v4i* wp = job.frag + (static_cast<size_t>(job.split) * a.sh.steps + s) * kDigits * 64 + lane;
       const v4i w[kDigits] = {wp[0], wp[64]};
       v4i f[4];
       to_fragments(x, f);
@@ -368,20 +368,20 @@ __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, La
 #pragma unroll
         for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[b], w[d], m[b + d], 0, 0, 0);
     }
-    const int32_t* c = job.scales + (static_cast<size_t>(job.split) * job.blocks + g) * 96 + (lane & 31);
+    const int32_t* c = job.scales + (static_cast<size_t>(job.split) * a.sh.blocks + g) * 96 + (lane & 31);
     const int32_t sc[3] = {c[0], c[32], c[64]};
     combine(m, sc, acc);
   }
-  store(job, job.split, q, acc);
+  store(job.dst, bytes, a.d_out, job.split, q, acc);
 }
 
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
-// jobs and their chunks of inputs without a pause: the next chunk's residues, of this job or the next, are in
-// flight in registers while the matrix cores work on this one's out of the other half of the LDS.
-template <int kColWaves, int kPasses>
+// jobs and their chunks of two blocks of inputs without a pause: the next chunk's residues, of this job or the
+// next, are in flight in registers while the matrix cores work on this one's out of the other half of the LDS.
+template <int kColWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
-  constexpr uint32_t kCols = kColWaves * 32, kChunk = kWaves * kPasses / kColWaves, kChunkBlocks = kChunk / kBlockSteps;
-  static_assert(kChunk % kBlockSteps == 0 && kFoldBlocks % kChunkBlocks == 0, "whole blocks, and reductions between chunks");
+  constexpr uint32_t kCols = kColWaves * 32, kChunkBlocks = 2;
+  static_assert(kChunk == kChunkBlocks * kBlockSteps && kFoldBlocks % kChunkBlocks == 0, "whole blocks, and reductions between chunks");
   __shared__ v4i lds[2][kColWaves * kChunk * kStepFrags];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits;
@@ -398,17 +398,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
   };
   Job job;
   if (!seek(&job)) return;
-  Chunk<kColWaves, kPasses> chunk;
-  Weights w;
-  // waves without a row tile in a job's last split contract the last tile again, which costs no time of the others
-  auto source = [&](const Job& j) { return source_of(j, min(j.split * each + row_wave, tiles - 1)); };
-  const bool works = row_wave < each;
-  chunk.fetch(job, 0);
+  const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
+  // waves without a row tile in a job's last split contract the last tile again, which costs no time of the others;
+  // those without one in any have no steps
+  auto source = [&](const Job& j) { return source_of(a, j, min(j.split * each + row_wave, tiles - 1)); };
+  const uint32_t my_steps = row_wave < each ? steps : 0;
+  Stage<kColWaves> stage;
+  Weights w[kChunkBlocks];
+#pragma unroll
+  for (int p = 0; p < kColWaves; ++p) {
+    stage.fetch(tb, a, job, 0, p);
+    stage.place(lds[0], p);
+  }
   Source src = source(job);
 #pragma unroll
-  for (uint32_t s = 0; s < kBlockSteps; ++s) w.load_step(src.frag, 0, s);
-  w.load_scales(src.scales, 0);
-  chunk.place(lds[0]);
+  for (uint32_t g = 0; g < kChunkBlocks; ++g) {
+#pragma unroll
+    for (uint32_t s = 0; s < kBlockSteps; ++s) w[g].load_step(src, g, s);
+    w[g].load_scales(src, g, blocks);
+  }
   __syncthreads();
   uint32_t buf = 0;
   for (bool going = true; going;) {
@@ -418,33 +426,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
     int64_t acc[16];
     clear(acc);
     Job after = job;
-    for (uint32_t g0 = 0; g0 < job.blocks; g0 += kChunkBlocks, buf ^= 1) {
-      const bool last = g0 + kChunkBlocks >= job.blocks;
+    for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks, buf ^= 1) {
+      const bool last = g0 + kChunkBlocks >= blocks;
       if (last) {
         going = seek(&after);
         src = source(after);
       }
-      const uint32_t g1 = last ? 0 : g0 + kChunkBlocks;  // where the next chunk begins
-      if (!last || going) chunk.fetch(after, g1 * kBlockSteps);
-      if (works) {
-        if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
-        const v4i* f = lds[buf] + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
-        const uint32_t blocks = min(kChunkBlocks, job.blocks - g0);
-        const Source here = source(job);
-        v4i x[2][4];
-        read(f, x[0]);
-        for (uint32_t g = 0; g < blocks; ++g) {
-          const bool more = g + 1 < blocks;
-          const v4i* f_next = more ? f + kBlockSteps * kStepFrags : f;
-          contract(f, job.steps - (g0 + g) * kBlockSteps, f_next, more ? here : src, more ? g0 + g + 1 : g1, w, x, acc);
-          f = f_next;
-        }
+      // where the next chunk begins; past the last job's end there is nothing to fetch
+      const uint32_t g1 = last ? 0 : g0 + kChunkBlocks, s0 = g0 * kBlockSteps, s1 = !last || going ? g1 * kBlockSteps : steps;
+      const v4i* f = lds[buf] + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
+      v4i x[4];
+      stage.fetch(tb, a, after, s1, 0);
+      if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+      read(f, x);
+      contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
+      if (kColWaves == 2) {
+        stage.place(lds[buf ^ 1], 0);
+        stage.fetch(tb, a, after, s1, 1);
       }
-      if (last && works && tile < tiles) {
-        job.dst += col_wave * 32;
-        store(job, tile, q, acc);
-      }
-      if (!last || going) chunk.place(lds[buf ^ 1]);
+      f += kBlockSteps * kStepFrags;
+      contract(f, max(my_steps, s0 + kBlockSteps) - (s0 + kBlockSteps), f, src, g1 + 1, blocks, w[1], x, acc);
+      if (last && row_wave < each && tile < tiles) store(job.dst + col_wave * 32, bytes, a.d_out, tile, q, acc);
+      stage.place(lds[buf ^ 1], kColWaves - 1);
       __syncthreads();
     }
     job = after;
@@ -464,14 +467,14 @@ __global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layer
   }
 }
 
-template <int kColWaves, int kPasses>
+template <int kColWaves>
 hipError_t launch_chunked(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
   constexpr uint32_t kRowWaves = kWaves / kColWaves;
   const uint32_t splits = (a.sh.tiles + kRowWaves - 1) / kRowWaves;
   const uint64_t jobs = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / (32 * kColWaves)) * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const uint32_t grid = jobs < t.num_cus ? static_cast<uint32_t>(jobs) : t.num_cus;
-  mac_fp8_kernel<kColWaves, kPasses><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  mac_fp8_kernel<kColWaves><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
 }
 
@@ -517,7 +520,7 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
   }
   if (a.sh.tiles > 1) {
     const uint32_t four = (a.sh.tiles + 3) / 4 * 4, eight = (a.sh.tiles + 7) / 8 * 8;
-    return four < eight ? launch_chunked<2, 1>(t, a, count, s) : launch_chunked<1, 1>(t, a, count, s);
+    return four < eight ? launch_chunked<2>(t, a, count, s) : launch_chunked<1>(t, a, count, s);
   }
   const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols);
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
