@@ -10,6 +10,8 @@
 // digits and twelve; what the rounding to 64ths costs is 2^-7 at most of a weight below 1/8, 2^-16 of the largest one.
 // T = a + 2^16 b + 2^32 c with a and b from two digit sums each and c from one; a block's scale enters
 // in 64-bit integers, and the sum over the blocks is reduced once an output.
+#include <algorithm>
+
 #include "digits.hpp"
 
 namespace ckks {
@@ -22,8 +24,7 @@ constexpr uint32_t kBlockSteps = kBlock / kStep;
 constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 64-bit sums
 constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
 constexpr int kDigits = 2;            // of a weight
-constexpr int kWaves = 8;             // of a workgroup of the chunked kernel
-constexpr uint32_t kChunk = 8;         // steps that are in LDS at a time, and the next as many
+constexpr uint32_t kChunkBlocks = 2, kChunk = kChunkBlocks * kBlockSteps;  // blocks and steps that go into LDS at a time
 constexpr int kStepFrags = 4 * 64;    // 16-byte residue fragments of a step: four digits, 64 lanes
 
 // Encoded weights (written once a layer):
@@ -113,6 +114,10 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
   }
 }
 
+// LDS that the digits of 32 columns take.
+constexpr size_t kLdsBytes = 160 << 10;
+size_t strip_bytes(const Shape& s) { return static_cast<size_t>(s.steps + kChunk - 1) / kChunk * kChunk * kStepFrags * 16; }
+
 // A layer, or a layer for each expert, and what it is applied to.
 struct Layers {
   const uint8_t* w;       // [experts]: fragments, then scales
@@ -187,7 +192,7 @@ __device__ __forceinline__ Range range_of(uint32_t jobs) {
 // Residues on their way to LDS: 16 consecutive inputs of one column a lane.  Unit u of a chunk is step u / kColWaves of
 // columns 32 (u % kColWaves) and on; a wave takes every 8th, one a pass.  Inputs past d_in read as zero through
 // the buffer range check.
-template <int kColWaves>
+template <int kWaves, int kColWaves>
 struct Stage {
   uint32_t x[16];
   __device__ __forceinline__ void fetch(const Tables& tb, const Layers& a, const Job& job, uint32_t step0, int pass) {
@@ -378,10 +383,12 @@ __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, La
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
 // jobs and their chunks of two blocks of inputs without a pause: the next chunk's residues, of this job or the
 // next, are in flight in registers while the matrix cores work on this one's out of the other half of the LDS.
-template <int kColWaves>
+template <int kWaves, int kColWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
-  constexpr uint32_t kCols = kColWaves * 32, kChunkBlocks = 2;
-  static_assert(kChunk == kChunkBlocks * kBlockSteps && kFoldBlocks % kChunkBlocks == 0, "whole blocks, and reductions between chunks");
+  constexpr uint32_t kCols = kColWaves * 32;
+  constexpr int kPasses = kChunk * kColWaves / kWaves;
+  static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
+  static_assert(kFoldBlocks % kChunkBlocks == 0, "reductions between chunks");
   __shared__ v4i lds[2][kColWaves * kChunk * kStepFrags];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits;
@@ -403,10 +410,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
   // those without one in any have no steps
   auto source = [&](const Job& j) { return source_of(a, j, min(j.split * each + row_wave, tiles - 1)); };
   const uint32_t my_steps = row_wave < each ? steps : 0;
-  Stage<kColWaves> stage;
+  Stage<kWaves, kColWaves> stage;
   Weights w[kChunkBlocks];
 #pragma unroll
-  for (int p = 0; p < kColWaves; ++p) {
+  for (int p = 0; p < kPasses; ++p) {
     stage.fetch(tb, a, job, 0, p);
     stage.place(lds[0], p);
   }
@@ -440,16 +447,100 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
       if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
       read(f, x);
       contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
-      if (kColWaves == 2) {
+      if (kPasses == 2) {
         stage.place(lds[buf ^ 1], 0);
         stage.fetch(tb, a, after, s1, 1);
       }
       f += kBlockSteps * kStepFrags;
       contract(f, max(my_steps, s0 + kBlockSteps) - (s0 + kBlockSteps), f, src, g1 + 1, blocks, w[1], x, acc);
       if (last && row_wave < each && tile < tiles) store(job.dst + col_wave * 32, bytes, a.d_out, tile, q, acc);
-      stage.place(lds[buf ^ 1], kColWaves - 1);
+      stage.place(lds[buf ^ 1], kPasses - 1);
       __syncthreads();
     }
+    job = after;
+  }
+}
+
+// Inputs whose digits all fit the LDS: a workgroup converts its columns once a job and its waves walk the row tiles of
+// the job's split, kRowWaves apart, with nothing to wait for but their weights.  During the last of them a chunk's
+// place in LDS is given to the next job's residues as soon as every wave is through with it, so that only
+// this pass has barriers and the matrix cores do not pause between jobs.
+template <int kWaves, int kColWaves>
+__global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
+  constexpr uint32_t kCols = kColWaves * 32, kRowWaves = kWaves / kColWaves;
+  constexpr int kPasses = kChunk * kColWaves / kWaves;
+  static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
+  constexpr uint32_t kChunkFrags = kColWaves * kChunk * kStepFrags;
+  extern __shared__ v4i whole[];  // [chunks][kChunkFrags]
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
+  const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kRowWaves - 1) / kRowWaves;
+  const Range range = range_of(jobs);
+  uint32_t id = range.first;
+  auto seek = [&](Job* job) {
+    for (; id < range.end; id += range.stride)
+      if (place_of(tb, a, kCols, splits, id, job)) {
+        id += range.stride;
+        return true;
+      }
+    return false;
+  };
+  Job job;
+  if (!seek(&job)) return;
+  const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
+  auto source = [&](const Job& j, uint32_t at) { return source_of(a, j, min(j.split * each + at, tiles - 1)); };
+  Stage<kWaves, kColWaves> stage;
+  Weights w[kChunkBlocks];
+  for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks)
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      stage.fetch(tb, a, job, g0 * kBlockSteps, p);
+      stage.place(whole + g0 / kChunkBlocks * kChunkFrags, p);
+    }
+  Source src = source(job, row_wave);
+#pragma unroll
+  for (uint32_t g = 0; g < kChunkBlocks; ++g) {
+#pragma unroll
+    for (uint32_t s = 0; s < kBlockSteps; ++s) w[g].load_step(src, g, s);
+    w[g].load_scales(src, g, blocks);
+  }
+  __syncthreads();
+  for (bool going = true; going;) {
+    const Modulus q = modulus(tb.q[job.limb]);
+    const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
+    Job after = job;
+    for (uint32_t pass = 0; pass < passes; ++pass) {
+      const uint32_t at = pass * kRowWaves + row_wave, tile = job.split * each + at;
+      const bool last = pass + 1 == passes, works = at < each && tile < tiles;
+      const uint32_t my_steps = works ? steps : 0;
+      if (last) going = seek(&after);
+      int64_t acc[16];
+      clear(acc);
+      for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks) {
+        const bool end = g0 + kChunkBlocks >= blocks;
+        if (end) src = source(after, last ? row_wave : at + kRowWaves);
+        const uint32_t g1 = end ? 0 : g0 + kChunkBlocks, s0 = g0 * kBlockSteps, s1 = going ? s0 : steps;
+        v4i* chunk = whole + g0 / kChunkBlocks * kChunkFrags;
+        const v4i* f = chunk + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
+        v4i x[4];
+        if (last) stage.fetch(tb, a, after, s1, 0);
+        if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+        read(f, x);
+        contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
+        if (kPasses == 2 && last) {
+          __syncthreads();
+          stage.place(chunk, 0);
+          stage.fetch(tb, a, after, s1, 1);
+        }
+        f += kBlockSteps * kStepFrags;
+        contract(f, max(my_steps, s0 + kBlockSteps) - (s0 + kBlockSteps), f, src, g1 + 1, blocks, w[1], x, acc);
+        if (last) {
+          __syncthreads();
+          stage.place(chunk, kPasses - 1);
+        }
+      }
+      if (works) store(job.dst + col_wave * 32, bytes, a.d_out, tile, q, acc);
+    }
+    __syncthreads();
     job = after;
   }
 }
@@ -467,14 +558,21 @@ __global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layer
   }
 }
 
-template <int kColWaves>
-hipError_t launch_chunked(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
+template <int kWaves, int kColWaves, bool kWhole>
+hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
   constexpr uint32_t kRowWaves = kWaves / kColWaves;
-  const uint32_t splits = (a.sh.tiles + kRowWaves - 1) / kRowWaves;
-  const uint64_t jobs = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / (32 * kColWaves)) * splits;
+  const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / (32 * kColWaves));
+  const uint32_t most = t.num_cus * (8 / kWaves), groups = (a.sh.tiles + kRowWaves - 1) / kRowWaves;
+  // the chunked kernel has one row tile a wave; the whole one splits the rows only where the columns alone leave CUs idle
+  const uint32_t splits = kWhole ? static_cast<uint32_t>(std::min<uint64_t>(groups, (most + strips - 1) / strips)) : groups;
+  const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  const uint32_t grid = jobs < t.num_cus ? static_cast<uint32_t>(jobs) : t.num_cus;
-  mac_fp8_kernel<kColWaves><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  const uint32_t grid = jobs < most ? static_cast<uint32_t>(jobs) : most;
+  if constexpr (kWhole)
+    mac_fp8_whole_kernel<kWaves, kColWaves><<<grid, kWaves * 64, strip_bytes(a.sh) * kColWaves, s>>>(
+        t, a, splits, static_cast<uint32_t>(jobs));
+  else
+    mac_fp8_kernel<kWaves, kColWaves><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
 }
 
@@ -520,7 +618,9 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
   }
   if (a.sh.tiles > 1) {
     const uint32_t four = (a.sh.tiles + 3) / 4 * 4, eight = (a.sh.tiles + 7) / 8 * 8;
-    return four < eight ? launch_chunked<2>(t, a, count, s) : launch_chunked<1>(t, a, count, s);
+    if (2 * strip_bytes(a.sh) <= kLdsBytes && four < eight) return launch<8, 2, true>(t, a, count, s);
+    if (strip_bytes(a.sh) <= kLdsBytes) return launch<8, 1, true>(t, a, count, s);
+    return four < eight ? launch<8, 2, false>(t, a, count, s) : launch<8, 1, false>(t, a, count, s);
   }
   const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols);
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
