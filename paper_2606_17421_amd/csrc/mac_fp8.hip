@@ -197,7 +197,9 @@ struct Stage {
   uint32_t x[16];
   __device__ __forceinline__ void fetch(const Tables& tb, const Layers& a, const Job& job, uint32_t step0, int pass) {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t bytes = row_bytes(tb, a), u = wave + pass * kWaves, base = (step0 + u / kColWaves) * kStep;
+    uint32_t bytes = row_bytes(tb, a);
+    asm volatile("" : "+s"(bytes));  // else the 16 rows' offsets are kept in registers
+    const uint32_t u = wave + pass * kWaves, base = (step0 + u / kColWaves) * kStep;
     const uint32_t rows = base < a.d_in ? min(a.d_in - base, kStep) : 0;
     const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint32_t*>(job.src) + u % kColWaves * 32 + (rows ? static_cast<size_t>(base) * (bytes >> 2) : 0),
@@ -245,6 +247,11 @@ __device__ __forceinline__ void combine(const v16i (&m)[kPairs], const int32_t (
 __device__ __forceinline__ void clear(int64_t (&acc)[16]) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0;
+}
+
+__device__ __forceinline__ void reduce(const int64_t (&acc)[16], const Modulus& q, uint32_t (&y)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) y[r] = reduce(acc[r], q);
 }
 
 // The sum so far, reduced, goes on as a product.
@@ -318,8 +325,8 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
 }
 
 // A row tile's outputs; rows past d_out are out of range.
-__device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile, const Modulus& q,
-                                      const int64_t (&acc)[16]) {
+__device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile,
+                                      const uint32_t (&y)[16]) {
   const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
   const uint32_t rows = min(d_out - row0, 32u);
   const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(dst + static_cast<size_t>(row0) * (bytes >> 2), 0,
@@ -328,7 +335,7 @@ __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_
   for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
     v4i u;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(reduce(acc[4 * r4 + r], q));
+    for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(y[4 * r4 + r]);
     __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
   }
 }
@@ -377,7 +384,9 @@ __global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, La
     const int32_t sc[3] = {c[0], c[32], c[64]};
     combine(m, sc, acc);
   }
-  store(job.dst, bytes, a.d_out, job.split, q, acc);
+  uint32_t y[16];
+  reduce(acc, q, y);
+  store(job.dst, bytes, a.d_out, job.split, y);
 }
 
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
@@ -453,7 +462,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
       }
       f += kBlockSteps * kStepFrags;
       contract(f, max(my_steps, s0 + kBlockSteps) - (s0 + kBlockSteps), f, src, g1 + 1, blocks, w[1], x, acc);
-      if (last && row_wave < each && tile < tiles) store(job.dst + col_wave * 32, bytes, a.d_out, tile, q, acc);
+      if (last && row_wave < each && tile < tiles) {
+        uint32_t y[16];
+        reduce(acc, q, y);
+        store(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
+      }
       stage.place(lds[buf ^ 1], kPasses - 1);
       __syncthreads();
     }
@@ -465,15 +478,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
 // the job's split, kRowWaves apart, with nothing to wait for but their weights.  During the last of them a chunk's
 // place in LDS is given to the next job's residues as soon as every wave is through with it, so that only
 // this pass has barriers and the matrix cores do not pause between jobs.
-template <int kWaves, int kColWaves>
+//
+// The row tiles that are no multiple of kRowWaves come first.  Where they are at most half of it (and others
+// follow), with kJoin, two waves take a tile's chunks half and half and their sums meet in LDS.
+template <int kWaves, int kColWaves, bool kJoin>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
   constexpr uint32_t kCols = kColWaves * 32, kRowWaves = kWaves / kColWaves;
   constexpr int kPasses = kChunk * kColWaves / kWaves;
   static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
   constexpr uint32_t kChunkFrags = kColWaves * kChunk * kStepFrags;
-  extern __shared__ v4i whole[];  // [chunks][kChunkFrags]
+  extern __shared__ v4i whole[];  // [chunks][kChunkFrags], with kJoin [kWaves / 2][4][64]
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kRowWaves - 1) / kRowWaves;
+  const uint32_t rest = each - (passes - 1) * kRowWaves;  // row tiles of the first pass
   const Range range = range_of(jobs);
   uint32_t id = range.first;
   auto seek = [&](Job* job) {
@@ -487,6 +504,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   Job job;
   if (!seek(&job)) return;
   const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
+  const uint32_t chunks = (blocks + kChunkBlocks - 1) / kChunkBlocks;
+  // the wave's row tile of a pass, counted in the split, and its chunks
+  const bool joins = kJoin && passes > 1 && rest <= kRowWaves / 2 && chunks > 1, upper = joins && row_wave >= kRowWaves / 2;
+  const uint32_t at0 = upper ? row_wave - kRowWaves / 2 : row_wave, half = joins ? (chunks + 1) / 2 : chunks;
+  const uint32_t begin0 = upper ? half : 0, end0 = upper ? chunks : half;
+  auto at_of = [&](uint32_t pass) { return pass == 0 ? at0 : rest + (pass - 1) * kRowWaves + row_wave; };
   auto source = [&](const Job& j, uint32_t at) { return source_of(a, j, min(j.split * each + at, tiles - 1)); };
   Stage<kWaves, kColWaves> stage;
   Weights w[kChunkBlocks];
@@ -496,12 +519,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       stage.fetch(tb, a, job, g0 * kBlockSteps, p);
       stage.place(whole + g0 / kChunkBlocks * kChunkFrags, p);
     }
-  Source src = source(job, row_wave);
+  Source src = source(job, at0);
 #pragma unroll
   for (uint32_t g = 0; g < kChunkBlocks; ++g) {
 #pragma unroll
-    for (uint32_t s = 0; s < kBlockSteps; ++s) w[g].load_step(src, g, s);
-    w[g].load_scales(src, g, blocks);
+    for (uint32_t s = 0; s < kBlockSteps; ++s) w[g].load_step(src, begin0 * kChunkBlocks + g, s);
+    w[g].load_scales(src, begin0 * kChunkBlocks + g, blocks);
   }
   __syncthreads();
   for (bool going = true; going;) {
@@ -509,21 +532,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
     const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
     Job after = job;
     for (uint32_t pass = 0; pass < passes; ++pass) {
-      const uint32_t at = pass * kRowWaves + row_wave, tile = job.split * each + at;
-      const bool last = pass + 1 == passes, works = at < each && tile < tiles;
-      const uint32_t my_steps = works ? steps : 0;
+      const uint32_t at = at_of(pass), tile = job.split * each + at;
+      const bool last = pass + 1 == passes, works = (pass != 0 || at < rest) && tile < tiles;
+      const uint32_t my_steps = works ? steps : 0, begin = pass == 0 ? begin0 : 0, end = pass == 0 ? end0 : chunks;
       if (last) going = seek(&after);
       int64_t acc[16];
       clear(acc);
-      for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks) {
-        const bool end = g0 + kChunkBlocks >= blocks;
-        if (end) src = source(after, last ? row_wave : at + kRowWaves);
-        const uint32_t g1 = end ? 0 : g0 + kChunkBlocks, s0 = g0 * kBlockSteps, s1 = going ? s0 : steps;
-        v4i* chunk = whole + g0 / kChunkBlocks * kChunkFrags;
+      for (uint32_t c = begin; c < end; ++c) {
+        if (c + 1 == end) src = source(after, last ? at0 : at_of(pass + 1));
+        const uint32_t g0 = c * kChunkBlocks, g1 = c + 1 < end ? g0 + kChunkBlocks : last ? begin0 * kChunkBlocks : 0;
+        const uint32_t s0 = g0 * kBlockSteps, s1 = going ? s0 : steps;
+        v4i* chunk = whole + c * kChunkFrags;
         const v4i* f = chunk + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
         v4i x[4];
         if (last) stage.fetch(tb, a, after, s1, 0);
-        if (g0 != 0 && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+        if (c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
         read(f, x);
         contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
         if (kPasses == 2 && last) {
@@ -538,7 +561,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
           stage.place(chunk, kPasses - 1);
         }
       }
-      if (works) store(job.dst + col_wave * 32, bytes, a.d_out, tile, q, acc);
+      uint32_t y[16];
+      reduce(acc, q, y);
+      if (joins && pass == 0) {
+        v4i* sums = whole + chunks * kChunkFrags + (wave % (kWaves / 2)) * 256 + (threadIdx.x & 63);
+        if (upper)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            v4i v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = static_cast<int>(y[4 * r4 + r]);
+            sums[r4 * 64] = v;
+          }
+        __syncthreads();
+        if (!upper)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const v4i v = sums[r4 * 64];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[4 * r4 + r] = add_mod(y[4 * r4 + r], static_cast<uint32_t>(v[r]), q.q);
+          }
+      }
+      if (works && !(upper && pass == 0)) store(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
     }
     __syncthreads();
     job = after;
@@ -558,6 +602,14 @@ __global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layer
   }
 }
 
+// Passes of `row_waves` waves over the row tiles, in halves: the rest of the tiles may take half a pass (see
+// mac_fp8_whole_kernel).
+uint32_t half_passes(const Shape& s, uint32_t row_waves, bool whole) {
+  const uint32_t full = s.tiles / row_waves, rest = s.tiles % row_waves;
+  const bool joins = whole && full > 0 && rest <= row_waves / 2 && s.steps > kChunk;
+  return 2 * full + (rest == 0 ? 0 : joins ? 1 : 2);
+}
+
 template <int kWaves, int kColWaves, bool kWhole>
 hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
   constexpr uint32_t kRowWaves = kWaves / kColWaves;
@@ -568,10 +620,12 @@ hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t 
   const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const uint32_t grid = jobs < most ? static_cast<uint32_t>(jobs) : most;
-  if constexpr (kWhole)
-    mac_fp8_whole_kernel<kWaves, kColWaves><<<grid, kWaves * 64, strip_bytes(a.sh) * kColWaves, s>>>(
-        t, a, splits, static_cast<uint32_t>(jobs));
-  else
+  if constexpr (kWhole) {
+    const size_t strip = strip_bytes(a.sh) * kColWaves, join = kWaves / 2 * 64 * 16 * 4;
+    const bool joins = strip + join <= kLdsBytes;
+    const auto k = joins ? mac_fp8_whole_kernel<kWaves, kColWaves, true> : mac_fp8_whole_kernel<kWaves, kColWaves, false>;
+    k<<<grid, kWaves * 64, joins ? strip + join : strip, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  } else
     mac_fp8_kernel<kWaves, kColWaves><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
 }
@@ -617,9 +671,11 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
     return hipGetLastError();
   }
   if (a.sh.tiles > 1) {
-    const uint32_t four = (a.sh.tiles + 3) / 4 * 4, eight = (a.sh.tiles + 7) / 8 * 8;
-    if (2 * strip_bytes(a.sh) <= kLdsBytes && four < eight) return launch<8, 2, true>(t, a, count, s);
-    if (strip_bytes(a.sh) <= kLdsBytes) return launch<8, 1, true>(t, a, count, s);
+    // passes over the row tiles for two column tiles, in halves: one of 8 or two of 4 at a time
+    const bool two = 2 * strip_bytes(a.sh) <= kLdsBytes, whole = strip_bytes(a.sh) <= kLdsBytes;
+    const uint32_t eight = 2 * half_passes(a.sh, 8, whole), four = half_passes(a.sh, 4, two);
+    if (two && four < eight) return launch<8, 2, true>(t, a, count, s);
+    if (whole) return launch<8, 1, true>(t, a, count, s);
     return four < eight ? launch<8, 2, false>(t, a, count, s) : launch<8, 1, false>(t, a, count, s);
   }
   const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols);
