@@ -118,6 +118,9 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
 constexpr size_t kLdsBytes = 160 << 10;
 size_t strip_bytes(const Shape& s) { return static_cast<size_t>(s.steps + kChunk - 1) / kChunk * kChunk * kStepFrags * 16; }
 
+template <int kWaves>
+constexpr size_t kJoinBytes = kWaves / 2 * 256 * 16;
+
 // A layer, or a layer for each expert, and what it is applied to.
 struct Layers {
   const uint8_t* w;       // [experts]: fragments, then scales
@@ -189,24 +192,30 @@ __device__ __forceinline__ Range range_of(uint32_t jobs) {
   return {begin + (id >> 3), (G - xcd + 7) / 8, begin + each + (xcd < rest)};
 }
 
-// Residues on their way to LDS: 16 consecutive inputs of one column a lane.  Unit u of a chunk is step u / kColWaves of
-// columns 32 (u % kColWaves) and on; a wave takes every 8th, one a pass.  Inputs past d_in read as zero through
-// the buffer range check.
+// 16 consecutive inputs of one column a lane: lane l has column l % 32 of those at `src`, and the first or the second
+// half of the 32 inputs from `base` on.  Inputs past d_in read as zero through the buffer range check.
+__device__ __forceinline__ void fetch_step(const Tables& tb, const Layers& a, const uint32_t* src, uint32_t base,
+                                           uint32_t (&x)[16]) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t bytes = row_bytes(tb, a);
+  asm volatile("" : "+s"(bytes));  // else the 16 rows' offsets are kept in registers
+  const uint32_t rows = base < a.d_in ? min(a.d_in - base, kStep) : 0;
+  const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint32_t*>(src) + (rows ? static_cast<size_t>(base) * (bytes >> 2) : 0), 0, static_cast<int>(rows * bytes),
+      kRsrcWord3);
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * bytes + (lane & 31) * 4, 0, 0);
+}
+
+// Residues on their way to LDS.  Unit u of a chunk is step u / kColWaves of columns 32 (u % kColWaves) and on; a wave
+// takes every kWaves-th, one a pass.
 template <int kWaves, int kColWaves>
 struct Stage {
   uint32_t x[16];
   __device__ __forceinline__ void fetch(const Tables& tb, const Layers& a, const Job& job, uint32_t step0, int pass) {
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint32_t bytes = row_bytes(tb, a);
-    asm volatile("" : "+s"(bytes));  // else the 16 rows' offsets are kept in registers
-    const uint32_t u = wave + pass * kWaves, base = (step0 + u / kColWaves) * kStep;
-    const uint32_t rows = base < a.d_in ? min(a.d_in - base, kStep) : 0;
-    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint32_t*>(job.src) + u % kColWaves * 32 + (rows ? static_cast<size_t>(base) * (bytes >> 2) : 0),
-        0, static_cast<int>(rows * bytes), kRsrcWord3);
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * bytes + (lane & 31) * 4, 0, 0);
+    const uint32_t u = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + pass * kWaves;
+    fetch_step(tb, a, job.src + u % kColWaves * 32, (step0 + u / kColWaves) * kStep, x);
   }
   // As digit fragments [column tile][step] in LDS.
   __device__ __forceinline__ void place(v4i* lds, int pass) const {
@@ -340,53 +349,90 @@ __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_
   }
 }
 
-// A wave has 32 columns and one row tile, and its residues go from memory to registers to the matrix cores: a
-// lane's digits of 16 inputs of one column are its operand, so there is no LDS and nothing to wait for
-// but the loads.
-constexpr uint32_t kThinCols = kThreads / 64 * 32;
-__global__ __launch_bounds__(kThreads, 2) void mac_fp8_thin_kernel(Tables tb, Layers a) {
+// Onto the sums of the waves of a workgroup's upper half those of its lower half's, through LDS [waves / 2][4][64], and so
+// on until the first of `slices` waves has the sum of all.
+__device__ __forceinline__ void join(uint32_t (&y)[16], uint32_t q, v4i* sums, uint32_t wave, uint32_t waves, uint32_t slices) {
+  for (uint32_t half = waves / 2; slices > 1; half /= 2, slices /= 2) {
+    v4i* at = sums + (wave % half) * 256 + (threadIdx.x & 63);
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        v4i v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = static_cast<int>(y[4 * r4 + r]);
+        at[r4 * 64] = v;
+      }
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const v4i v = at[r4 * 64];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[4 * r4 + r] = add_mod(y[4 * r4 + r], static_cast<uint32_t>(v[r]), q);
+      }
+    }
+    if (slices > 2) __syncthreads();
+  }
+}
+
+// A wave has 32 columns, one row tile and one of `slices` shares of the blocks, and its residues go from memory to
+// registers to the matrix cores: a lane's digits of 16 inputs of one column are its operand, so there is no LDS and
+// nothing to wait for but the loads, of which those of four steps are in flight.
+constexpr int kThinWaves = 8;  // of a workgroup, at most
+__global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
+  __shared__ v4i sums[kThinWaves / 2 * 256];
   Job job;
-  if (!place_of(tb, a, kThinCols, 1, range_of(gridDim.x).first, &job)) return;
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  job.src += wave * 32;
-  job.dst += wave * 32;
-  const uint32_t bytes = row_bytes(tb, a);
+  const uint32_t waves = blockDim.x / 64, strips = waves / slices;
+  if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % strips, slice = wave / strips;
+  const uint32_t blocks = a.sh.blocks, each = (blocks + slices - 1) / slices, steps = a.sh.steps;
+  const uint32_t begin = min(blocks, slice * each), end = min(blocks, begin + each);
   const Modulus q = modulus(tb.q[job.limb]);
   const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
+  const Source src = source_of(a, job, job.split);
+  job.src += strip * 32;
+  uint32_t x[kBlockSteps][16];
+  Weights w;
+#pragma unroll
+  for (uint32_t s = 0; s < kBlockSteps; ++s)
+    if (s == 0 || s < steps) {
+      fetch_step(tb, a, job.src, (begin * kBlockSteps + s) * kStep, x[s]);
+      w.load_step(src, begin, s);
+    }
+  w.load_scales(src, begin, blocks);
   int64_t acc[16];
   clear(acc);
-  for (uint32_t g = 0; g < a.sh.blocks; ++g) {
-    if (g != 0 && g % kFoldBlocks == 0) fold(q, c32, acc);
+  for (uint32_t g = begin; g < end; ++g) {
+    if (g != begin && (g - begin) % kFoldBlocks == 0) fold(q, c32, acc);
+    const uint32_t left = steps - g * kBlockSteps;
+    const bool more = g + 1 < end;
     v16i m[kPairs];
 #pragma unroll
-    for (int p = 0; p < kPairs; ++p) m[p] = v16i{};
-    const uint32_t end = min(a.sh.steps, (g + 1) * kBlockSteps);
-    for (uint32_t s = g * kBlockSteps; s < end; ++s) {
-      const uint32_t base = s * kStep;
-      // inputs past d_in read as zero through the buffer range check
-      const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint32_t*>(job.src) + static_cast<size_t>(base) * (bytes >> 2), 0,
-          static_cast<int>(min(a.d_in - base, kStep) * bytes), kRsrcWord3);
-      uint32_t x[16];
+    for (uint32_t s = 0; s < kBlockSteps; ++s) {
+      if (s < left) {
+        v4i f[4];
+        to_fragments(x[s], f);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        x[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane >> 5) * 16 + i) * bytes + (lane & 31) * 4, 0, 0);
-      const v4i* wp = job.frag + (static_cast<size_t>(job.split) * a.sh.steps + s) * kDigits * 64 + lane;
-      const v4i w[kDigits] = {wp[0], wp[64]};
-      v4i f[4];
-      to_fragments(x, f);
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int d = 0; d < kDigits; ++d) m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[b], w[d], m[b + d], 0, 0, 0);
+          for (int d = kDigits - 1; d >= 0; --d) {
+            const bool first = s == 0 && (b == 0 || d == 1);
+            m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[b], w.w[s][d], first ? v16i{} : m[b + d], 0, 0, 0);
+          }
+      }
+      if (more) {
+        fetch_step(tb, a, job.src, ((g + 1) * kBlockSteps + s) * kStep, x[s]);
+        w.load_step(src, g + 1, s);
+      }
     }
-    const int32_t* c = job.scales + (static_cast<size_t>(job.split) * a.sh.blocks + g) * 96 + (lane & 31);
-    const int32_t sc[3] = {c[0], c[32], c[64]};
-    combine(m, sc, acc);
+    combine(m, w.sc, acc);
+    if (more) w.load_scales(src, g + 1, blocks);
   }
   uint32_t y[16];
   reduce(acc, q, y);
-  store(job.dst, bytes, a.d_out, job.split, y);
+  join(y, q.q, sums, wave, waves, slices);
+  if (slice == 0) store(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
 }
 
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
@@ -475,27 +521,26 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
 }
 
 // Inputs whose digits all fit the LDS: a workgroup converts its columns once a job and its waves walk the row tiles of
-// the job's split, kRowWaves apart, with nothing to wait for but their weights.  During the last of them a chunk's
+// the job's split, kWaves apart, with nothing to wait for but their weights.  During the last of them a chunk's
 // place in LDS is given to the next job's residues as soon as every wave is through with it, so that only
 // this pass has barriers and the matrix cores do not pause between jobs.
 //
-// The row tiles that are no multiple of kRowWaves come first.  Where they are at most half of it (and others
+// The row tiles that are no multiple of kWaves come first.  Where they are at most half of it (and others
 // follow), with kJoin, two waves take a tile's chunks half and half and their sums meet in LDS.
-template <int kWaves, int kColWaves, bool kJoin>
+template <int kWaves, bool kJoin>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
-  constexpr uint32_t kCols = kColWaves * 32, kRowWaves = kWaves / kColWaves;
-  constexpr int kPasses = kChunk * kColWaves / kWaves;
+  constexpr int kPasses = kChunk / kWaves;
   static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
-  constexpr uint32_t kChunkFrags = kColWaves * kChunk * kStepFrags;
+  constexpr uint32_t kChunkFrags = kChunk * kStepFrags;
   extern __shared__ v4i whole[];  // [chunks][kChunkFrags], with kJoin [kWaves / 2][4][64]
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
-  const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kRowWaves - 1) / kRowWaves;
-  const uint32_t rest = each - (passes - 1) * kRowWaves;  // row tiles of the first pass
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kWaves - 1) / kWaves;
+  const uint32_t rest = each - (passes - 1) * kWaves;  // row tiles of the first pass
   const Range range = range_of(jobs);
   uint32_t id = range.first;
   auto seek = [&](Job* job) {
     for (; id < range.end; id += range.stride)
-      if (place_of(tb, a, kCols, splits, id, job)) {
+      if (place_of(tb, a, 32, splits, id, job)) {
         id += range.stride;
         return true;
       }
@@ -506,12 +551,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
   const uint32_t chunks = (blocks + kChunkBlocks - 1) / kChunkBlocks;
   // the wave's row tile of a pass, counted in the split, and its chunks
-  const bool joins = kJoin && passes > 1 && rest <= kRowWaves / 2 && chunks > 1, upper = joins && row_wave >= kRowWaves / 2;
-  const uint32_t at0 = upper ? row_wave - kRowWaves / 2 : row_wave, half = joins ? (chunks + 1) / 2 : chunks;
+  const bool joins = kJoin && passes > 1 && rest <= kWaves / 2 && chunks > 1, upper = joins && wave >= kWaves / 2;
+  const uint32_t at0 = upper ? wave - kWaves / 2 : wave, half = joins ? (chunks + 1) / 2 : chunks;
   const uint32_t begin0 = upper ? half : 0, end0 = upper ? chunks : half;
-  auto at_of = [&](uint32_t pass) { return pass == 0 ? at0 : rest + (pass - 1) * kRowWaves + row_wave; };
+  auto at_of = [&](uint32_t pass) { return pass == 0 ? at0 : rest + (pass - 1) * kWaves + wave; };
   auto source = [&](const Job& j, uint32_t at) { return source_of(a, j, min(j.split * each + at, tiles - 1)); };
-  Stage<kWaves, kColWaves> stage;
+  Stage<kWaves, 1> stage;
   Weights w[kChunkBlocks];
   for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks)
 #pragma unroll
@@ -543,7 +588,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
         const uint32_t g0 = c * kChunkBlocks, g1 = c + 1 < end ? g0 + kChunkBlocks : last ? begin0 * kChunkBlocks : 0;
         const uint32_t s0 = g0 * kBlockSteps, s1 = going ? s0 : steps;
         v4i* chunk = whole + c * kChunkFrags;
-        const v4i* f = chunk + col_wave * kChunk * kStepFrags + (threadIdx.x & 63);
+        const v4i* f = chunk + (threadIdx.x & 63);
         v4i x[4];
         if (last) stage.fetch(tb, a, after, s1, 0);
         if (c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
@@ -563,26 +608,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       }
       uint32_t y[16];
       reduce(acc, q, y);
-      if (joins && pass == 0) {
-        v4i* sums = whole + chunks * kChunkFrags + (wave % (kWaves / 2)) * 256 + (threadIdx.x & 63);
-        if (upper)
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            v4i v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = static_cast<int>(y[4 * r4 + r]);
-            sums[r4 * 64] = v;
-          }
-        __syncthreads();
-        if (!upper)
-#pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const v4i v = sums[r4 * 64];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[4 * r4 + r] = add_mod(y[4 * r4 + r], static_cast<uint32_t>(v[r]), q.q);
-          }
-      }
-      if (works && !(upper && pass == 0)) store(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
+      if (joins && pass == 0) join(y, q.q, whole + chunks * kChunkFrags, wave, kWaves, 2);
+      if (works && !(upper && pass == 0)) store(job.dst, bytes, a.d_out, tile, y);
     }
     __syncthreads();
     job = after;
@@ -602,32 +629,81 @@ __global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layer
   }
 }
 
-// Passes of `row_waves` waves over the row tiles, in halves: the rest of the tiles may take half a pass (see
-// mac_fp8_whole_kernel).
-uint32_t half_passes(const Shape& s, uint32_t row_waves, bool whole) {
-  const uint32_t full = s.tiles / row_waves, rest = s.tiles % row_waves;
-  const bool joins = whole && full > 0 && rest <= row_waves / 2 && s.steps > kChunk;
-  return 2 * full + (rest == 0 ? 0 : joins ? 1 : 2);
+uint32_t ceil_div(uint64_t a, uint32_t b) { return static_cast<uint32_t>((a + b - 1) / b); }
+
+hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStream_t s) {
+  uint32_t slices = 1;  // eight waves a CU where the blocks allow it
+  while (slices < kThinWaves && 2 * slices <= a.sh.blocks && waves * slices < t.num_cus * 8ull) slices *= 2;
+  const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
+  const uint64_t grid = waves * slices / group;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
+  mac_fp8_thin_kernel<<<static_cast<uint32_t>(grid), group * 64, 0, s>>>(t, a, slices);
+  return hipGetLastError();
 }
 
-template <int kWaves, int kColWaves, bool kWhole>
-hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
-  constexpr uint32_t kRowWaves = kWaves / kColWaves;
-  const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / (32 * kColWaves));
-  const uint32_t most = t.num_cus * (8 / kWaves), groups = (a.sh.tiles + kRowWaves - 1) / kRowWaves;
-  // the chunked kernel has one row tile a wave; the whole one splits the rows only where the columns alone leave CUs idle
-  const uint32_t splits = kWhole ? static_cast<uint32_t>(std::min<uint64_t>(groups, (most + strips - 1) / strips)) : groups;
+template <int kWaves, int kColWaves>
+hipError_t launch_chunked(const Tables& t, const Layers& a, uint64_t strips, hipStream_t s) {
+  const uint32_t splits = ceil_div(a.sh.tiles, kWaves / kColWaves);
+  const uint64_t jobs = strips / kColWaves * splits;
+  if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
+  mac_fp8_kernel<kWaves, kColWaves><<<static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus)), kWaves * 64, 0, s>>>(
+      t, a, splits, static_cast<uint32_t>(jobs));
+  return hipGetLastError();
+}
+
+template <int kWaves>
+hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint32_t splits, hipStream_t s) {
   const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  const uint32_t grid = jobs < most ? static_cast<uint32_t>(jobs) : most;
-  if constexpr (kWhole) {
-    const size_t strip = strip_bytes(a.sh) * kColWaves, join = kWaves / 2 * 64 * 16 * 4;
-    const bool joins = strip + join <= kLdsBytes;
-    const auto k = joins ? mac_fp8_whole_kernel<kWaves, kColWaves, true> : mac_fp8_whole_kernel<kWaves, kColWaves, false>;
-    k<<<grid, kWaves * 64, joins ? strip + join : strip, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
-  } else
-    mac_fp8_kernel<kWaves, kColWaves><<<grid, kWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
+  const size_t strip = strip_bytes(a.sh), both = strip + kJoinBytes<kWaves>;
+  if (both <= kLdsBytes)
+    mac_fp8_whole_kernel<kWaves, true><<<grid, kWaves * 64, both, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  else
+    mac_fp8_whole_kernel<kWaves, false><<<grid, kWaves * 64, strip, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
+}
+
+// The time of the whole kernel in hundredths of that of a chunked job, and its row splits: rounds of jobs over the
+// workgroups that fit the GPU, times `pass` for each pass over the row tiles and `fill` for the residues.
+struct Plan {
+  uint64_t time;
+  uint32_t splits;
+};
+Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t waves, uint32_t pass, uint32_t fill) {
+  Plan best{~0ull, 1};
+  for (uint32_t splits = 1; splits <= 8 && splits <= sh.tiles; ++splits) {
+    const uint32_t each = ceil_div(sh.tiles, splits), full = each / waves, rest = each % waves;
+    const uint32_t halves = 2 * full + (rest == 0 ? 0 : full > 0 && rest <= waves / 2 && sh.steps > kChunk ? 1 : 2);
+    const uint64_t rounds = ceil_div(strips * splits, t.num_cus * (8 / waves));
+    const uint64_t time = rounds * (pass * halves / 2 + fill);
+    if (time < best.time) best = {time, splits};
+  }
+  return best;
+}
+
+hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
+  const Shape& sh = a.sh;
+  const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / 32);
+  // No more than 32 outputs, two row tiles of one block of inputs, or too few columns for the other kernels.  Thin : the
+  // others, us, 2^14, 4 limbs: 16 -> 64 18 : 31, 128 -> 64 27 : 34, 256 -> 64 40 : 36, 64 -> 128 36 : 36; 2^10, 2 limbs:
+  // 512 -> 128 8 : 12, 4096 -> 64 20 : 45, 1024 -> 256 15 : 18, 4096 -> 1024 171 : 121; 2^12, 2 limbs: 300 -> 64 8 : 10,
+  // 1024 -> 128 25 : 22.
+  if (sh.tiles <= 1 || (sh.tiles == 2 && sh.blocks <= 1) || strips * sh.tiles <= t.num_cus * 4ull)
+    return launch_thin(t, a, strips * sh.tiles, s);
+  // A chunked job is 8 row tiles of one column tile or 4 of two; the others by a fit of their times.  2^14, 4 limbs, us, 4 x
+  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 512 -> 128 94 : 119 : 109, 512 -> 256 170 : 169 : 170, 512 -> 512 327 :
+  // 318 : 288, 1024 -> 256 306 : 308 : 320, 1024 -> 384 442 : 525 : 436, 1024 -> 512 581 : 572 : 535; 2^15 1024 -> 2048
+  // 4530 : 4290 : 3720.  One block of inputs gives a wave too little to do between the barriers: 128 -> 512 161 : 139 : 143.
+  const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
+  const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
+  const bool four = 2 * (strip_bytes(sh) + kJoinBytes<4>) <= kLdsBytes;
+  if (sh.blocks > 1 && strip_bytes(sh) <= kLdsBytes) {
+    const Plan plan = four ? plan_whole(t, sh, strips, 4, 80, 38) : plan_whole(t, sh, strips, 8, 82, 23);
+    if (plan.time < wide && plan.time < tall)
+      return four ? launch_whole<4>(t, a, strips, plan.splits, s) : launch_whole<8>(t, a, strips, plan.splits, s);
+  }
+  return wide < tall ? launch_chunked<8, 2>(t, a, strips, s) : launch_chunked<8, 1>(t, a, strips, s);
 }
 
 }  // namespace
@@ -670,18 +746,7 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
     experts_zero_kernel<<<dim3(64, count < 1024 ? count : 1024), kThreads, 0, s>>>(t, a, count);
     return hipGetLastError();
   }
-  if (a.sh.tiles > 1) {
-    // passes over the row tiles for two column tiles, in halves: one of 8 or two of 4 at a time
-    const bool two = 2 * strip_bytes(a.sh) <= kLdsBytes, whole = strip_bytes(a.sh) <= kLdsBytes;
-    const uint32_t eight = 2 * half_passes(a.sh, 8, whole), four = half_passes(a.sh, 4, two);
-    if (two && four < eight) return launch<8, 2, true>(t, a, count, s);
-    if (whole) return launch<8, 1, true>(t, a, count, s);
-    return four < eight ? launch<8, 2, false>(t, a, count, s) : launch<8, 1, false>(t, a, count, s);
-  }
-  const uint64_t grid = static_cast<uint64_t>(count) * limbs * (2 * t.n / kThinCols);
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  mac_fp8_thin_kernel<<<static_cast<uint32_t>(grid), kThreads, 0, s>>>(t, a);
-  return hipGetLastError();
+  return launch(t, a, count, s);
 }
 
 }  // namespace ckks
