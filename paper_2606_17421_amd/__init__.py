@@ -170,6 +170,7 @@ class Context:
         _check(_lib.ckks_ctx_create(ctypes.byref(h), log_n, limbs, arr, device), "ckks_ctx_create")
         self.handle = h
         self.log_n, self.n, self.limbs, self.device = log_n, 1 << log_n, limbs, device
+        self.fp8_bytes = {}     # of encoded 8-bit layers, by their sizes
         buf = (_u32 * limbs)()
         _check(_lib.ckks_ctx_moduli(h, buf), "ckks_ctx_moduli")
         self.moduli = tuple(int(x) for x in buf)
@@ -393,10 +394,13 @@ def ckks_linear_mac_q4(ctx: Context, w_q4, ct_in, ct_out, d_out: int, d_in: int,
 
 
 def ckks_fp8_weight_bytes(ctx: Context, d_out: int, d_in: int, limbs: int) -> int:
-    v = _lib.ckks_fp8_weight_bytes(ctx.handle, d_out, d_in, limbs)
-    if v == ctypes.c_size_t(-1).value:
-        raise ValueError("invalid 8-bit weight request")
-    return int(v)
+    v = ctx.fp8_bytes.get((d_out, d_in, limbs))     # asked by every call: a second call into the library is 1 us
+    if v is None:
+        v = _lib.ckks_fp8_weight_bytes(ctx.handle, d_out, d_in, limbs)
+        if v == ctypes.c_size_t(-1).value:
+            raise ValueError("invalid 8-bit weight request")
+        ctx.fp8_bytes[d_out, d_in, limbs] = v
+    return v
 
 
 def _words(t) -> int:
