@@ -159,11 +159,11 @@ __global__ __launch_bounds__(kThreads) void experts_status_kernel(Layers a, uint
 }
 
 // Request, limb, `cols` columns and share of the row tiles of a workgroup's job; false where the request names no
-// expert or no bundle.  Jobs are numbered by request, limb, column strip and row split, so that neighbours share
-// columns or weights.
+// expert or no bundle.  An XCD's jobs are numbered by request, limb, column strip and row split, so that neighbours
+// share columns or weights; the strips of a limb (`cols` at most 128 of 2^11 and more) are a multiple of the 8 XCDs.
 __device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, uint32_t id, Job* job) {
   const uint32_t n = tb.n, strips = 2 * n / cols, per = strips * a.limbs * splits;
-  const uint32_t r = id / per, in = id - r * per;
+  const uint32_t r = id / (per / 8), in = id - r * (per / 8) + (blockIdx.x & 7) * (per / 8);
   const uint32_t split = in % splits, lc = in / splits, l = lc / strips, col0 = (lc - l * strips) * cols;
   uint32_t e, b;
   const bool good = named(a, r, &e, &b);
@@ -179,17 +179,15 @@ __device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint
   return true;
 }
 
-// Consecutive workgroup ids alternate XCDs; the workgroups of one XCD take a contiguous range of `jobs`, next to each
-// other at any time: `first`, then every `stride`-th below `end`.
+// Consecutive workgroup ids alternate XCDs; each XCD has an eighth of every request's columns, so that requests that name
+// nothing leave no XCD idle (13 of 16 requests of 200 -> 333 at 2^11 and 2 limbs: 103 -> 86 us), and its workgroups take
+// jobs next to each other at any time: `first`, then every `stride`-th below `end`.
 struct Range {
   uint32_t first, stride, end;
 };
 __device__ __forceinline__ Range range_of(uint32_t jobs) {
-  const uint32_t G = gridDim.x, id = blockIdx.x;
-  if (G < 8) return {id, G, jobs};
-  const uint32_t xcd = id & 7, each = jobs / 8, rest = jobs % 8;  // the first `rest` XCDs take one more
-  const uint32_t begin = xcd * each + min(xcd, rest);
-  return {begin + (id >> 3), (G - xcd + 7) / 8, begin + each + (xcd < rest)};
+  const uint32_t xcd = blockIdx.x & 7;
+  return {blockIdx.x >> 3, (gridDim.x - xcd + 7) / 8, jobs / 8};
 }
 
 // 16 consecutive inputs of one column a lane: lane l has column l % 32 of those at `src`, and the first or the second
@@ -521,18 +519,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Laye
 }
 
 // Inputs whose digits all fit the LDS: a workgroup converts its columns once a job and its waves walk the row tiles of
-// the job's split, kWaves apart, with nothing to wait for but their weights.  During the last of them a chunk's
-// place in LDS is given to the next job's residues as soon as every wave is through with it, so that only
-// this pass has barriers and the matrix cores do not pause between jobs.
+// the job's split, kWaves apart, with nothing to wait for but their weights.  The next job's residues are converted
+// meanwhile: where the LDS has room for both (kTwice) a piece with each chunk, from the first on, and one barrier a
+// job; else during the last pass, when a chunk's place is given to them as soon as every wave is through with it.
 //
 // The row tiles that are no multiple of kWaves come first.  Where they are at most half of it (and others
 // follow), with kJoin, two waves take a tile's chunks half and half and their sums meet in LDS.
-template <int kWaves, bool kJoin>
+template <int kWaves, bool kJoin, bool kTwice>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
   constexpr int kPasses = kChunk / kWaves;
   static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
   constexpr uint32_t kChunkFrags = kChunk * kStepFrags;
-  extern __shared__ v4i whole[];  // [chunks][kChunkFrags], with kJoin [kWaves / 2][4][64]
+  extern __shared__ v4i lds[];  // [chunks][kChunkFrags], with kTwice twice, with kJoin [kWaves / 2][4][64]
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kWaves - 1) / kWaves;
   const uint32_t rest = each - (passes - 1) * kWaves;  // row tiles of the first pass
@@ -556,6 +554,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t begin0 = upper ? half : 0, end0 = upper ? chunks : half;
   auto at_of = [&](uint32_t pass) { return pass == 0 ? at0 : rest + (pass - 1) * kWaves + wave; };
   auto source = [&](const Job& j, uint32_t at) { return source_of(a, j, min(j.split * each + at, tiles - 1)); };
+  const uint32_t pieces = chunks * kPasses, strip = chunks * kChunkFrags;
+  v4i *const sums = lds + (kTwice ? 2 : 1) * strip, *whole = lds, *other = lds + strip;
   Stage<kWaves, 1> stage;
   Weights w[kChunkBlocks];
   for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks)
@@ -576,40 +576,64 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
     const Modulus q = modulus(tb.q[job.limb]);
     const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
     Job after = job;
+    if (kTwice) going = seek(&after);
+    const uint32_t wanted = kTwice && going ? pieces : 0;
+    uint32_t fetched = 0, placed = 0;  // pieces of the next job
+    auto place_piece = [&] {
+      stage.place(other + placed / kPasses * kChunkFrags, placed % kPasses);
+      ++placed;
+    };
+    auto fetch_piece = [&] {
+      stage.fetch(tb, a, after, fetched / kPasses * kChunk, fetched % kPasses);
+      ++fetched;
+    };
     for (uint32_t pass = 0; pass < passes; ++pass) {
       const uint32_t at = at_of(pass), tile = job.split * each + at;
       const bool last = pass + 1 == passes, works = (pass != 0 || at < rest) && tile < tiles;
       const uint32_t my_steps = works ? steps : 0, begin = pass == 0 ? begin0 : 0, end = pass == 0 ? end0 : chunks;
-      if (last) going = seek(&after);
+      if (!kTwice && last) going = seek(&after);
       int64_t acc[16];
       clear(acc);
       for (uint32_t c = begin; c < end; ++c) {
-        if (c + 1 == end) src = source(after, last ? at0 : at_of(pass + 1));
+        if (c + 1 == end) src = last ? source(after, at0) : source(job, at_of(pass + 1));
         const uint32_t g0 = c * kChunkBlocks, g1 = c + 1 < end ? g0 + kChunkBlocks : last ? begin0 * kChunkBlocks : 0;
         const uint32_t s0 = g0 * kBlockSteps, s1 = going ? s0 : steps;
         v4i* chunk = whole + c * kChunkFrags;
         const v4i* f = chunk + (threadIdx.x & 63);
         v4i x[4];
-        if (last) stage.fetch(tb, a, after, s1, 0);
+        if (!kTwice && last) stage.fetch(tb, a, after, s1, 0);
+        if (kTwice) {
+          if (placed < fetched) place_piece();
+          if (fetched < wanted) fetch_piece();
+        }
         if (c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
         read(f, x);
         contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
-        if (kPasses == 2 && last) {
+        if (!kTwice && kPasses == 2 && last) {
           __syncthreads();
           stage.place(chunk, 0);
           stage.fetch(tb, a, after, s1, 1);
         }
         f += kBlockSteps * kStepFrags;
         contract(f, max(my_steps, s0 + kBlockSteps) - (s0 + kBlockSteps), f, src, g1 + 1, blocks, w[1], x, acc);
-        if (last) {
+        if (!kTwice && last) {
           __syncthreads();
           stage.place(chunk, kPasses - 1);
         }
       }
       uint32_t y[16];
       reduce(acc, q, y);
-      if (joins && pass == 0) join(y, q.q, whole + chunks * kChunkFrags, wave, kWaves, 2);
+      if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
       if (works && !(upper && pass == 0)) store(job.dst, bytes, a.d_out, tile, y);
+    }
+    if (kTwice) {
+      while (placed < wanted) {
+        if (placed == fetched) fetch_piece();
+        place_piece();
+      }
+      v4i* const done = whole;
+      whole = other;
+      other = done;
     }
     __syncthreads();
     job = after;
@@ -656,11 +680,12 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
-  const size_t strip = strip_bytes(a.sh), both = strip + kJoinBytes<kWaves>;
-  if (both <= kLdsBytes)
-    mac_fp8_whole_kernel<kWaves, true><<<grid, kWaves * 64, both, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
-  else
-    mac_fp8_whole_kernel<kWaves, false><<<grid, kWaves * 64, strip, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  const size_t strip = strip_bytes(a.sh), join = kJoinBytes<kWaves>, room = kLdsBytes / (8 / kWaves);
+  const auto k = 2 * strip + join <= room ? mac_fp8_whole_kernel<kWaves, true, true>
+                 : strip + join <= room   ? mac_fp8_whole_kernel<kWaves, true, false>
+                                          : mac_fp8_whole_kernel<kWaves, false, false>;
+  const size_t bytes = 2 * strip + join <= room ? 2 * strip + join : strip + join <= room ? strip + join : strip;
+  k<<<grid, kWaves * 64, bytes, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
 }
 
