@@ -10,6 +10,20 @@
 // digits and twelve; what the rounding to 64ths costs is 2^-7 at most of a weight below 1/8, 2^-16 of the largest one.
 // T = a + 2^16 b + 2^32 c with a and b from two digit sums each and c from one; a block's scale enters
 // in 64-bit integers, and the sum over the blocks is reduced once an output.
+//
+// Four kernels share the arithmetic, chosen in launch():
+//   thin     few outputs or few columns: residues go from memory through registers to the matrix cores; bound by
+//            memory (1024 -> 16 at 2^13, 3 limbs: 42.6 us, 4.8 TB/s, what a large copy reaches).
+//   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57 ms, 1.05e15 int8 products/s).
+//   whole    up to 1280 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.63 ms,
+//            1.2e15 products/s; a large int8 matrix product of the library's makes 1.03e15).
+// What bounds the last two: power and issue.  The matrix pipe is busy 62% of the cycles of 1024 -> 2048 and the chip
+// holds 1.86 GHz (48% and 2.06 GHz chunked, and 10% less time with zero residues).  Beside the 32 matrix
+// operations of a block, 8 issue cycles each, stand 48 multiply-adds of 8.7 cycles and 71 other vector
+// operations of 4.5: measured alone, 20 matrix operations and 80 shift-adds overlap (309 and 192 ns alone, 320 together), with 80
+// multiply-adds they do not (313 and 311 alone, 411 together).  Measured without effect or worse: sums combined between
+// the same wave's matrix operations (3.65 -> 3.85 ms), wave priorities by phase or by half, a delayed half, four-wave
+// workgroups for the chunked kernel (4.2 -> 4.8 ms), stores or loads past the caches.
 #include <algorithm>
 
 #include "digits.hpp"
@@ -118,8 +132,9 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
 constexpr size_t kLdsBytes = 160 << 10;
 size_t strip_bytes(const Shape& s) { return static_cast<size_t>(s.steps + kChunk - 1) / kChunk * kChunk * kStepFrags * 16; }
 
+constexpr size_t kWaveSums = 16 * 64 * 4;  // of a wave's outputs that meet another's
 template <int kWaves>
-constexpr size_t kJoinBytes = kWaves / 2 * 256 * 16;
+constexpr size_t kJoinBytes = kWaves / 2 * kWaveSums;
 
 // A layer, or a layer for each expert, and what it is applied to.
 struct Layers {
@@ -189,6 +204,19 @@ __device__ __forceinline__ Range range_of(uint32_t jobs) {
   const uint32_t xcd = blockIdx.x & 7;
   return {blockIdx.x >> 3, (gridDim.x - xcd + 7) / 8, jobs / 8};
 }
+
+// A persistent workgroup's jobs in turn, those of requests that name nothing left out.
+struct Jobs {
+  Range range;
+  __device__ __forceinline__ bool next(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, Job* job) {
+    while (range.first < range.end) {
+      const uint32_t id = range.first;
+      range.first += range.stride;
+      if (place_of(tb, a, cols, splits, id, job)) return true;
+    }
+    return false;
+  }
+};
 
 // 16 consecutive inputs of one column a lane: lane l has column l % 32 of those at `src`, and the first or the second
 // half of the 32 inputs from `base` on.  Inputs past d_in read as zero through the buffer range check.
@@ -436,31 +464,21 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
 // jobs and their chunks of two blocks of inputs without a pause: the next chunk's residues, of this job or the
 // next, are in flight in registers while the matrix cores work on this one's out of the other half of the LDS.
-template <int kWaves, int kColWaves>
-__global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
+template <int kColWaves>
+__global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
+  constexpr int kWaves = 8, kPasses = kChunk * kColWaves / kWaves;  // a pass a chunk, or one a block
   constexpr uint32_t kCols = kColWaves * 32;
-  constexpr int kPasses = kChunk * kColWaves / kWaves;
-  static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
   static_assert(kFoldBlocks % kChunkBlocks == 0, "reductions between chunks");
   __shared__ v4i lds[2][kColWaves * kChunk * kStepFrags];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits;
-  const Range range = range_of(jobs);
-  uint32_t id = range.first;
-  // the next job from id on that names an expert and a bundle
-  auto seek = [&](Job* job) {
-    for (; id < range.end; id += range.stride)
-      if (place_of(tb, a, kCols, splits, id, job)) {
-        id += range.stride;
-        return true;
-      }
-    return false;
-  };
+  Jobs list{range_of(jobs)};
+  auto seek = [&](Job* job) { return list.next(tb, a, kCols, splits, job); };
   Job job;
   if (!seek(&job)) return;
   const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
-  // waves without a row tile in a job's last split contract the last tile again, which costs no time of the others;
-  // those without one in any have no steps
+  // waves without a row tile in a job's last split contract the last tile again, so that no weights are merged from two
+  // paths, which costs registers; those without one in any have no steps
   auto source = [&](const Job& j) { return source_of(a, j, min(j.split * each + row_wave, tiles - 1)); };
   const uint32_t my_steps = row_wave < each ? steps : 0;
   Stage<kWaves, kColWaves> stage;
@@ -534,16 +552,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kWaves - 1) / kWaves;
   const uint32_t rest = each - (passes - 1) * kWaves;  // row tiles of the first pass
-  const Range range = range_of(jobs);
-  uint32_t id = range.first;
-  auto seek = [&](Job* job) {
-    for (; id < range.end; id += range.stride)
-      if (place_of(tb, a, 32, splits, id, job)) {
-        id += range.stride;
-        return true;
-      }
-    return false;
-  };
+  Jobs list{range_of(jobs)};
+  auto seek = [&](Job* job) { return list.next(tb, a, 32, splits, job); };
   Job job;
   if (!seek(&job)) return;
   const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
@@ -656,8 +666,8 @@ __global__ __launch_bounds__(kThreads) void experts_zero_kernel(Tables tb, Layer
 uint32_t ceil_div(uint64_t a, uint32_t b) { return static_cast<uint32_t>((a + b - 1) / b); }
 
 hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStream_t s) {
-  uint32_t slices = 1;  // eight waves a CU where the blocks allow it
-  while (slices < kThinWaves && 2 * slices <= a.sh.blocks && waves * slices < t.num_cus * 8ull) slices *= 2;
+  uint32_t slices = 1;  // up to eight waves a CU, as many as run at a time (1024 -> 16 at 2^13, 3 limbs, twelve : six, 48.9 : 42.6 us)
+  while (slices < kThinWaves && 2 * slices <= a.sh.blocks && 2 * waves * slices <= t.num_cus * 8ull) slices *= 2;
   const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
   const uint64_t grid = waves * slices / group;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
@@ -665,12 +675,12 @@ hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStre
   return hipGetLastError();
 }
 
-template <int kWaves, int kColWaves>
+template <int kColWaves>
 hipError_t launch_chunked(const Tables& t, const Layers& a, uint64_t strips, hipStream_t s) {
-  const uint32_t splits = ceil_div(a.sh.tiles, kWaves / kColWaves);
+  const uint32_t splits = ceil_div(a.sh.tiles, 8 / kColWaves);
   const uint64_t jobs = strips / kColWaves * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  mac_fp8_kernel<kWaves, kColWaves><<<static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus)), kWaves * 64, 0, s>>>(
+  mac_fp8_chunked_kernel<kColWaves><<<static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus)), 512, 0, s>>>(
       t, a, splits, static_cast<uint32_t>(jobs));
   return hipGetLastError();
 }
@@ -680,12 +690,19 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
-  const size_t strip = strip_bytes(a.sh), join = kJoinBytes<kWaves>, room = kLdsBytes / (8 / kWaves);
-  const auto k = 2 * strip + join <= room ? mac_fp8_whole_kernel<kWaves, true, true>
-                 : strip + join <= room   ? mac_fp8_whole_kernel<kWaves, true, false>
-                                          : mac_fp8_whole_kernel<kWaves, false, false>;
-  const size_t bytes = 2 * strip + join <= room ? 2 * strip + join : strip + join <= room ? strip + join : strip;
-  k<<<grid, kWaves * 64, bytes, s>>>(t, a, splits, static_cast<uint32_t>(jobs));
+  const size_t strip = strip_bytes(a.sh), join = kJoinBytes<kWaves>;
+  const uint32_t n = static_cast<uint32_t>(jobs);
+  if constexpr (kWaves == 4) {  // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs: 91 -> 88 us)
+    if (2 * (2 * strip + join) <= kLdsBytes)
+      mac_fp8_whole_kernel<4, true, true><<<grid, 256, 2 * strip + join, s>>>(t, a, splits, n);
+    else
+      mac_fp8_whole_kernel<4, true, false><<<grid, 256, strip + join, s>>>(t, a, splits, n);
+  } else {
+    if (strip + join <= kLdsBytes)
+      mac_fp8_whole_kernel<8, true, false><<<grid, 512, strip + join, s>>>(t, a, splits, n);
+    else
+      mac_fp8_whole_kernel<8, false, false><<<grid, 512, strip, s>>>(t, a, splits, n);
+  }
   return hipGetLastError();
 }
 
@@ -696,10 +713,11 @@ struct Plan {
   uint32_t splits;
 };
 Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t waves, uint32_t pass, uint32_t fill) {
+  const bool shares = sh.steps > kChunk && strip_bytes(sh) + waves / 2 * kWaveSums <= kLdsBytes;  // a tile between two waves
   Plan best{~0ull, 1};
   for (uint32_t splits = 1; splits <= 8 && splits <= sh.tiles; ++splits) {
     const uint32_t each = ceil_div(sh.tiles, splits), full = each / waves, rest = each % waves;
-    const uint32_t halves = 2 * full + (rest == 0 ? 0 : full > 0 && rest <= waves / 2 && sh.steps > kChunk ? 1 : 2);
+    const uint32_t halves = 2 * full + (rest == 0 ? 0 : full > 0 && rest <= waves / 2 && shares ? 1 : 2);
     const uint64_t rounds = ceil_div(strips * splits, t.num_cus * (8 / waves));
     const uint64_t time = rounds * (pass * halves / 2 + fill);
     if (time < best.time) best = {time, splits};
@@ -711,24 +729,24 @@ hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t 
   const Shape& sh = a.sh;
   const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / 32);
   // No more than 32 outputs, two row tiles of one block of inputs, or too few columns for the other kernels.  Thin : the
-  // others, us, 2^14, 4 limbs: 16 -> 64 18 : 31, 128 -> 64 27 : 34, 256 -> 64 40 : 36, 64 -> 128 36 : 36; 2^10, 2 limbs:
-  // 512 -> 128 8 : 12, 4096 -> 64 20 : 45, 1024 -> 256 15 : 18, 4096 -> 1024 171 : 121; 2^12, 2 limbs: 300 -> 64 8 : 10,
-  // 1024 -> 128 25 : 22.
+  // best of the others, us, 2^14, 4 limbs: 16 -> 64 20 : 33, 128 -> 64 33 : 41, 256 -> 64 51 : 49, 64 -> 128 44 : 42; 2^10, 2
+  // limbs: 512 -> 128 8 : 12, 4096 -> 64 28 : 45, 1024 -> 256 15 : 18, 4096 -> 1024 171 : 121; 2^12, 2 limbs: 300 -> 64 8 :
+  // 10, 1024 -> 128 25 : 22.
   if (sh.tiles <= 1 || (sh.tiles == 2 && sh.blocks <= 1) || strips * sh.tiles <= t.num_cus * 4ull)
     return launch_thin(t, a, strips * sh.tiles, s);
   // A chunked job is 8 row tiles of one column tile or 4 of two; the others by a fit of their times.  2^14, 4 limbs, us, 4 x
-  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 512 -> 128 94 : 119 : 109, 512 -> 256 170 : 169 : 170, 512 -> 512 327 :
-  // 318 : 288, 1024 -> 256 306 : 308 : 320, 1024 -> 384 442 : 525 : 436, 1024 -> 512 581 : 572 : 535; 2^15 1024 -> 2048
-  // 4530 : 4290 : 3720.  One block of inputs gives a wave too little to do between the barriers: 128 -> 512 161 : 139 : 143.
+  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 256 -> 128 59 : 73 : 66, 128 -> 512 159 : 140 : 125, 512 -> 256 167 :
+  // 165 : 163, 512 -> 512 316 : 310 : 278, 1024 -> 256 296 : 296 : 306, 1024 -> 384 425 : 513 : 422, 1024 -> 512 555 : 552 : 516,
+  // 1280 -> 512 698 : 685 : 641; 2^15 1024 -> 2048 4530 : 4290 : 3640.
   const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
   const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
   const bool four = 2 * (strip_bytes(sh) + kJoinBytes<4>) <= kLdsBytes;
-  if (sh.blocks > 1 && strip_bytes(sh) <= kLdsBytes) {
+  if (strip_bytes(sh) <= kLdsBytes) {
     const Plan plan = four ? plan_whole(t, sh, strips, 4, 80, 38) : plan_whole(t, sh, strips, 8, 82, 23);
     if (plan.time < wide && plan.time < tall)
       return four ? launch_whole<4>(t, a, strips, plan.splits, s) : launch_whole<8>(t, a, strips, plan.splits, s);
   }
-  return wide < tall ? launch_chunked<8, 2>(t, a, strips, s) : launch_chunked<8, 1>(t, a, strips, s);
+  return wide < tall ? launch_chunked<2>(t, a, strips, s) : launch_chunked<1>(t, a, strips, s);
 }
 
 }  // namespace
