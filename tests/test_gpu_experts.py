@@ -59,10 +59,12 @@ def test_many_columns(gpu_lib, d_out, d_in):
 
 
 @gpu
-def test_requests_that_name_nothing(gpu_lib):
+@pytest.mark.parametrize("d_out,d_in", [(5, 5), (40, 70), (130, 1300), (290, 1500), (300, 200), (270, 400), (300, 900), (290, 1200)])
+def test_requests_that_name_nothing(gpu_lib, d_out, d_in):
+    """At the ends and between good ones, and in every kernel of the layer."""
     big, small = 2 ** 31 - 1, -(2 ** 31)
-    check(gpu_lib, 10, 2, 2, [-1, 0, 2, 1, big, small, 1, 0], [0, -1, 0, 1, 0, 0, 2, big], 2, 40, 70, 640)
-    check(gpu_lib, 10, 1, 1, [-1], [0], 1, 5, 5, 641)
+    check(gpu_lib, 11, 4, 2, [-1, 0, 2, 1, big, small, 1, 0], [0, -1, 0, 1, 0, 0, 2, big], 2, d_out, d_in, 640)
+    check(gpu_lib, 10, 1, 1, [-1], [0], 1, d_out, d_in, 641)
 
 
 @gpu

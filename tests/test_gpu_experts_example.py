@@ -1,0 +1,22 @@
+"""The encrypted mixture-of-experts example: encryption, the experts' products over
+8-bit weights, rescale, the gated sums, rescale and decryption, as a server runs them."""
+import importlib.util
+import os
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EXAMPLE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "encrypted_experts.py")
+
+
+def test_encrypted_experts_example(gpu_lib):
+    spec = importlib.util.spec_from_file_location("encrypted_experts", EXAMPLE)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    out = mod.main(seed=7)
+    assert out["requests"] == 7                      # four experts of the first bundle, three of the second
+    assert out["status"] == [0] * 7 + [1] * 3
+    # 2 * 40 * 512 slots within six standard deviations of the sum of all roundings and errors
+    assert out["worst_over_sd"] <= 6
+    assert out["largest"] > 1000 * out["worst_error"]

@@ -120,6 +120,23 @@ def test_many_outputs_of_many_columns(gpu_lib, d_in, d_out):
 
 
 @gpu
+@pytest.mark.parametrize("d_in", [40, 250, 300, 512, 600, 1000, 1024, 1100, 1280])
+@pytest.mark.parametrize("d_out", [290, 380, 420, 512, 530])
+def test_row_tiles_and_passes(gpu_lib, d_out, d_in):
+    """Whole passes over the row tiles, and rests of one to seven tiles that waves share or do not, with the
+    inputs of one and of several chunks in LDS."""
+    check_many(gpu_lib, d_out, d_in, 490 + d_in + d_out)
+
+
+@gpu
+@pytest.mark.parametrize("log_n,limbs", [(10, 1), (10, 3), (11, 2), (12, 2)])
+@pytest.mark.parametrize("d_out,d_in", [(9, 1500), (33, 700), (200, 130), (700, 300), (900, 900), (1100, 1100), (1500, 40)])
+def test_few_columns(gpu_lib, log_n, limbs, d_out, d_in):
+    """Inputs in shares that are summed, and rows split over workgroups."""
+    check(gpu_lib, log_n, limbs, d_out, d_in, 495 + d_in, rows=sorted({0, 7, 31 % d_out, d_out // 2, d_out - 2, d_out - 1}))
+
+
+@gpu
 @pytest.mark.parametrize("d_in", [1152, 2048, 2049, 2500, 4100, 9000])
 def test_deep_contractions(gpu_lib, d_in):
     check(gpu_lib, 10, 1, 70, d_in, 400 + d_in, rows=[0, 1, 16, 33, 69])
