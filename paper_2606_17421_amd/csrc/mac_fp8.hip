@@ -17,13 +17,14 @@
 //   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57 ms, 1.05e15 int8 products/s).
 //   whole    up to 1280 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.63 ms,
 //            1.2e15 products/s; a large int8 matrix product of the library's makes 1.03e15).
-// What bounds the last two: power and issue.  The matrix pipe is busy 62% of the cycles of 1024 -> 2048 and the chip
-// holds 1.86 GHz (48% and 2.06 GHz chunked, and 10% less time with zero residues).  Beside the 32 matrix
-// operations of a block, 8 issue cycles each, stand 48 multiply-adds of 8.7 cycles and 71 other vector
-// operations of 4.5: measured alone, 20 matrix operations and 80 shift-adds overlap (309 and 192 ns alone, 320 together), with 80
-// multiply-adds they do not (313 and 311 alone, 411 together).  Measured without effect or worse: sums combined between
-// the same wave's matrix operations (3.65 -> 3.85 ms), wave priorities by phase or by half, a delayed half, four-wave
-// workgroups for the chunked kernel (4.2 -> 4.8 ms), stores or loads past the caches.
+// What bounds the last two: issue and power.  A block of a row tile takes a SIMD 1680 cycles in 1024 -> 2048: its 32 matrix
+// operations keep the matrix pipe busy for 1024 of them (61%) and take 16 issue cycles each, beside 48 multiply-adds of 8.7
+// and 72 other vector operations of 4.5, 1250 of the 1680 (measured alone: 20 matrix operations and 80 shift-adds of
+// another wave take 309 and 192 ns, 320 together; with 80 multiply-adds 313 and 311, 411 together).  The chip holds 1.87 GHz
+// (2.06 GHz and 48% chunked; a loop of nothing but matrix operations on random numbers makes 1.75e15 products/s at
+// 1.7 GHz).  Without the weights' loads it takes 7% less, without the residues' 3%.  Measured without effect or worse:
+// sums combined between the same wave's matrix operations (3.65 -> 3.85 ms), wave priorities by phase or by half, a
+// delayed half, four-wave workgroups for the chunked kernel (4.2 -> 4.8 ms), stores or loads past the caches.
 #include <algorithm>
 
 #include "digits.hpp"
