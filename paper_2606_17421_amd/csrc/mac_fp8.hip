@@ -270,30 +270,65 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
-// A block's digit sums, times its scales, onto the 64-bit sums.
-__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const int32_t (&sc)[3], int64_t (&acc)[16]) {
+// A lane's outputs of a row tile.  The matrix operands are residues, then weights: lane l has row l % 32 and 16 of the 32
+// columns.  With no more than 8 rows they change places, so that a lane has one column and four rows, 4 (l / 32) and on, and
+// the steps below take a quarter of the operations (52 requests of 11 -> 1 at 2^16 and 3 limbs: @@F).
+constexpr int kFewRows = 8;
+template <bool kFew>
+constexpr int kOuts = kFew ? 4 : 16;
+
+template <bool kFew>
+__device__ __forceinline__ v16i product(v4i x, v4i w, v16i m) {
+  return kFew ? __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, m, 0, 0, 0) : __builtin_amdgcn_mfma_i32_32x32x32_i8(x, w, m, 0, 0, 0);
+}
+
+// A lane's three scale constants of a block, for each of its rows.
+template <bool kFew>
+struct Scales {
+  int32_t of[3][kFew ? 4 : 1];
+  __device__ __forceinline__ void load(const int32_t* block) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    acc[r] += static_cast<int64_t>(sc[0]) * (m[0][r] + (m[1][r] << 8));
-    acc[r] += static_cast<int64_t>(sc[1]) * (m[2][r] + (m[3][r] << 8));
-    acc[r] += static_cast<int64_t>(sc[2]) * m[4][r];
+    for (int i = 0; i < 3; ++i) {
+      if constexpr (kFew) {
+        const v4i v = *reinterpret_cast<const v4i*>(block + i * 32 + 4 * ((threadIdx.x >> 5) & 1));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) of[i][r] = v[r];
+      } else {
+        of[i][0] = block[i * 32 + (threadIdx.x & 31)];
+      }
+    }
+  }
+};
+
+// A block's digit sums, times its scales, onto the 64-bit sums.
+template <bool kFew>
+__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const Scales<kFew>& sc, int64_t (&acc)[kOuts<kFew>]) {
+#pragma unroll
+  for (int r = 0; r < kOuts<kFew>; ++r) {
+    const int k = kFew ? r : 0;
+    acc[r] += static_cast<int64_t>(sc.of[0][k]) * (m[0][r] + (m[1][r] << 8));
+    acc[r] += static_cast<int64_t>(sc.of[1][k]) * (m[2][r] + (m[3][r] << 8));
+    acc[r] += static_cast<int64_t>(sc.of[2][k]) * m[4][r];
   }
 }
 
-__device__ __forceinline__ void clear(int64_t (&acc)[16]) {
+template <int kN>
+__device__ __forceinline__ void clear(int64_t (&acc)[kN]) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0;
+  for (int r = 0; r < kN; ++r) acc[r] = 0;
 }
 
-__device__ __forceinline__ void reduce(const int64_t (&acc)[16], const Modulus& q, uint32_t (&y)[16]) {
+template <int kN>
+__device__ __forceinline__ void reduce(const int64_t (&acc)[kN], const Modulus& q, uint32_t (&y)[kN]) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) y[r] = reduce(acc[r], q);
+  for (int r = 0; r < kN; ++r) y[r] = reduce(acc[r], q);
 }
 
 // The sum so far, reduced, goes on as a product.
-__device__ __forceinline__ void fold(const Modulus& q, int32_t c32, int64_t (&acc)[16]) {
+template <int kN>
+__device__ __forceinline__ void fold(const Modulus& q, int32_t c32, int64_t (&acc)[kN]) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
+  for (int r = 0; r < kN; ++r) acc[r] = static_cast<int64_t>(static_cast<int32_t>(reduce(acc[r], q))) * c32;
 }
 
 // Where a wave finds a row tile's weights.
@@ -311,18 +346,17 @@ __device__ __forceinline__ Source source_of(const Layers& a, const Job& job, uin
 // used, so that two blocks' contractions cover the loads (and the residues' before them, since a wave's loads are
 // waited for in order); steps past the layer's last read as zero through the
 // buffer range check.
+template <bool kFew>
 struct Weights {
   v4i w[kBlockSteps][kDigits];
-  int32_t sc[3];
+  Scales<kFew> sc;
   __device__ __forceinline__ void load_step(const Source& src, uint32_t block, uint32_t s) {
     const uint32_t at = (block * kBlockSteps + s) * (kDigits * 1024) + (threadIdx.x & 63) * 16;
 #pragma unroll
     for (int d = 0; d < kDigits; ++d) w[s][d] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(src.frag, at + d * 1024, 0, 0);
   }
   __device__ __forceinline__ void load_scales(const Source& src, uint32_t block, uint32_t blocks) {
-    const int32_t* c = src.scales + static_cast<size_t>(min(block, blocks - 1)) * 96;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) sc[i] = c[i * 32 + (threadIdx.x & 31)];
+    sc.load(src.scales + static_cast<size_t>(min(block, blocks - 1)) * 96);
   }
 };
 
@@ -336,7 +370,7 @@ __device__ __forceinline__ void read(const v4i* f, v4i (&x)[4]) {
 // and onto the 64-bit sums.  A digit of the next step's residues is read as soon as this step's is used, those at
 // `f_next` during the last one; the weights of block `after` of `next` take the place of those used.
 __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i* f_next, const Source& next, uint32_t after,
-                                         uint32_t blocks, Weights& w, v4i (&x)[4], int64_t (&acc)[16]) {
+                                         uint32_t blocks, Weights<false>& w, v4i (&x)[4], int64_t (&acc)[16]) {
   v16i m[kPairs];
 #pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s) {
@@ -347,7 +381,7 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
 #pragma unroll
         for (int d = kDigits - 1; d >= 0; --d) {
           const bool first = s == 0 && (b == 0 || d == 1);  // of sum b + d
-          m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[b], w.w[s][d], first ? v16i{} : m[b + d], 0, 0, 0);
+          m[b + d] = product<false>(x[b], w.w[s][d], first ? v16i{} : m[b + d]);
         }
         x[b] = ahead[b * 64];
         __builtin_amdgcn_sched_barrier(0);
@@ -356,34 +390,42 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
     w.load_step(next, after, s);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (steps != 0) combine(m, w.sc, acc);
+  if (steps != 0) combine<false>(m, w.sc, acc);
   w.load_scales(next, after, blocks);
 }
 
 // A row tile's outputs; rows past d_out are out of range.
+template <bool kFew>
 __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile,
-                                      const uint32_t (&y)[16]) {
+                                      const uint32_t (&y)[kOuts<kFew>]) {
   const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
   const uint32_t rows = min(d_out - row0, 32u);
   const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(dst + static_cast<size_t>(row0) * (bytes >> 2), 0,
                                                        static_cast<int>(rows * bytes), kRsrcWord3);
+  if constexpr (kFew) {
 #pragma unroll
-  for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
-    v4i u;
+    for (int r = 0; r < 4; ++r)
+      __builtin_amdgcn_raw_buffer_store_b32(y[r], out, (4 * (lane >> 5) + r) * bytes + (lane & 31) * 4, 0, 0);
+  } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(y[4 * r4 + r]);
-    __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
+    for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
+      v4i u;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(y[4 * r4 + r]);
+      __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
+    }
   }
 }
 
-// Onto the sums of the waves of a workgroup's upper half those of its lower half's, through LDS [waves / 2][4][64], and so
-// on until the first of `slices` waves has the sum of all.
-__device__ __forceinline__ void join(uint32_t (&y)[16], uint32_t q, v4i* sums, uint32_t wave, uint32_t waves, uint32_t slices) {
+// Onto the sums of a workgroup's lower waves those of its upper half's, through LDS [waves / 2][outputs / 4][64], and so on
+// until the first waves / slices have the sums of all.
+template <int kN>
+__device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, uint32_t wave, uint32_t waves, uint32_t slices) {
   for (uint32_t half = waves / 2; slices > 1; half /= 2, slices /= 2) {
-    v4i* at = sums + (wave % half) * 256 + (threadIdx.x & 63);
+    v4i* at = sums + (wave % half) * (kN / 4 * 64) + (threadIdx.x & 63);
     if (wave >= half && wave < 2 * half) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
+      for (int r4 = 0; r4 < kN / 4; ++r4) {
         v4i v;
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] = static_cast<int>(y[4 * r4 + r]);
@@ -393,7 +435,7 @@ __device__ __forceinline__ void join(uint32_t (&y)[16], uint32_t q, v4i* sums, u
     __syncthreads();
     if (wave < half) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
+      for (int r4 = 0; r4 < kN / 4; ++r4) {
         const v4i v = at[r4 * 64];
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[4 * r4 + r] = add_mod(y[4 * r4 + r], static_cast<uint32_t>(v[r]), q);
@@ -407,8 +449,9 @@ __device__ __forceinline__ void join(uint32_t (&y)[16], uint32_t q, v4i* sums, u
 // registers to the matrix cores: a lane's digits of 16 inputs of one column are its operand, so there is no LDS and
 // nothing to wait for but the loads, of which those of four steps are in flight.
 constexpr int kThinWaves = 8;  // of a workgroup, at most
+template <bool kFew>
 __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
-  __shared__ v4i sums[kThinWaves / 2 * 256];
+  __shared__ v4i sums[kThinWaves / 2 * kOuts<kFew> * 16];
   Job job;
   const uint32_t waves = blockDim.x / 64, strips = waves / slices;
   if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
@@ -420,7 +463,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
   const Source src = source_of(a, job, job.split);
   job.src += strip * 32;
   uint32_t x[kBlockSteps][16];
-  Weights w;
+  Weights<kFew> w;
 #pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s)
     if (s == 0 || s < steps) {
@@ -428,7 +471,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
       w.load_step(src, begin, s);
     }
   w.load_scales(src, begin, blocks);
-  int64_t acc[16];
+  int64_t acc[kOuts<kFew>];
   clear(acc);
   for (uint32_t g = begin; g < end; ++g) {
     if (g != begin && (g - begin) % kFoldBlocks == 0) fold(q, c32, acc);
@@ -445,7 +488,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 #pragma unroll
           for (int d = kDigits - 1; d >= 0; --d) {
             const bool first = s == 0 && (b == 0 || d == 1);
-            m[b + d] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[b], w.w[s][d], first ? v16i{} : m[b + d], 0, 0, 0);
+            m[b + d] = product<kFew>(f[b], w.w[s][d], first ? v16i{} : m[b + d]);
           }
       }
       if (more) {
@@ -453,13 +496,64 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
         w.load_step(src, g + 1, s);
       }
     }
-    combine(m, w.sc, acc);
+    combine<kFew>(m, w.sc, acc);
     if (more) w.load_scales(src, g + 1, blocks);
   }
-  uint32_t y[16];
+  uint32_t y[kOuts<kFew>];
   reduce(acc, q, y);
   join(y, q.q, sums, wave, waves, slices);
-  if (slice == 0) store(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
+  if (slice == 0) store<kFew>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
+}
+
+// One block of inputs: a wave converts its 32 columns once, keeps their digits in registers and goes through the row tiles
+// of its split, the next tile's weights in flight.  No LDS, and nothing that waves wait for together.
+constexpr int kShortWaves = 4;  // of a workgroup, next to each other
+template <int kSteps, bool kFew>
+__global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
+  Job job;
+  if (!place_of(tb, a, kShortWaves * 32, splits, range_of(gridDim.x).first, &job)) return;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = a.sh.tiles;
+  const uint32_t each = (tiles + splits - 1) / splits, begin = job.split * each, end = min(tiles, begin + each);
+  if (begin >= end) return;
+  const Modulus q = modulus(tb.q[job.limb]);
+  job.src += wave * 32;
+  job.dst += wave * 32;
+  Weights<kFew> w;
+  auto load = [&](uint32_t tile) {
+    const Source src = source_of(a, job, tile);
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s) w.load_step(src, 0, s);
+    w.load_scales(src, 0, 1);
+  };
+  v4i f[kSteps][4];
+  {
+    uint32_t x[kSteps][16];
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s) fetch_step(tb, a, job.src, s * kStep, x[s]);
+    load(begin);
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s) to_fragments(x[s], f[s]);
+  }
+  for (uint32_t tile = begin; tile < end; ++tile) {
+    v16i m[kPairs];
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int d = kDigits - 1; d >= 0; --d) {
+          const bool first = s == 0 && (b == 0 || d == 1);
+          m[b + d] = product<kFew>(f[s][b], w.w[s][d], first ? v16i{} : m[b + d]);
+        }
+    const Scales<kFew> sc = w.sc;
+    load(min(tile + 1, end - 1));
+    int64_t acc[kOuts<kFew>];
+    clear(acc);
+    combine<kFew>(m, sc, acc);
+    uint32_t y[kOuts<kFew>];
+    reduce(acc, q, y);
+    store<kFew>(job.dst, row_bytes(tb, a), a.d_out, tile, y);
+  }
 }
 
 // A workgroup has kColWaves tiles of 32 columns and 8 / kColWaves row tiles, a wave one of each, and goes through
@@ -483,7 +577,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
   auto source = [&](const Job& j) { return source_of(a, j, min(j.split * each + row_wave, tiles - 1)); };
   const uint32_t my_steps = row_wave < each ? steps : 0;
   Stage<kWaves, kColWaves> stage;
-  Weights w[kChunkBlocks];
+  Weights<false> w[kChunkBlocks];
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     stage.fetch(tb, a, job, 0, p);
@@ -528,7 +622,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
       if (last && row_wave < each && tile < tiles) {
         uint32_t y[16];
         reduce(acc, q, y);
-        store(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
+        store<false>(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
       }
       stage.place(lds[buf ^ 1], kPasses - 1);
       __syncthreads();
@@ -568,7 +662,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t pieces = chunks * kPasses, strip = chunks * kChunkFrags;
   v4i *const sums = lds + (kTwice ? 2 : 1) * strip, *whole = lds, *other = lds + strip;
   Stage<kWaves, 1> stage;
-  Weights w[kChunkBlocks];
+  Weights<false> w[kChunkBlocks];
   for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks)
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
@@ -635,7 +729,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       uint32_t y[16];
       reduce(acc, q, y);
       if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
-      if (works && !(upper && pass == 0)) store(job.dst, bytes, a.d_out, tile, y);
+      if (works && !(upper && pass == 0)) store<false>(job.dst, bytes, a.d_out, tile, y);
     }
     if (kTwice) {
       while (placed < wanted) {
@@ -672,7 +766,23 @@ hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStre
   const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
   const uint64_t grid = waves * slices / group;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  mac_fp8_thin_kernel<<<static_cast<uint32_t>(grid), group * 64, 0, s>>>(t, a, slices);
+  const auto k = a.d_out <= kFewRows ? mac_fp8_thin_kernel<true> : mac_fp8_thin_kernel<false>;
+  k<<<static_cast<uint32_t>(grid), group * 64, 0, s>>>(t, a, slices);
+  return hipGetLastError();
+}
+
+hipError_t launch_short(const Tables& t, const Layers& a, uint64_t strips, hipStream_t s) {
+  // eight waves a CU where the row tiles allow it
+  const uint32_t splits = static_cast<uint32_t>(std::min<uint64_t>(a.sh.tiles, (t.num_cus * 8ull + strips - 1) / strips));
+  const uint64_t grid = strips / kShortWaves * splits;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
+  const auto k = a.d_out <= kFewRows ? (a.sh.steps == 1   ? mac_fp8_short_kernel<1, true>
+                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, true>
+                                                          : mac_fp8_short_kernel<4, true>)
+                                     : (a.sh.steps == 1   ? mac_fp8_short_kernel<1, false>
+                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, false>
+                                                          : mac_fp8_short_kernel<4, false>);
+  k<<<static_cast<uint32_t>(grid), kShortWaves * 64, 0, s>>>(t, a, splits);
   return hipGetLastError();
 }
 
@@ -733,6 +843,7 @@ hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t 
   // best of the others, us, 2^14, 4 limbs: 16 -> 64 20 : 33, 128 -> 64 33 : 41, 256 -> 64 51 : 49, 64 -> 128 44 : 42; 2^10, 2
   // limbs: 512 -> 128 8 : 12, 4096 -> 64 28 : 45, 1024 -> 256 15 : 18, 4096 -> 1024 171 : 121; 2^12, 2 limbs: 300 -> 64 8 :
   // 10, 1024 -> 128 25 : 22.
+  if (sh.blocks == 1) return launch_short(t, a, strips, s);
   if (sh.tiles <= 1 || (sh.tiles == 2 && sh.blocks <= 1) || strips * sh.tiles <= t.num_cus * 4ull)
     return launch_thin(t, a, strips * sh.tiles, s);
   // A chunked job is 8 row tiles of one column tile or 4 of two; the others by a fit of their times.  2^14, 4 limbs, us, 4 x
