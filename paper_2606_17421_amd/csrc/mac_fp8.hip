@@ -40,6 +40,7 @@ constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 6
 constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
 constexpr int kDigits = 2;            // of a weight
 constexpr uint32_t kChunkBlocks = 2, kChunk = kChunkBlocks * kBlockSteps;  // blocks and steps that go into LDS at a time
+constexpr int kNonTemporal = 2;        // cache policy of a buffer instruction
 constexpr int kStepFrags = 4 * 64;    // 16-byte residue fragments of a step: four digits, 64 lanes
 
 // Encoded weights (written once a layer):
@@ -270,42 +271,50 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
-// A lane's outputs of a row tile.  The matrix operands are residues, then weights: lane l has row l % 32 and 16 of the 32
-// columns.  With no more than 8 rows they change places, so that a lane has one column and four rows, 4 (l / 32) and on, and
-// the steps below take a quarter of the operations (52 requests of 11 -> 1 at 2^16 and 3 limbs: @@F).
-constexpr int kFewRows = 8;
-template <bool kFew>
-constexpr int kOuts = kFew ? 4 : 16;
+// Which of its row tile's outputs a lane has.
+//   kRows     residues times weights: row l % 32, and of the 32 columns 4 (l / 32) + 8 i + 0 .. 3.
+//   kColumns  weights times residues: column l % 32, rows 4 (l / 32) + 8 i + 0 .. 3.  Stores fill whole lines and can pass
+//             the caches by, but scales are 16 times as many registers.
+//   kFew      kColumns for at most 8 rows: the rows of i = 0 alone, a quarter of the steps that close a block and an
+//             output (52 requests of 11 -> 1 at 2^16 and 3 limbs: 479 -> 388 us).
+enum Form { kRows, kColumns, kFew };
+constexpr uint32_t kFewRows = 8;
+template <Form kForm>
+constexpr int kOuts = kForm == kFew ? 4 : 16;
 
-template <bool kFew>
+template <Form kForm>
 __device__ __forceinline__ v16i product(v4i x, v4i w, v16i m) {
-  return kFew ? __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, m, 0, 0, 0) : __builtin_amdgcn_mfma_i32_32x32x32_i8(x, w, m, 0, 0, 0);
+  return kForm == kRows ? __builtin_amdgcn_mfma_i32_32x32x32_i8(x, w, m, 0, 0, 0)
+                        : __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, m, 0, 0, 0);
 }
 
 // A lane's three scale constants of a block, for each of its rows.
-template <bool kFew>
+template <Form kForm>
 struct Scales {
-  int32_t of[3][kFew ? 4 : 1];
+  int32_t of[3][kForm == kRows ? 1 : kOuts<kForm>];
   __device__ __forceinline__ void load(const int32_t* block) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      if constexpr (kFew) {
-        const v4i v = *reinterpret_cast<const v4i*>(block + i * 32 + 4 * ((threadIdx.x >> 5) & 1));
-#pragma unroll
-        for (int r = 0; r < 4; ++r) of[i][r] = v[r];
-      } else {
+      if constexpr (kForm == kRows) {
         of[i][0] = block[i * 32 + (threadIdx.x & 31)];
+      } else {
+#pragma unroll
+        for (int r4 = 0; r4 < kOuts<kForm> / 4; ++r4) {
+          const v4i v = *reinterpret_cast<const v4i*>(block + i * 32 + 8 * r4 + 4 * ((threadIdx.x >> 5) & 1));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) of[i][4 * r4 + r] = v[r];
+        }
       }
     }
   }
 };
 
 // A block's digit sums, times its scales, onto the 64-bit sums.
-template <bool kFew>
-__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const Scales<kFew>& sc, int64_t (&acc)[kOuts<kFew>]) {
+template <Form kForm>
+__device__ __forceinline__ void combine(const v16i (&m)[kPairs], const Scales<kForm>& sc, int64_t (&acc)[kOuts<kForm>]) {
 #pragma unroll
-  for (int r = 0; r < kOuts<kFew>; ++r) {
-    const int k = kFew ? r : 0;
+  for (int r = 0; r < kOuts<kForm>; ++r) {
+    const int k = kForm == kRows ? 0 : r;
     acc[r] += static_cast<int64_t>(sc.of[0][k]) * (m[0][r] + (m[1][r] << 8));
     acc[r] += static_cast<int64_t>(sc.of[1][k]) * (m[2][r] + (m[3][r] << 8));
     acc[r] += static_cast<int64_t>(sc.of[2][k]) * m[4][r];
@@ -346,10 +355,10 @@ __device__ __forceinline__ Source source_of(const Layers& a, const Job& job, uin
 // used, so that two blocks' contractions cover the loads (and the residues' before them, since a wave's loads are
 // waited for in order); steps past the layer's last read as zero through the
 // buffer range check.
-template <bool kFew>
+template <Form kForm>
 struct Weights {
   v4i w[kBlockSteps][kDigits];
-  Scales<kFew> sc;
+  Scales<kForm> sc;
   __device__ __forceinline__ void load_step(const Source& src, uint32_t block, uint32_t s) {
     const uint32_t at = (block * kBlockSteps + s) * (kDigits * 1024) + (threadIdx.x & 63) * 16;
 #pragma unroll
@@ -370,7 +379,7 @@ __device__ __forceinline__ void read(const v4i* f, v4i (&x)[4]) {
 // and onto the 64-bit sums.  A digit of the next step's residues is read as soon as this step's is used, those at
 // `f_next` during the last one; the weights of block `after` of `next` take the place of those used.
 __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i* f_next, const Source& next, uint32_t after,
-                                         uint32_t blocks, Weights<false>& w, v4i (&x)[4], int64_t (&acc)[16]) {
+                                         uint32_t blocks, Weights<kRows>& w, v4i (&x)[4], int64_t (&acc)[16]) {
   v16i m[kPairs];
 #pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s) {
@@ -381,7 +390,7 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
 #pragma unroll
         for (int d = kDigits - 1; d >= 0; --d) {
           const bool first = s == 0 && (b == 0 || d == 1);  // of sum b + d
-          m[b + d] = product<false>(x[b], w.w[s][d], first ? v16i{} : m[b + d]);
+          m[b + d] = product<kRows>(x[b], w.w[s][d], first ? v16i{} : m[b + d]);
         }
         x[b] = ahead[b * 64];
         __builtin_amdgcn_sched_barrier(0);
@@ -390,22 +399,23 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
     w.load_step(next, after, s);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (steps != 0) combine<false>(m, w.sc, acc);
+  if (steps != 0) combine<kRows>(m, w.sc, acc);
   w.load_scales(next, after, blocks);
 }
 
 // A row tile's outputs; rows past d_out are out of range.
-template <bool kFew>
+template <Form kForm>
 __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile,
-                                      const uint32_t (&y)[kOuts<kFew>]) {
+                                      const uint32_t (&y)[kOuts<kForm>]) {
   const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
   const uint32_t rows = min(d_out - row0, 32u);
   const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(dst + static_cast<size_t>(row0) * (bytes >> 2), 0,
                                                        static_cast<int>(rows * bytes), kRsrcWord3);
-  if constexpr (kFew) {
+  if constexpr (kForm != kRows) {  // past the caches: 16 -> 512 at 2^14 and 4 limbs 66 -> 57 us; partial lines so, 269
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      __builtin_amdgcn_raw_buffer_store_b32(y[r], out, (4 * (lane >> 5) + r) * bytes + (lane & 31) * 4, 0, 0);
+    for (int r = 0; r < kOuts<kForm>; ++r)
+      __builtin_amdgcn_raw_buffer_store_b32(y[r], out, (8 * (r / 4) + 4 * (lane >> 5) + r % 4) * bytes + (lane & 31) * 4, 0,
+                                            kNonTemporal);
   } else {
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
@@ -449,9 +459,9 @@ __device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, u
 // registers to the matrix cores: a lane's digits of 16 inputs of one column are its operand, so there is no LDS and
 // nothing to wait for but the loads, of which those of four steps are in flight.
 constexpr int kThinWaves = 8;  // of a workgroup, at most
-template <bool kFew>
+template <Form kForm>
 __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
-  __shared__ v4i sums[kThinWaves / 2 * kOuts<kFew> * 16];
+  __shared__ v4i sums[kThinWaves / 2 * kOuts<kForm> * 16];
   Job job;
   const uint32_t waves = blockDim.x / 64, strips = waves / slices;
   if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
@@ -463,7 +473,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
   const Source src = source_of(a, job, job.split);
   job.src += strip * 32;
   uint32_t x[kBlockSteps][16];
-  Weights<kFew> w;
+  Weights<kForm> w;
 #pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s)
     if (s == 0 || s < steps) {
@@ -471,7 +481,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
       w.load_step(src, begin, s);
     }
   w.load_scales(src, begin, blocks);
-  int64_t acc[kOuts<kFew>];
+  int64_t acc[kOuts<kForm>];
   clear(acc);
   for (uint32_t g = begin; g < end; ++g) {
     if (g != begin && (g - begin) % kFoldBlocks == 0) fold(q, c32, acc);
@@ -488,7 +498,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 #pragma unroll
           for (int d = kDigits - 1; d >= 0; --d) {
             const bool first = s == 0 && (b == 0 || d == 1);
-            m[b + d] = product<kFew>(f[b], w.w[s][d], first ? v16i{} : m[b + d]);
+            m[b + d] = product<kForm>(f[b], w.w[s][d], first ? v16i{} : m[b + d]);
           }
       }
       if (more) {
@@ -496,19 +506,19 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
         w.load_step(src, g + 1, s);
       }
     }
-    combine<kFew>(m, w.sc, acc);
+    combine<kForm>(m, w.sc, acc);
     if (more) w.load_scales(src, g + 1, blocks);
   }
-  uint32_t y[kOuts<kFew>];
+  uint32_t y[kOuts<kForm>];
   reduce(acc, q, y);
   join(y, q.q, sums, wave, waves, slices);
-  if (slice == 0) store<kFew>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
+  if (slice == 0) store<kForm>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
 }
 
 // One block of inputs: a wave converts its 32 columns once, keeps their digits in registers and goes through the row tiles
-// of its split, the next tile's weights in flight.  No LDS, and nothing that waves wait for together.
+// of its split, the next tile's weights in flight (its scales would be 48 registers more).  No LDS, and nothing that waves wait for together.
 constexpr int kShortWaves = 4;  // of a workgroup, next to each other
-template <int kSteps, bool kFew>
+template <int kSteps, Form kForm>
 __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
   Job job;
   if (!place_of(tb, a, kShortWaves * 32, splits, range_of(gridDim.x).first, &job)) return;
@@ -518,12 +528,11 @@ __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tabl
   const Modulus q = modulus(tb.q[job.limb]);
   job.src += wave * 32;
   job.dst += wave * 32;
-  Weights<kFew> w;
+  Weights<kForm> w;
   auto load = [&](uint32_t tile) {
     const Source src = source_of(a, job, tile);
 #pragma unroll
     for (uint32_t s = 0; s < kSteps; ++s) w.load_step(src, 0, s);
-    w.load_scales(src, 0, 1);
   };
   v4i f[kSteps][4];
   {
@@ -535,6 +544,7 @@ __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tabl
     for (uint32_t s = 0; s < kSteps; ++s) to_fragments(x[s], f[s]);
   }
   for (uint32_t tile = begin; tile < end; ++tile) {
+    w.load_scales(source_of(a, job, tile), 0, 1);
     v16i m[kPairs];
 #pragma unroll
     for (uint32_t s = 0; s < kSteps; ++s)
@@ -543,16 +553,15 @@ __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tabl
 #pragma unroll
         for (int d = kDigits - 1; d >= 0; --d) {
           const bool first = s == 0 && (b == 0 || d == 1);
-          m[b + d] = product<kFew>(f[s][b], w.w[s][d], first ? v16i{} : m[b + d]);
+          m[b + d] = product<kForm>(f[s][b], w.w[s][d], first ? v16i{} : m[b + d]);
         }
-    const Scales<kFew> sc = w.sc;
     load(min(tile + 1, end - 1));
-    int64_t acc[kOuts<kFew>];
+    int64_t acc[kOuts<kForm>];
     clear(acc);
-    combine<kFew>(m, sc, acc);
-    uint32_t y[kOuts<kFew>];
+    combine<kForm>(m, w.sc, acc);
+    uint32_t y[kOuts<kForm>];
     reduce(acc, q, y);
-    store<kFew>(job.dst, row_bytes(tb, a), a.d_out, tile, y);
+    store<kForm>(job.dst, row_bytes(tb, a), a.d_out, tile, y);
   }
 }
 
@@ -577,7 +586,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
   auto source = [&](const Job& j) { return source_of(a, j, min(j.split * each + row_wave, tiles - 1)); };
   const uint32_t my_steps = row_wave < each ? steps : 0;
   Stage<kWaves, kColWaves> stage;
-  Weights<false> w[kChunkBlocks];
+  Weights<kRows> w[kChunkBlocks];
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     stage.fetch(tb, a, job, 0, p);
@@ -622,7 +631,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
       if (last && row_wave < each && tile < tiles) {
         uint32_t y[16];
         reduce(acc, q, y);
-        store<false>(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
+        store<kRows>(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
       }
       stage.place(lds[buf ^ 1], kPasses - 1);
       __syncthreads();
@@ -662,7 +671,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t pieces = chunks * kPasses, strip = chunks * kChunkFrags;
   v4i *const sums = lds + (kTwice ? 2 : 1) * strip, *whole = lds, *other = lds + strip;
   Stage<kWaves, 1> stage;
-  Weights<false> w[kChunkBlocks];
+  Weights<kRows> w[kChunkBlocks];
   for (uint32_t g0 = 0; g0 < blocks; g0 += kChunkBlocks)
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
@@ -729,7 +738,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       uint32_t y[16];
       reduce(acc, q, y);
       if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
-      if (works && !(upper && pass == 0)) store<false>(job.dst, bytes, a.d_out, tile, y);
+      if (works && !(upper && pass == 0)) store<kRows>(job.dst, bytes, a.d_out, tile, y);
     }
     if (kTwice) {
       while (placed < wanted) {
@@ -766,7 +775,7 @@ hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStre
   const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
   const uint64_t grid = waves * slices / group;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  const auto k = a.d_out <= kFewRows ? mac_fp8_thin_kernel<true> : mac_fp8_thin_kernel<false>;
+  const auto k = a.d_out <= kFewRows ? mac_fp8_thin_kernel<kFew> : mac_fp8_thin_kernel<kRows>;
   k<<<static_cast<uint32_t>(grid), group * 64, 0, s>>>(t, a, slices);
   return hipGetLastError();
 }
@@ -776,12 +785,12 @@ hipError_t launch_short(const Tables& t, const Layers& a, uint64_t strips, hipSt
   const uint32_t splits = static_cast<uint32_t>(std::min<uint64_t>(a.sh.tiles, (t.num_cus * 8ull + strips - 1) / strips));
   const uint64_t grid = strips / kShortWaves * splits;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  const auto k = a.d_out <= kFewRows ? (a.sh.steps == 1   ? mac_fp8_short_kernel<1, true>
-                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, true>
-                                                          : mac_fp8_short_kernel<4, true>)
-                                     : (a.sh.steps == 1   ? mac_fp8_short_kernel<1, false>
-                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, false>
-                                                          : mac_fp8_short_kernel<4, false>);
+  const auto k = a.d_out <= kFewRows ? (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kFew>
+                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kFew>
+                                                          : mac_fp8_short_kernel<4, kFew>)
+                                     : (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kColumns>
+                                        : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kColumns>
+                                                          : mac_fp8_short_kernel<4, kColumns>);
   k<<<static_cast<uint32_t>(grid), kShortWaves * 64, 0, s>>>(t, a, splits);
   return hipGetLastError();
 }
