@@ -134,9 +134,7 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
 constexpr size_t kLdsBytes = 160 << 10;
 size_t strip_bytes(const Shape& s) { return static_cast<size_t>(s.steps + kChunk - 1) / kChunk * kChunk * kStepFrags * 16; }
 
-constexpr size_t kWaveSums = 16 * 64 * 4;  // of a wave's outputs that meet another's
-template <int kWaves>
-constexpr size_t kJoinBytes = kWaves / 2 * kWaveSums;
+constexpr size_t kWaveSums = 16 * 64 * 4;  // a wave's outputs of a row tile, on their way to another wave or to memory
 
 // A layer, or a layer for each expert, and what it is applied to.
 struct Layers {
@@ -403,11 +401,20 @@ __device__ __forceinline__ void contract(const v4i* f, uint32_t steps, const v4i
   w.load_scales(next, after, blocks);
 }
 
-// A row tile's outputs; rows past d_out are out of range.
+// LDS accesses of a wave's lanes before it come before those after it: the hardware keeps a wave's order, the compiler
+// would not.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A row tile's outputs; rows past d_out are out of range.  With kRows through the wave's 4 KiB of LDS at `turn`.
 template <Form kForm>
 __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_out, uint32_t tile,
-                                      const uint32_t (&y)[kOuts<kForm>]) {
-  const uint32_t lane = threadIdx.x & 63, row0 = tile * 32;
+                                      const uint32_t (&y)[kOuts<kForm>], v4i* turn = nullptr) {
+  uint32_t lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // else the addresses below are kept in registers, and others are spilled
+  const uint32_t row0 = tile * 32;
   const uint32_t rows = min(d_out - row0, 32u);
   const rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(dst + static_cast<size_t>(row0) * (bytes >> 2), 0,
                                                        static_cast<int>(rows * bytes), kRsrcWord3);
@@ -416,14 +423,19 @@ __device__ __forceinline__ void store(uint32_t* dst, uint32_t bytes, uint32_t d_
     for (int r = 0; r < kOuts<kForm>; ++r)
       __builtin_amdgcn_raw_buffer_store_b32(y[r], out, (8 * (r / 4) + 4 * (lane >> 5) + r % 4) * bytes + (lane & 31) * 4, 0,
                                             kNonTemporal);
-  } else {
+  } else {  // lanes exchange rows and columns through LDS: 16-byte piece k of row r is at k ^ (r % 8), free of bank conflicts
+    const uint32_t row = lane & 31, h = lane >> 5;
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {  // four adjacent columns
-      v4i u;
+    for (uint32_t r4 = 0; r4 < 4; ++r4)
+      turn[row * 8 + ((2 * r4 + h) ^ (row & 7))] = v4i{static_cast<int>(y[4 * r4]), static_cast<int>(y[4 * r4 + 1]),
+                                                       static_cast<int>(y[4 * r4 + 2]), static_cast<int>(y[4 * r4 + 3])};
+    wave_fence();
 #pragma unroll
-      for (int r = 0; r < 4; ++r) u[r] = static_cast<int>(y[4 * r4 + r]);
-      __builtin_amdgcn_raw_buffer_store_b128(u, out, (lane & 31) * bytes + (8 * r4 + 4 * (lane >> 5)) * 4, 0, 0);
+    for (uint32_t i = 0; i < 4; ++i) {
+      const uint32_t r = 8 * i + (lane >> 3), k = lane & 7;
+      __builtin_amdgcn_raw_buffer_store_b128(turn[r * 8 + (k ^ (r & 7))], out, r * bytes + k * 16, 0, kNonTemporal);
     }
+    wave_fence();
   }
 }
 
@@ -461,7 +473,7 @@ __device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, u
 constexpr int kThinWaves = 8;  // of a workgroup, at most
 template <Form kForm>
 __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
-  __shared__ v4i sums[kThinWaves / 2 * kOuts<kForm> * 16];
+  __shared__ v4i sums[kThinWaves * kOuts<kForm> * 16];
   Job job;
   const uint32_t waves = blockDim.x / 64, strips = waves / slices;
   if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
@@ -512,7 +524,8 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
   uint32_t y[kOuts<kForm>];
   reduce(acc, q, y);
   join(y, q.q, sums, wave, waves, slices);
-  if (slice == 0) store<kForm>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y);
+  if (slices > 1) __syncthreads();  // the sums' place is written again
+  if (slice == 0) store<kForm>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y, sums + wave * (kOuts<kForm> * 16));
 }
 
 // One block of inputs: a wave converts its 32 columns once, keeps their digits in registers and goes through the row tiles
@@ -574,6 +587,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
   constexpr uint32_t kCols = kColWaves * 32;
   static_assert(kFoldBlocks % kChunkBlocks == 0, "reductions between chunks");
   __shared__ v4i lds[2][kColWaves * kChunk * kStepFrags];
+  __shared__ v4i turn[kWaves * 256];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col_wave = wave % kColWaves, row_wave = wave / kColWaves;
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits;
   Jobs list{range_of(jobs)};
@@ -631,7 +645,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
       if (last && row_wave < each && tile < tiles) {
         uint32_t y[16];
         reduce(acc, q, y);
-        store<kRows>(job.dst + col_wave * 32, bytes, a.d_out, tile, y);
+        store<kRows>(job.dst + col_wave * 32, bytes, a.d_out, tile, y, turn + wave * 256);
       }
       stage.place(lds[buf ^ 1], kPasses - 1);
       __syncthreads();
@@ -646,13 +660,13 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
 // job; else during the last pass, when a chunk's place is given to them as soon as every wave is through with it.
 //
 // The row tiles that are no multiple of kWaves come first.  Where they are at most half of it (and others
-// follow), with kJoin, two waves take a tile's chunks half and half and their sums meet in LDS.
-template <int kWaves, bool kJoin, bool kTwice>
+// follow) two waves take a tile's chunks half and half and their sums meet in LDS.
+template <int kWaves, bool kTwice>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
   constexpr int kPasses = kChunk / kWaves;
   static_assert(kPasses == 1 || kPasses == 2, "a pass a chunk, or one a block");
   constexpr uint32_t kChunkFrags = kChunk * kStepFrags;
-  extern __shared__ v4i lds[];  // [chunks][kChunkFrags], with kTwice twice, with kJoin [kWaves / 2][4][64]
+  extern __shared__ v4i lds[];  // [chunks][kChunkFrags], with kTwice twice, then [kWaves][256]
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = a.sh.tiles, each = (tiles + splits - 1) / splits, passes = (each + kWaves - 1) / kWaves;
   const uint32_t rest = each - (passes - 1) * kWaves;  // row tiles of the first pass
@@ -663,7 +677,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   const uint32_t steps = a.sh.steps, blocks = a.sh.blocks, bytes = row_bytes(tb, a);
   const uint32_t chunks = (blocks + kChunkBlocks - 1) / kChunkBlocks;
   // the wave's row tile of a pass, counted in the split, and its chunks
-  const bool joins = kJoin && passes > 1 && rest <= kWaves / 2 && chunks > 1, upper = joins && wave >= kWaves / 2;
+  const bool joins = passes > 1 && rest <= kWaves / 2 && chunks > 1, upper = joins && wave >= kWaves / 2;
   const uint32_t at0 = upper ? wave - kWaves / 2 : wave, half = joins ? (chunks + 1) / 2 : chunks;
   const uint32_t begin0 = upper ? half : 0, end0 = upper ? chunks : half;
   auto at_of = [&](uint32_t pass) { return pass == 0 ? at0 : rest + (pass - 1) * kWaves + wave; };
@@ -737,8 +751,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       }
       uint32_t y[16];
       reduce(acc, q, y);
-      if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
-      if (works && !(upper && pass == 0)) store<kRows>(job.dst, bytes, a.d_out, tile, y);
+      if (joins && pass == 0) {
+        join(y, q.q, sums, wave, kWaves, 2);
+        __syncthreads();  // the sums' place is written again
+      }
+      if (works && !(upper && pass == 0)) store<kRows>(job.dst, bytes, a.d_out, tile, y, sums + wave * 256);
     }
     if (kTwice) {
       while (placed < wanted) {
@@ -810,18 +827,15 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint64_t jobs = strips * splits;
   if (jobs > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
-  const size_t strip = strip_bytes(a.sh), join = kJoinBytes<kWaves>;
+  const size_t strip = strip_bytes(a.sh), sums = kWaves * kWaveSums;
   const uint32_t n = static_cast<uint32_t>(jobs);
   if constexpr (kWaves == 4) {  // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs: 91 -> 88 us)
-    if (2 * (2 * strip + join) <= kLdsBytes)
-      mac_fp8_whole_kernel<4, true, true><<<grid, 256, 2 * strip + join, s>>>(t, a, splits, n);
+    if (2 * (2 * strip + sums) <= kLdsBytes)
+      mac_fp8_whole_kernel<4, true><<<grid, 256, 2 * strip + sums, s>>>(t, a, splits, n);
     else
-      mac_fp8_whole_kernel<4, true, false><<<grid, 256, strip + join, s>>>(t, a, splits, n);
+      mac_fp8_whole_kernel<4, false><<<grid, 256, strip + sums, s>>>(t, a, splits, n);
   } else {
-    if (strip + join <= kLdsBytes)
-      mac_fp8_whole_kernel<8, true, false><<<grid, 512, strip + join, s>>>(t, a, splits, n);
-    else
-      mac_fp8_whole_kernel<8, false, false><<<grid, 512, strip, s>>>(t, a, splits, n);
+    mac_fp8_whole_kernel<8, false><<<grid, 512, strip + sums, s>>>(t, a, splits, n);
   }
   return hipGetLastError();
 }
@@ -833,11 +847,10 @@ struct Plan {
   uint32_t splits;
 };
 Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t waves, uint32_t pass, uint32_t fill) {
-  const bool shares = sh.steps > kChunk && strip_bytes(sh) + waves / 2 * kWaveSums <= kLdsBytes;  // a tile between two waves
   Plan best{~0ull, 1};
   for (uint32_t splits = 1; splits <= 8 && splits <= sh.tiles; ++splits) {
     const uint32_t each = ceil_div(sh.tiles, splits), full = each / waves, rest = each % waves;
-    const uint32_t halves = 2 * full + (rest == 0 ? 0 : full > 0 && rest <= waves / 2 && shares ? 1 : 2);
+    const uint32_t halves = 2 * full + (rest == 0 ? 0 : full > 0 && rest <= waves / 2 && sh.steps > kChunk ? 1 : 2);
     const uint64_t rounds = ceil_div(strips * splits, t.num_cus * (8 / waves));
     const uint64_t time = rounds * (pass * halves / 2 + fill);
     if (time < best.time) best = {time, splits};
@@ -861,8 +874,8 @@ hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t 
   // 1280 -> 512 698 : 685 : 641; 2^15 1024 -> 2048 4530 : 4290 : 3640.
   const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
   const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
-  const bool four = 2 * (strip_bytes(sh) + kJoinBytes<4>) <= kLdsBytes;
-  if (strip_bytes(sh) <= kLdsBytes) {
+  const bool four = 2 * (strip_bytes(sh) + 4 * kWaveSums) <= kLdsBytes;
+  if (strip_bytes(sh) + 8 * kWaveSums <= kLdsBytes) {
     const Plan plan = four ? plan_whole(t, sh, strips, 4, 80, 38) : plan_whole(t, sh, strips, 8, 82, 23);
     if (plan.time < wide && plan.time < tall)
       return four ? launch_whole<4>(t, a, strips, plan.splits, s) : launch_whole<8>(t, a, strips, plan.splits, s);
