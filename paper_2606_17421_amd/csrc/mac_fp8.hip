@@ -12,10 +12,12 @@
 // in 64-bit integers, and the sum over the blocks is reduced once an output.
 //
 // Four kernels share the arithmetic, chosen in launch():
+//   short    one block of inputs, their digits in registers (at 2^14, 4 limbs: 64 -> 256 40 us, 4.2 TB/s, outputs for the
+//            most part; 128 -> 512 91 us, 3.7 TB/s).
 //   thin     few outputs or few columns: residues go from memory through registers to the matrix cores; bound by
-//            memory (1024 -> 16 at 2^13, 3 limbs: 42.6 us, 4.8 TB/s, what a large copy reaches).
+//            memory (1024 -> 16 at 2^13, 3 limbs: 42 us, 4.8 TB/s, what a large copy reaches).
 //   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57 ms, 1.05e15 int8 products/s).
-//   whole    up to 1280 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.63 ms,
+//   whole    up to 1024 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.64 ms,
 //            1.2e15 products/s; a large int8 matrix product of the library's makes 1.03e15).
 // What bounds the last two: issue and power.  A block of a row tile takes a SIMD 1680 cycles in 1024 -> 2048: its 32 matrix
 // operations keep the matrix pipe busy for 1024 of them (61%) and take 16 issue cycles each, beside 48 multiply-adds of 8.7
@@ -351,8 +353,7 @@ __device__ __forceinline__ Source source_of(const Layers& a, const Job& job, uin
 
 // A wave's weights and scales of one block.  They are loaded again, for the block after the next, as soon as they are
 // used, so that two blocks' contractions cover the loads (and the residues' before them, since a wave's loads are
-// waited for in order); steps past the layer's last read as zero through the
-// buffer range check.
+// waited for in order); steps past the layer's last read as zero through the buffer range check.
 template <Form kForm>
 struct Weights {
   v4i w[kBlockSteps][kDigits];
@@ -465,6 +466,7 @@ __device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, u
     }
     if (slices > 2) __syncthreads();
   }
+  wave_fence();  // the sums' place, a wave's own by now, is written again
 }
 
 // A wave has 32 columns, one row tile and one of `slices` shares of the blocks, and its residues go from memory to
@@ -524,12 +526,12 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
   uint32_t y[kOuts<kForm>];
   reduce(acc, q, y);
   join(y, q.q, sums, wave, waves, slices);
-  if (slices > 1) __syncthreads();  // the sums' place is written again
   if (slice == 0) store<kForm>(job.dst + strip * 32, row_bytes(tb, a), a.d_out, job.split, y, sums + wave * (kOuts<kForm> * 16));
 }
 
 // One block of inputs: a wave converts its 32 columns once, keeps their digits in registers and goes through the row tiles
-// of its split, the next tile's weights in flight (its scales would be 48 registers more).  No LDS, and nothing that waves wait for together.
+// of its split, the next tile's weights in flight (its scales would be 48 registers more).  No LDS, and nothing that waves
+// wait for together (64 -> 256 at 2^14 and 4 limbs: 40 us; as chunks through LDS 72).
 constexpr int kShortWaves = 4;  // of a workgroup, next to each other
 template <int kSteps, Form kForm>
 __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
@@ -751,10 +753,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
       }
       uint32_t y[16];
       reduce(acc, q, y);
-      if (joins && pass == 0) {
-        join(y, q.q, sums, wave, kWaves, 2);
-        __syncthreads();  // the sums' place is written again
-      }
+      if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
       if (works && !(upper && pass == 0)) store<kRows>(job.dst, bytes, a.d_out, tile, y, sums + wave * 256);
     }
     if (kTwice) {
@@ -861,17 +860,16 @@ Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t wave
 hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
   const Shape& sh = a.sh;
   const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / 32);
-  // No more than 32 outputs, two row tiles of one block of inputs, or too few columns for the other kernels.  Thin : the
-  // best of the others, us, 2^14, 4 limbs: 16 -> 64 20 : 33, 128 -> 64 33 : 41, 256 -> 64 51 : 49, 64 -> 128 44 : 42; 2^10, 2
-  // limbs: 512 -> 128 8 : 12, 4096 -> 64 28 : 45, 1024 -> 256 15 : 18, 4096 -> 1024 171 : 121; 2^12, 2 limbs: 300 -> 64 8 :
-  // 10, 1024 -> 128 25 : 22.
-  if (sh.blocks == 1) return launch_short(t, a, strips, s);
-  if (sh.tiles <= 1 || (sh.tiles == 2 && sh.blocks <= 1) || strips * sh.tiles <= t.num_cus * 4ull)
+  if (sh.blocks == 1) return launch_short(t, a, strips, s);  // 2^14, 4 limbs, short : thin: 64 -> 256 40 : 72 us
+  // No more than 32 outputs, or too few columns for the other kernels.  Thin : the best of the others, us, 2^14, 4 limbs:
+  // 256 -> 16 31 : 42, 256 -> 64 48 : 46, 1024 -> 64 152 : 142; 2^10, 2 limbs: 512 -> 128 8.7 : 9.3, 1024 -> 256 16 : 18,
+  // 1024 -> 512 27 : 19; 2^12, 2 limbs: 300 -> 64 10.5 : 11.0, 256 -> 256 18 : 13, 1024 -> 128 35 : 24.
+  if (sh.tiles <= 1 || strips * sh.tiles <= t.num_cus * 4ull)
     return launch_thin(t, a, strips * sh.tiles, s);
   // A chunked job is 8 row tiles of one column tile or 4 of two; the others by a fit of their times.  2^14, 4 limbs, us, 4 x
-  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 256 -> 128 59 : 73 : 66, 128 -> 512 159 : 140 : 125, 512 -> 256 167 :
-  // 165 : 163, 512 -> 512 316 : 310 : 278, 1024 -> 256 296 : 296 : 306, 1024 -> 384 425 : 513 : 422, 1024 -> 512 555 : 552 : 516,
-  // 1280 -> 512 698 : 685 : 641; 2^15 1024 -> 2048 4530 : 4290 : 3640.
+  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 256 -> 128 58 : 73 : 62, 256 -> 256 103 : 101 : 96, 300 -> 333 191 :
+  // 238 : 159, 512 -> 256 165 : 166 : 162, 512 -> 512 320 : 316 : 278, 1024 -> 256 297 : 300 : 306, 1024 -> 384 426 : 523 :
+  // 424, 1024 -> 512 569 : 566 : 520; 2^15, 4 limbs, 1024 -> 2048 4530 : 4290 : 3640.
   const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
   const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
   const bool four = 2 * (strip_bytes(sh) + 4 * kWaveSums) <= kLdsBytes;
