@@ -147,7 +147,7 @@ struct Layers {
   const int32_t* expert;  // [requests], or null: expert 0
   const int32_t* bundle;  // [requests], or null: the request's own number
   int32_t* status;        // [requests], or null
-  uint32_t experts, bundles, d_out, d_in, limbs;
+  uint32_t experts, bundles, count, d_out, d_in, limbs;
   Shape sh;
 };
 
@@ -176,15 +176,16 @@ __global__ __launch_bounds__(kThreads) void experts_status_kernel(Layers a, uint
 }
 
 // Request, limb, `cols` columns and share of the row tiles of a workgroup's job; false where the request names no
-// expert or no bundle.  An XCD's jobs are numbered by request, limb, column strip and row split, so that neighbours
-// share columns or weights; the strips of a limb (`cols` at most 128 of 2^11 and more) are a multiple of the 8 XCDs.
+// expert or no bundle.  An XCD has an eighth of every limb's columns (`cols` at most 128 of 2^11 and more, so there are
+// that many), its jobs numbered by limb, request, column strip and row split: neighbours share weights or columns, and a
+// limb of a bundle stays in the caches for the requests that name it too (16 requests of 4 bundles of 1024 -> 64 at 2^12, 3
+// limbs: 415 us with all limbs of a request in turn, 343 so).
 __device__ __forceinline__ bool place_of(const Tables& tb, const Layers& a, uint32_t cols, uint32_t splits, uint32_t id, Job* job) {
-  const uint32_t n = tb.n, strips = 2 * n / cols, per = strips * a.limbs * splits;
-  const uint32_t r = id / (per / 8), in = id - r * (per / 8) + (blockIdx.x & 7) * (per / 8);
-  const uint32_t split = in % splits, lc = in / splits, l = lc / strips, col0 = (lc - l * strips) * cols;
+  const uint32_t n = tb.n, strips = 2 * n / cols / 8, split = id % splits, u = id / splits, v = u / strips;
+  const uint32_t l = v / a.count, r = v - l * a.count, col0 = ((blockIdx.x & 7) * strips + u - v * strips) * cols;
   uint32_t e, b;
   const bool good = named(a, r, &e, &b);
-  if (a.status && in == 0 && threadIdx.x == 0) a.status[r] = good ? kExpertOk : kExpertBadRequest;
+  if (a.status && l == 0 && col0 == 0 && split == 0 && threadIdx.x == 0) a.status[r] = good ? kExpertOk : kExpertBadRequest;
   if (!good) return false;
   const uint8_t* w = a.w + e * a.w_bytes;
   const size_t at = (static_cast<size_t>(col0 >> tb.log_n) * a.limbs + l) * n + (col0 & (n - 1));
@@ -911,7 +912,7 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
                           const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
                           uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, hipStream_t s) {
   Layers a{static_cast<const uint8_t*>(w_fp8), fp8_weight_bytes(d_out, d_in, limbs), ct_in, ct_out, expert, bundle, status,
-           experts, bundles, d_out, d_in, limbs, shape_of(d_out, d_in, limbs)};
+           experts, bundles, count, d_out, d_in, limbs, shape_of(d_out, d_in, limbs)};
   if (d_out == 0) {
     if (!status) return hipSuccess;
     experts_status_kernel<<<(count + kThreads - 1) / kThreads, kThreads, 0, s>>>(a, count);
