@@ -273,8 +273,8 @@ enum ckks_expert_status {
 
 /* Experts' layers in one call: request r is ckks_linear_mac_fp8 of expert[r]'s weights over bundle[r] of
  * the inputs.  An expert may have any number of requests, none included, and a bundle may be
- * named by several (tokens that go to two experts); requests of one expert next to each other share its
- * weights in the caches.  The lists are read on the device, so a call can be captured with room for the
+ * named by several (tokens that go to two experts); requests of one expert or one bundle next to each
+ * other share what they read in the caches.  The lists are read on the device, so a call can be captured with room for the
  * most requests: one that names no expert (-1) or no bundle leaves its outputs as they were and says
  * so in `status`.
  *   w_fp8   device [experts]: ckks_linear_encode_fp8's outputs for the same d_out, d_in and limbs,

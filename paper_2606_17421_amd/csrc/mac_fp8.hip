@@ -16,17 +16,18 @@
 //            most part; 128 -> 512 91 us, 3.7 TB/s).
 //   thin     few outputs or few columns: residues go from memory through registers to the matrix cores; bound by
 //            memory (1024 -> 16 at 2^13, 3 limbs: 42 us, 4.8 TB/s, what a large copy reaches).
-//   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57 ms, 1.05e15 int8 products/s).
-//   whole    up to 1024 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.64 ms,
-//            1.2e15 products/s; a large int8 matrix product of the library's makes 1.03e15).
+//   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57-1.65 ms over boxes,
+//            1.0e15 int8 products/s).
+//   whole    up to 1024 inputs: they stay in LDS while the waves walk the row tiles (1024 -> 2048 at 2^15, 4 limbs: 3.64-3.85
+//            ms, 1.15e15 products/s; large int8 matrix products of the library's make 1.0e15 to 1.2e15).
 // What bounds the last two: issue and power.  A block of a row tile takes a SIMD 1680 cycles in 1024 -> 2048: its 32 matrix
 // operations keep the matrix pipe busy for 1024 of them (61%) and take 16 issue cycles each, beside 48 multiply-adds of 8.7
 // and 72 other vector operations of 4.5, 1250 of the 1680 (measured alone: 20 matrix operations and 80 shift-adds of
-// another wave take 309 and 192 ns, 320 together; with 80 multiply-adds 313 and 311, 411 together).  The chip holds 1.87 GHz
-// (2.06 GHz and 48% chunked; a loop of nothing but matrix operations on random numbers makes 1.75e15 products/s at
+// another wave take 309 and 192 ns, 320 together; with 80 multiply-adds 313 and 311, 411 together).  The chip holds 1.83-1.87
+// GHz (1.96-2.06 GHz and 50% chunked; a loop of nothing but matrix operations on random numbers makes 1.75e15 products/s at
 // 1.7 GHz).  Without the weights' loads it takes 7% less, without the residues' 3%.  Measured without effect or worse:
 // sums combined between the same wave's matrix operations (3.65 -> 3.85 ms), wave priorities by phase or by half, a
-// delayed half, four-wave workgroups for the chunked kernel (4.2 -> 4.8 ms), stores or loads past the caches.
+// delayed half, four-wave workgroups for the chunked kernel (4.2 -> 4.8 ms), loads past the caches.
 #include <algorithm>
 
 #include "digits.hpp"
