@@ -29,11 +29,12 @@ def numbers(codes) -> np.ndarray:
 
 def plaintexts(codes, scales, block_rows: int, scale: float) -> np.ndarray:
     """The integers rint(64 f) rint(scales * scale / 64), as Python integers (object array d_out x d_in); NaN weights
-    and scales that are no finite number are zero."""
+    and scales that are NaN, infinite or scaled to 2^63 and more are zero."""
     f = numbers(codes)
     v = np.rint(64 * np.nan_to_num(f, nan=0.0)).astype(np.int64)
     s = np.asarray(scales, np.float32).astype(np.float64)
-    s = np.rint(np.where(np.isfinite(s), s, 0.0) * (scale / 64))
+    s = np.where(np.isfinite(s), s, 0.0) * (scale / 64)
+    s = np.rint(np.where(abs(s) < 2.0 ** 63, s, 0.0))
     s = np.vectorize(int, otypes=[object])(s) if s.size else s.astype(object)
     row, col = np.arange(v.shape[0]) // block_rows, np.arange(v.shape[1]) // BLOCK
     return v.astype(object) * s[row][:, col]

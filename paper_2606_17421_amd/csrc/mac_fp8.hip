@@ -122,8 +122,9 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
   uint32_t r = 0;
   if (row < d_out) {
     const float s = scales[static_cast<size_t>(row / block_rows) * blocks + block];
-    const bool fine = isfinite(s);
-    if (fine) r = reduce_f64_int(rint(static_cast<double>(s) * scale), q, tb.q_recip[l]);
+    const double v = static_cast<double>(s) * scale;
+    const bool fine = fabs(v) < 9223372036854775808.0;  // 2^63; no infinity and no NaN
+    if (fine) r = reduce_f64_int(rint(v), q, tb.q_recip[l]);
     if (bad && !fine && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
   }
 #pragma unroll

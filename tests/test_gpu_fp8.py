@@ -192,6 +192,22 @@ def test_huge_scales(gpu_lib):
 
 
 @gpu
+def test_scales_past_63_bits_are_counted(gpu_lib):
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    codes, _ = layer(527, 9, 640)
+    scales = np.array([[2.0 ** 63, -(2.0 ** 63), np.nextafter(np.float32(2.0 ** 63), np.float32(0)), 3e38, 3.0]], np.float32)
+    bad = torch.zeros(1, dtype=torch.int32, device="cuda")
+    enc = encode(ck, ctx, codes, scales, 128, 2, 64.0, bad)
+    assert int(bad) == 3
+    ct = gen.uniform_residues(np.random.default_rng(528), (640, 2), ctx.moduli, ctx.n)
+    out = ck.empty_u32((9, 2, 2, ctx.n))
+    ck.ckks_linear_mac_fp8(ctx, enc, ck.to_device(ct), out, 9, 640, 2)
+    assert np.array_equal(ck.to_host_u32(out), OF.mac(codes, scales, ct, 128, 64.0, ctx.moduli).astype(np.uint32))
+
+
+@gpu
 def test_what_is_no_number_is_counted(gpu_lib):
     import torch
     ck = gpu_lib
