@@ -40,6 +40,7 @@ constexpr uint32_t kStep = 32;        // inputs of one matrix-core step
 constexpr uint32_t kBlock = 128;      // inputs that share a scale
 constexpr uint32_t kBlockSteps = kBlock / kStep;
 constexpr uint32_t kFoldBlocks = 8;   // most blocks between reductions of the 64-bit sums
+constexpr uint32_t kFewBlocks = 4;    // of a layer whose sums take the shorter of them
 constexpr int kPairs = 5;             // digit sums of a block: weight digit a times residue digit b in sum a + b
 constexpr int kDigits = 2;            // of a weight
 constexpr uint32_t kChunkBlocks = 2, kChunk = kChunkBlocks * kBlockSteps;  // blocks and steps that go into LDS at a time
@@ -274,6 +275,16 @@ __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {
   return min(u, u - m.q);
 }
 
+// The same for sums of at most kFewBlocks blocks, |T| <= 4 * 0.877e9 q < 0.82 q 2^32.  With the factor m of
+// q signed the quotient of T - m q lies within (0.82 + 0.5) q, which one conditional correction by 2 q and one by q take
+// to [0, q); one 64-bit multiply-add gives it (256 -> 1024 at 2^14 and 4 limbs: 294 -> 281 us, 128 -> 512: 92 -> 89).
+__device__ __forceinline__ uint32_t reduce_few(int64_t t, const Modulus& m) {
+  const int32_t k = static_cast<int32_t>(static_cast<uint32_t>(t) * m.qinv);
+  const uint32_t h = static_cast<uint32_t>((t - static_cast<int64_t>(k) * static_cast<int32_t>(m.q)) >> 32);
+  const uint32_t u = min(h, h + 2 * m.q);
+  return min(u, u - m.q);
+}
+
 // Which of its row tile's outputs a lane has.
 //   kRows     residues times weights: row l % 32, and of the 32 columns 4 (l / 32) + 8 i + 0 .. 3.
 //   kColumns  weights times residues: column l % 32, rows 4 (l / 32) + 8 i + 0 .. 3.  Stores fill whole lines and can pass
@@ -330,10 +341,10 @@ __device__ __forceinline__ void clear(int64_t (&acc)[kN]) {
   for (int r = 0; r < kN; ++r) acc[r] = 0;
 }
 
-template <int kN>
+template <bool kFewOf = false, int kN>
 __device__ __forceinline__ void reduce(const int64_t (&acc)[kN], const Modulus& q, uint32_t (&y)[kN]) {
 #pragma unroll
-  for (int r = 0; r < kN; ++r) y[r] = reduce(acc[r], q);
+  for (int r = 0; r < kN; ++r) y[r] = kFewOf ? reduce_few(acc[r], q) : reduce(acc[r], q);
 }
 
 // The sum so far, reduced, goes on as a product.
@@ -578,7 +589,7 @@ __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tabl
     clear(acc);
     combine<kForm>(m, w.sc, acc);
     uint32_t y[kOuts<kForm>];
-    reduce(acc, q, y);
+    reduce<true>(acc, q, y);
     store<kForm>(job.dst, row_bytes(tb, a), a.d_out, tile, y);
   }
 }
@@ -666,6 +677,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
 //
 // The row tiles that are no multiple of kWaves come first.  Where they are at most half of it (and others
 // follow) two waves take a tile's chunks half and half and their sums meet in LDS.
+// Four waves have at most kFewBlocks blocks, which are never folded.
 template <int kWaves, bool kTwice>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
   constexpr int kPasses = kChunk / kWaves;
@@ -739,7 +751,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
           if (placed < fetched) place_piece();
           if (fetched < wanted) fetch_piece();
         }
-        if (c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
+        if (kWaves == 8 && c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
         read(f, x);
         contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
         if (!kTwice && kPasses == 2 && last) {
@@ -755,7 +767,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
         }
       }
       uint32_t y[16];
-      reduce(acc, q, y);
+      reduce<kWaves == 4>(acc, q, y);
       if (joins && pass == 0) join(y, q.q, sums, wave, kWaves, 2);
       if (works && !(upper && pass == 0)) store<kRows>(job.dst, bytes, a.d_out, tile, y, sums + wave * 256);
     }
@@ -831,7 +843,9 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
   const size_t strip = strip_bytes(a.sh), sums = kWaves * kWaveSums;
   const uint32_t n = static_cast<uint32_t>(jobs);
-  if constexpr (kWaves == 4) {  // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs: 91 -> 88 us)
+  if constexpr (kWaves == 4) {
+    if (a.sh.blocks > kFewBlocks) return hipErrorInvalidConfiguration;
+    // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs: 91 -> 88 us)
     if (2 * (2 * strip + sums) <= kLdsBytes)
       mac_fp8_whole_kernel<4, true><<<grid, 256, 2 * strip + sums, s>>>(t, a, splits, n);
     else
@@ -875,7 +889,8 @@ hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t 
   // 424, 1024 -> 512 569 : 566 : 520; 2^15, 4 limbs, 1024 -> 2048 4530 : 4290 : 3640.
   const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
   const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
-  const bool four = 2 * (strip_bytes(sh) + 4 * kWaveSums) <= kLdsBytes;
+  const bool four = sh.blocks <= kFewBlocks;  // two workgroups' strips, and room for their outputs, fit the LDS
+  static_assert(2 * (kFewBlocks * kBlockSteps * kStepFrags * 16 + 4 * kWaveSums) <= kLdsBytes, "two workgroups a CU");
   if (strip_bytes(sh) + 8 * kWaveSums <= kLdsBytes) {
     const Plan plan = four ? plan_whole(t, sh, strips, 4, 80, 38) : plan_whole(t, sh, strips, 8, 82, 23);
     if (plan.time < wide && plan.time < tall)

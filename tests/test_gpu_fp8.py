@@ -153,16 +153,11 @@ def test_fewer_limbs_than_the_context(gpu_lib):
     check(gpu_lib, 11, 4, 33, 165, 520, limbs_used=2)
 
 
-@gpu
-@pytest.mark.parametrize("d_in", [128, 1024, 1100, 2100])
-@pytest.mark.parametrize("code", [0x7E, 0xFE, 0x5F, 0xDF])
-@pytest.mark.parametrize("limbs,d_out", [(1, 4), (1, 300), (MANY, 4), (MANY, 300)])
-def test_the_largest_sums(gpu_lib, limbs, d_out, code, d_in):
+def largest_sums(ck, limbs, d_out, code, d_in):
     """Every weight at an end of its range (28672 units) or of its low digit's (1920 = 8 * 256 - 128), every
     input at an end of the digits' range or q - 1, and scales whose constants are the largest centred
     residues: 2^32, 2^48 or 2^64 times the first prime's are (q - 1) / 2 or (q + 1) / 2."""
     import torch
-    ck = gpu_lib
     ctx = ctx_for(ck, 10, limbs)
     codes = np.full((d_out, d_in), code, np.uint8)
     q = ctx.moduli[0]
@@ -178,6 +173,21 @@ def test_the_largest_sums(gpu_lib, limbs, d_out, code, d_in):
                 got = run(ck, ctx, codes, scales, d_ct, 128, 64.0 * s)
                 want = OF.mac(codes[:1], scales[:1], ct[..., :1], 128, 64.0 * s, ctx.moduli).astype(np.int32)
                 assert bool((got == torch.from_numpy(want).cuda()).all()), (residue, shift, half)
+
+
+@gpu
+@pytest.mark.parametrize("d_in", [128, 1024, 1100, 2100])
+@pytest.mark.parametrize("code", [0x7E, 0xFE, 0x5F, 0xDF])
+@pytest.mark.parametrize("limbs,d_out", [(1, 4), (1, 300), (MANY, 4), (MANY, 300)])
+def test_the_largest_sums(gpu_lib, limbs, d_out, code, d_in):
+    largest_sums(gpu_lib, limbs, d_out, code, d_in)
+
+
+@gpu
+@pytest.mark.parametrize("d_in", [256, 384, 512])
+@pytest.mark.parametrize("code", [0x7E, 0xFE, 0x5F, 0xDF])
+def test_the_largest_sums_of_few_blocks(gpu_lib, code, d_in):
+    largest_sums(gpu_lib, MANY, 300, code, d_in)
 
 
 @gpu
