@@ -12,8 +12,8 @@
 // in 64-bit integers, and the sum over the blocks is reduced once an output.
 //
 // Four kernels share the arithmetic, chosen in launch():
-//   short    one block of inputs, their digits in registers (at 2^14, 4 limbs: 64 -> 256 40 us, 4.2 TB/s, outputs for the
-//            most part; 128 -> 512 91 us, 3.7 TB/s).
+//   short    one block of inputs, their digits in registers (at 2^14, 4 limbs: 64 -> 256 39 us, 4.3 TB/s, outputs for the
+//            most part; 128 -> 512 89 us, 3.8 TB/s).
 //   thin     few outputs or few columns: residues go from memory through registers to the matrix cores; bound by
 //            memory (1024 -> 16 at 2^13, 3 limbs: 42 us, 4.8 TB/s, what a large copy reaches).
 //   chunked  a row tile a wave, all inputs in turn (2048 -> 768 at 2^14, 4 limbs: 1.57-1.65 ms over boxes,
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 
 // One block of inputs: a wave converts its 32 columns once, keeps their digits in registers and goes through the row tiles
 // of its split, the next tile's weights in flight (its scales would be 48 registers more).  No LDS, and nothing that waves
-// wait for together (64 -> 256 at 2^14 and 4 limbs: 40 us; as chunks through LDS 72).
+// wait for together (64 -> 256 at 2^14 and 4 limbs: 39 us; as chunks through LDS 72).
 constexpr int kShortWaves = 4;  // of a workgroup, next to each other
 template <int kSteps, Form kForm>
 __global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
@@ -845,7 +845,7 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint32_t n = static_cast<uint32_t>(jobs);
   if constexpr (kWaves == 4) {
     if (a.sh.blocks > kFewBlocks) return hipErrorInvalidConfiguration;
-    // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs: 91 -> 88 us)
+    // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs, before the shorter reduction: 91 -> 88 us)
     if (2 * (2 * strip + sums) <= kLdsBytes)
       mac_fp8_whole_kernel<4, true><<<grid, 256, 2 * strip + sums, s>>>(t, a, splits, n);
     else
@@ -877,16 +877,16 @@ Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t wave
 hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
   const Shape& sh = a.sh;
   const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / 32);
-  if (sh.blocks == 1) return launch_short(t, a, strips, s);  // 2^14, 4 limbs, short : thin: 64 -> 256 40 : 72 us
+  if (sh.blocks == 1) return launch_short(t, a, strips, s);  // 2^14, 4 limbs, short : thin: 64 -> 256 39 : 72 us
   // No more than 32 outputs, or too few columns for the other kernels.  Thin : the best of the others, us, 2^14, 4 limbs:
-  // 256 -> 16 31 : 42, 256 -> 64 48 : 46, 1024 -> 64 152 : 142; 2^10, 2 limbs: 512 -> 128 8.7 : 9.3, 1024 -> 256 16 : 18,
-  // 1024 -> 512 27 : 19; 2^12, 2 limbs: 300 -> 64 10.5 : 11.0, 256 -> 256 18 : 13, 1024 -> 128 35 : 24.
+  // 256 -> 16 31 : 41, 256 -> 64 48 : 45, 1024 -> 64 150 : 140; 2^10, 2 limbs: 512 -> 128 8.2 : 9.3, 1024 -> 256 16 : 18,
+  // 1024 -> 512 27 : 19; 2^12, 2 limbs: 300 -> 64 10.3 : 10.9, 256 -> 256 18 : 13, 1024 -> 128 35 : 24.
   if (sh.tiles <= 1 || strips * sh.tiles <= t.num_cus * 4ull)
     return launch_thin(t, a, strips * sh.tiles, s);
   // A chunked job is 8 row tiles of one column tile or 4 of two; the others by a fit of their times.  2^14, 4 limbs, us, 4 x
-  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 256 -> 128 58 : 73 : 62, 256 -> 256 103 : 101 : 96, 300 -> 333 191 :
-  // 238 : 159, 512 -> 256 165 : 166 : 162, 512 -> 512 320 : 316 : 278, 1024 -> 256 297 : 300 : 306, 1024 -> 384 426 : 523 :
-  // 424, 1024 -> 512 569 : 566 : 520; 2^15, 4 limbs, 1024 -> 2048 4530 : 4290 : 3640.
+  // 2 : 8 x 1 : whole (of four waves up to 512 inputs): 256 -> 128 58 : 70 : 62, 256 -> 256 101 : 97 : 94, 300 -> 333 190 :
+  // 241 : 158, 512 -> 256 165 : 167 : 160, 512 -> 512 322 : 322 : 275, 1024 -> 256 298 : 302 : 310, 1024 -> 384 429 : 526 :
+  // 425, 1024 -> 512 571 : 573 : 525; 2^15, 4 limbs, 1024 -> 2048 4530 : 4290 : 3640.
   const uint64_t wide = ceil_div(strips / 2 * ceil_div(sh.tiles, 4), t.num_cus) * 100ull;
   const uint64_t tall = ceil_div(strips * ceil_div(sh.tiles, 8), t.num_cus) * 100ull;
   const bool four = sh.blocks <= kFewBlocks;  // two workgroups' strips, and room for their outputs, fit the LDS
