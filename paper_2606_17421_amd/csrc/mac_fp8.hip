@@ -488,11 +488,12 @@ __device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, u
 // nothing to wait for but the loads, of which those of four steps are in flight.
 constexpr int kThinWaves = 8;  // of a workgroup, at most
 template <Form kForm>
-__global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
+__global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices,
+                                                                        uint32_t group0) {
   __shared__ v4i sums[kThinWaves * kOuts<kForm> * 16];
   Job job;
   const uint32_t waves = blockDim.x / 64, strips = waves / slices;
-  if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
+  if (!place_of(tb, a, strips * 32, a.sh.tiles, (group0 + blockIdx.x) >> 3, &job)) return;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % strips, slice = wave / strips;
   const uint32_t blocks = a.sh.blocks, each = (blocks + slices - 1) / slices, steps = a.sh.steps;
   const uint32_t begin = min(blocks, slice * each), end = min(blocks, begin + each);
@@ -548,9 +549,10 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 // wait for together (64 -> 256 at 2^14 and 4 limbs: 39 us; as chunks through LDS 72).
 constexpr int kShortWaves = 4;  // of a workgroup, next to each other
 template <int kSteps, Form kForm>
-__global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
+__global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits,
+                                                                          uint32_t group0) {
   Job job;
-  if (!place_of(tb, a, kShortWaves * 32, splits, range_of(gridDim.x).first, &job)) return;
+  if (!place_of(tb, a, kShortWaves * 32, splits, (group0 + blockIdx.x) >> 3, &job)) return;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = a.sh.tiles;
   const uint32_t each = (tiles + splits - 1) / splits, begin = job.split * each, end = min(tiles, begin + each);
   if (begin >= end) return;
@@ -805,25 +807,25 @@ hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStre
   while (slices < kThinWaves && 2 * slices <= a.sh.blocks && 2 * waves * slices <= t.num_cus * 8ull) slices *= 2;
   const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
   const uint64_t grid = waves * slices / group;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const auto k = a.d_out <= kFewRows ? mac_fp8_thin_kernel<kFew> : mac_fp8_thin_kernel<kRows>;
-  k<<<static_cast<uint32_t>(grid), group * 64, 0, s>>>(t, a, slices);
-  return hipGetLastError();
+  return in_pieces(grid, [&](uint64_t first, uint32_t groups) {
+    k<<<groups, group * 64, 0, s>>>(t, a, slices, static_cast<uint32_t>(first));
+  });
 }
 
 hipError_t launch_short(const Tables& t, const Layers& a, uint64_t strips, hipStream_t s) {
   // eight waves a CU where the row tiles allow it
   const uint32_t splits = static_cast<uint32_t>(std::min<uint64_t>(a.sh.tiles, (t.num_cus * 8ull + strips - 1) / strips));
   const uint64_t grid = strips / kShortWaves * splits;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
   const auto k = a.d_out <= kFewRows ? (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kFew>
                                         : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kFew>
                                                           : mac_fp8_short_kernel<4, kFew>)
                                      : (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kColumns>
                                         : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kColumns>
                                                           : mac_fp8_short_kernel<4, kColumns>);
-  k<<<static_cast<uint32_t>(grid), kShortWaves * 64, 0, s>>>(t, a, splits);
-  return hipGetLastError();
+  return in_pieces(grid, [&](uint64_t first, uint32_t groups) {
+    k<<<groups, kShortWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(first));
+  });
 }
 
 template <int kColWaves>
