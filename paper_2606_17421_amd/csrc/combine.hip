@@ -139,14 +139,20 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(Tables tb, const uint
 hipError_t launch_combine(const Tables& t, const uint32_t* gates, const uint32_t* ct_in, uint32_t count,
                           const int32_t* terms, uint32_t bundles, uint32_t top, uint32_t* ct_out, uint32_t features,
                           uint32_t limbs, hipStream_t s) {
-  const uint64_t groups = static_cast<uint64_t>(bundles) * limbs * (t.n / kCols);
+  const uint32_t each = limbs * (t.n / kCols);  // workgroups of a bundle and share, 2^10 at most
+  const uint64_t groups = static_cast<uint64_t>(bundles) * each;
   // eight workgroups a CU where the features allow it
   const uint64_t want = (static_cast<uint64_t>(t.num_cus) * 8 + groups - 1) / groups;
   const uint32_t shares = static_cast<uint32_t>(want < features ? want : features);
-  if (groups * shares > 0x7FFFFFFFull) return hipErrorInvalidConfiguration;
-  combine_kernel<<<static_cast<uint32_t>(groups * shares), kThreads, 0, s>>>(t, gates, ct_in, count, terms, top, ct_out,
-                                                                             features, limbs, shares);
-  return hipGetLastError();
+  const uint32_t most = kMostGroups / (each * shares);  // bundles of a launch; shares are more than one of few groups only
+  const size_t bundle_words = static_cast<size_t>(2) * limbs * t.n * features;
+  for (uint32_t b = 0; b < bundles; b += most) {
+    const uint32_t now = bundles - b < most ? bundles - b : most;
+    combine_kernel<<<now * each * shares, kThreads, 0, s>>>(t, gates, ct_in, count, terms + static_cast<size_t>(b) * top, top,
+                                                            ct_out + b * bundle_words, features, limbs, shares);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ckks

@@ -66,3 +66,41 @@ def test_experts_in_two_pieces(gpu_lib, d_out, d_in):
 def test_experts_past_2_32_work_items(gpu_lib, d_in):
     """8 GiB of outputs: 2051 requests of 8 limbs of 2^16 coefficients, one output each."""
     check_experts(gpu_lib, 16, 8, 2051, 1, d_in)
+
+
+def check_sums(ck, log_n, limbs, bundles, features):
+    import torch
+    ctx = ctx_for(ck, log_n, limbs)
+    gates, y = residues(ctx, 3), residues(ctx, 3, features, 2, seed=8)
+    lists = [[0, 1], [2, -1], [1, 1], [-1, -1], [2, 0]]
+    want = ck.empty_u32((len(lists), features, 2, limbs, ctx.n))
+    ck.ckks_experts_combine(ctx, gates, y, ints(lists), want, features, limbs)
+    cols = [0, 1023, ctx.n - 1]
+    pick = lambda t: t[..., cols].cpu().numpy().view(np.uint32)  # noqa: E731
+    assert np.array_equal(pick(want), OF.combine(pick(gates), pick(y), lists, ctx.moduli).astype(np.uint32))
+    out = ck.empty_u32((bundles, features, 2, limbs, ctx.n))
+    out.fill_(-1)
+    terms = ints(lists)[torch.arange(bundles, device="cuda") % len(lists)].contiguous()
+    ck.ckks_experts_combine(ctx, gates, y, terms, out, features, limbs)
+    assert repeats(out, want)
+
+
+def room_for(gib):
+    import torch
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"needs {gib} GiB of device memory")
+
+
+@gpu
+def test_sums_in_two_pieces(gpu_lib):
+    check_sums(gpu_lib, 11, 16, 33001, 1)
+
+
+@gpu
+def test_sums_past_2_32_work_items(gpu_lib):
+    """128 GiB of outputs: 32771 bundles of one feature, 8 limbs of 2^16 coefficients."""
+    import torch
+    room_for(150)
+    check_sums(gpu_lib, 16, 8, 32771, 1)
+    torch.cuda.empty_cache()
