@@ -78,9 +78,9 @@ __device__ __forceinline__ int32_t units_of(uint32_t code, bool* nan) {
 }
 
 __global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __restrict__ w8, uint32_t d_out, uint32_t d_in,
-                                                            uint32_t steps, size_t lanes, int32_t* bad,
+                                                            uint32_t steps, size_t lanes, size_t group0, int32_t* bad,
                                                             v4i* __restrict__ frag) {
-  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;
+  const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;
   if (idx >= lanes) return;
   const uint32_t lane = idx & 63;
   const uint32_t step = static_cast<uint32_t>((idx >> 6) % steps), tile = static_cast<uint32_t>((idx >> 6) / steps);
@@ -111,9 +111,9 @@ __global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __res
 
 __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const float* __restrict__ scales, uint32_t d_out,
                                                              uint32_t block_rows, uint32_t blocks, uint32_t tiles,
-                                                             size_t total, double scale, int32_t* bad,
+                                                             size_t total, size_t group0, double scale, int32_t* bad,
                                                              int32_t* __restrict__ out) {
-  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][block][32]
+  const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][block][32]
   if (idx >= total) return;
   const uint32_t block = static_cast<uint32_t>((idx >> 5) % blocks);
   const size_t lt = (idx >> 5) / blocks;
@@ -916,15 +916,15 @@ hipError_t launch_encode_fp8(const Tables& t, const uint8_t* w8, const float* sc
   if (bad)
     if (hipError_t e = launch_zero(reinterpret_cast<uint32_t*>(bad), 1, s); e != hipSuccess) return e;
   const size_t lanes = static_cast<size_t>(sh.tiles) * sh.steps * 64;
-  if (lanes / kThreads > 0x7FFFFFFFu) return hipErrorInvalidConfiguration;
-  fp8_frag_kernel<<<static_cast<uint32_t>((lanes + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      w8, d_out, d_in, sh.steps, lanes, bad, reinterpret_cast<v4i*>(base));
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipError_t e = in_pieces((lanes + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
+    fp8_frag_kernel<<<groups, kThreads, 0, s>>>(w8, d_out, d_in, sh.steps, lanes, first, bad, reinterpret_cast<v4i*>(base));
+  });
+  if (e != hipSuccess) return e;
   const size_t total = static_cast<size_t>(limbs) * sh.tiles * sh.blocks * 32;
-  fp8_scale_kernel<<<static_cast<uint32_t>((total + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      t, scales, d_out, block_rows, sh.blocks, sh.tiles, total, scale / 64, bad,
-      reinterpret_cast<int32_t*>(base + sh.frag_bytes));
-  return hipGetLastError();
+  return in_pieces((total + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
+    fp8_scale_kernel<<<groups, kThreads, 0, s>>>(t, scales, d_out, block_rows, sh.blocks, sh.tiles, total, first, scale / 64,
+                                                 bad, reinterpret_cast<int32_t*>(base + sh.frag_bytes));
+  });
 }
 
 hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, const int32_t* expert,

@@ -104,3 +104,48 @@ def test_sums_past_2_32_work_items(gpu_lib):
     room_for(150)
     check_sums(gpu_lib, 16, 8, 32771, 1)
     torch.cuda.empty_cache()
+
+
+def check_encode(ck, log_n, limbs, d_out, d_in, block_rows, seed=930):
+    """Layers whose rows repeat every 32: the encoding of a row tile is that of a layer of 32 rows."""
+    import torch
+    ctx = ctx_for(ck, log_n, limbs)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    part = torch.randint(0, 256, (32, d_in), generator=g, device="cuda", dtype=torch.uint8)
+    part[(part & 127) == 127] = 3
+    blocks, tiles, steps = -(-d_in // 128), -(-d_out // 32), -(-d_in // 32)
+    scales = torch.randn((1, blocks), generator=g, device="cuda") * 2e-4
+    w8 = torch.empty((d_out, d_in), dtype=torch.uint8, device="cuda")
+    whole = d_out // 32 * 32
+    w8[:whole].view(-1, 32, d_in).copy_(part)
+    w8[whole:] = part[:d_out - whole]
+    bad = ints([5])
+    rows = -(-d_out // block_rows)
+    enc = torch.empty(ck.ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs), dtype=torch.uint8, device="cuda")
+    enc.fill_(0xEE)
+    ck.ckks_linear_encode_fp8(ctx, w8, scales.expand(rows, blocks).contiguous(), d_out, d_in, block_rows, limbs, 2.0 ** 30, enc, bad)
+    assert int(bad) == 0
+    del w8
+    one = torch.empty(ck.ckks_fp8_weight_bytes(ctx, 32, d_in, limbs), dtype=torch.uint8, device="cuda")
+    ck.ckks_linear_encode_fp8(ctx, part, scales, 32, d_in, 32, limbs, 2.0 ** 30, one)
+    frag, sc = steps * 2048, blocks * 3 * 32 * 4
+    full = d_out // 32
+    assert repeats(enc[:full * frag].view(full, -1), one[:frag].view(1, -1))
+    at = enc[tiles * frag:].view(limbs, tiles, sc)
+    for l in range(limbs):
+        assert repeats(at[l, :full], one[frag:].view(limbs, 1, sc)[l])
+
+
+@gpu
+@pytest.mark.parametrize("limbs,d_out,d_in", [(1, 16416, 16400), (16, 2080, 16400)])
+def test_encode_fp8_in_pieces(gpu_lib, limbs, d_out, d_in):
+    check_encode(gpu_lib, 10, limbs, d_out, d_in, 128)
+
+
+@gpu
+def test_encode_fp8_scales_past_2_32_work_items(gpu_lib):
+    """16 limbs of 2^16 inputs and as many outputs as there may be: 32 GiB of weights, 112 GiB encoded."""
+    import torch
+    room_for(170)
+    check_encode(gpu_lib, 10, 16, 524256, (1 << 16) + 128, 524256)
+    torch.cuda.empty_cache()
