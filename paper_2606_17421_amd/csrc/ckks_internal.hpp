@@ -140,6 +140,19 @@ __device__ __forceinline__ uint32_t reduce_f64_int(double v, uint32_t q, double 
 // Launchers (each returns hipSuccess or the launch error)
 // ---------------------------------------------------------------------------
 
+// Work of any number of workgroups, in launches of at most this many (a multiple of 8): HIP's work-items of a dimension
+// are a 32-bit number, and a launch of 2^32 and more runs what is left of it, without an error.
+constexpr uint32_t kMostGroups = 1u << 20;
+// launch(first, groups) starts the kernel whose workgroup 0 is workgroup `first` of the whole.
+template <typename Launch>
+hipError_t in_pieces(uint64_t groups, Launch launch) {
+  for (uint64_t first = 0; first < groups; first += kMostGroups) {
+    launch(first, static_cast<uint32_t>(groups - first < kMostGroups ? groups - first : kMostGroups));
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // In-place forward / inverse NTT of count_rows rows; logical row r uses limb
 // r % limbs and is physical row (r / limbs) * gstride + r % limbs of
 // rows[][N] (gstride 0 means limbs: packed [count][limbs][N]).
@@ -191,19 +204,6 @@ hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* sca
                             hipStream_t s);
 hipError_t launch_mac_q4(const Tables& t, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,
                          uint32_t d_in, uint32_t group, uint32_t limbs, bool zeros, hipStream_t s);
-
-// Work of any number of workgroups, in launches of at most this many (a multiple of 8): HIP's work-items of a dimension
-// are a 32-bit number, and a launch of 2^32 and more runs what is left of it, without an error.
-constexpr uint32_t kMostGroups = 1u << 20;
-// launch(first, groups) starts the kernel whose workgroup 0 is workgroup `first` of the whole.
-template <typename Launch>
-hipError_t in_pieces(uint64_t groups, Launch launch) {
-  for (uint64_t first = 0; first < groups; first += kMostGroups) {
-    launch(first, static_cast<uint32_t>(groups - first < kMostGroups ? groups - first : kMostGroups));
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
 
 // MAC over e4m3 weights with a scale for each block of 128 inputs and block_rows
 // outputs (mac_fp8.hip): count requests (expert, bundle); one layer is expert 0 of one

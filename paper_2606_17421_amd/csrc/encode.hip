@@ -435,10 +435,10 @@ hipError_t launch_poly(const Tables& t, const double* slots, uint32_t count, uin
 hipError_t launch_encode_scalar(const Tables& t, const double* w, size_t count, uint32_t limbs,
                                 double scale, uint32_t* w_enc, hipStream_t s) {
   if (count == 0) return hipSuccess;
-  const size_t grid = (count + kEncScalarThreads - 1) / kEncScalarThreads;
-  encode_scalar_kernel<<<static_cast<uint32_t>(grid), kEncScalarThreads, 0, s>>>(
-      t.q, t.q_recip, w, count, limbs, scale, w_enc);
-  return hipGetLastError();
+  return in_pieces((count + kEncScalarThreads - 1) / kEncScalarThreads, [&](uint64_t first, uint32_t groups) {
+    const size_t i = first * kEncScalarThreads;
+    encode_scalar_kernel<<<groups, kEncScalarThreads, 0, s>>>(t.q, t.q_recip, w + i, count - i, limbs, scale, w_enc + i * limbs);
+  });
 }
 
 hipError_t launch_encode_poly(const Tables& t, const double* slots, uint32_t count, uint32_t limbs,

@@ -149,3 +149,25 @@ def test_encode_fp8_scales_past_2_32_work_items(gpu_lib):
     room_for(170)
     check_encode(gpu_lib, 10, 16, 524256, (1 << 16) + 128, 524256)
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("d_out,d_in,rows", [(16416, 16400, 7), (65536 + 32, 65536, 11)])
+def test_encode_scalar_past_a_launch(gpu_lib, d_out, d_in, rows):
+    """More weights than a launch of 2^20 workgroups has, and than 2^32."""
+    import torch
+    ck = gpu_lib
+    room_for(60)
+    ctx = ctx_for(ck, 10, 1)
+    g = torch.Generator(device="cuda").manual_seed(940)
+    part = torch.randn((rows, d_in), generator=g, device="cuda", dtype=torch.float64)
+    w = torch.empty((d_out, d_in), dtype=torch.float64, device="cuda")
+    for r in range(rows):
+        w[r::rows] = part[r]
+    enc = torch.full((d_out, d_in), -1, dtype=torch.int32, device="cuda")
+    ck.ckks_linear_encode_scalar(ctx, w, d_out, d_in, 1, 2.0 ** 26, enc)
+    del w
+    q = ctx.moduli[0]
+    want = torch.round(part * 2.0 ** 26).to(torch.int64).remainder(q).to(torch.int32)
+    assert repeats(enc, want)
+    torch.cuda.empty_cache()
