@@ -764,9 +764,15 @@ __global__ __launch_bounds__(kThreads) void ct_add_kernel(Tables tb, const uint3
 hipError_t launch_ct_add(const Tables& t, const uint32_t* a, const uint32_t* b, uint32_t count, uint32_t limbs,
                          uint32_t* out, hipStream_t s) {
   if (count == 0) return hipSuccess;
-  ct_add_kernel<<<grid_for((static_cast<size_t>(count) * 2 * limbs << t.log_n) / 4), kThreads, 0, s>>>(t, a, b, count,
-                                                                                                     limbs, out);
-  return hipGetLastError();
+  const size_t words = static_cast<size_t>(2) * limbs << t.log_n;
+  const uint32_t most = kMostGroups / grid_for(words / 4);  // ciphertexts of a launch
+  for (uint32_t i = 0; i < count;) {
+    const uint32_t now = count - i < most ? count - i : most;
+    ct_add_kernel<<<grid_for(now * words / 4), kThreads, 0, s>>>(t, a + i * words, b + i * words, now, limbs, out + i * words);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    i += now;
+  }
+  return hipSuccess;
 }
 
 size_t rotate_workspace_bytes(const Tables& t, uint32_t inputs, uint32_t rotations) {
@@ -775,9 +781,13 @@ size_t rotate_workspace_bytes(const Tables& t, uint32_t inputs, uint32_t rotatio
 
 hipError_t launch_automorphism(const Tables& t, const uint32_t* in, size_t rows, uint32_t galois, uint32_t* out,
                                hipStream_t s) {
-  if (rows == 0) return hipSuccess;
-  automorphism_kernel<<<grid_for(rows << t.log_n), kThreads, 0, s>>>(t, in, rows, galois, out);
-  return hipGetLastError();
+  const size_t most = (static_cast<size_t>(kMostGroups) * kThreads) >> t.log_n;  // rows of a launch
+  for (size_t r = 0; r < rows; r += most) {
+    const size_t now = rows - r < most ? rows - r : most;
+    automorphism_kernel<<<grid_for(now << t.log_n), kThreads, 0, s>>>(t, in + (r << t.log_n), now, galois, out + (r << t.log_n));
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // `rotations` rotations of `inputs` ciphertexts (element m of in_seq from ct):

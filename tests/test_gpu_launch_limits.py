@@ -171,3 +171,42 @@ def test_encode_scalar_past_a_launch(gpu_lib, d_out, d_in, rows):
     want = torch.round(part * 2.0 ** 26).to(torch.int64).remainder(q).to(torch.int32)
     assert repeats(enc, want)
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("rows", [66003, (1 << 20) + 5])
+def test_automorphism_past_a_launch(gpu_lib, rows):
+    import torch
+    ck = gpu_lib
+    log_n = 12
+    room_for(40)
+    ctx = ctx_for(ck, log_n, 1)
+    part = residues(ctx, 5)[:, 0].contiguous()
+    want = torch.empty_like(part)
+    ck.ckks_automorphism(ctx, part, 5, 5, want)
+    src = part[torch.arange(rows, device="cuda") % 5]
+    out = torch.full_like(src, -1)
+    ck.ckks_automorphism(ctx, src, rows, 5, out)
+    assert repeats(out, want)
+    del src, out
+    torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("count", [16411, 1048583])
+def test_add_past_a_launch(gpu_lib, count):
+    """In place, 16 words of each coefficient a ciphertext: up to 128 GiB."""
+    import torch
+    ck = gpu_lib
+    room_for(150 if count > 1 << 20 else 8)
+    ctx = ctx_for(ck, 11, 8)
+    part = residues(ctx, 3, 2)
+    want = torch.empty_like(part)
+    ck.ckks_add(ctx, part, part, 3, 8, want)
+    a = ck.empty_u32((count, 2, 8, ctx.n))
+    for r in range(3):
+        a[r::3] = part[r]
+    ck.ckks_add(ctx, a, a, count, 8, a)
+    assert repeats(a, want)
+    del a
+    torch.cuda.empty_cache()
