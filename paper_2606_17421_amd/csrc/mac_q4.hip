@@ -82,9 +82,9 @@ template <bool kZeros>
 __global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __restrict__ w4,
                                                            const uint8_t* __restrict__ zeros, uint32_t d_out,
                                                            uint32_t d_in, uint32_t group, uint32_t groups,
-                                                           uint32_t steps, size_t lanes,
+                                                           uint32_t steps, size_t lanes, size_t group0,
                                                            Frag<kZeros>* __restrict__ frag) {
-  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;
+  const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;
   if (idx >= lanes) return;
   const uint32_t lane = idx & 63;
   const uint32_t step = static_cast<uint32_t>((idx >> 6) % steps), tile = static_cast<uint32_t>((idx >> 6) / steps);
@@ -120,9 +120,9 @@ __global__ __launch_bounds__(kThreads) void q4_frag_kernel(const uint8_t* __rest
 __global__ __launch_bounds__(kThreads) void q4_scale_kernel(Tables tb, const float* __restrict__ scales,
                                                             bool zeros, uint32_t d_out, uint32_t group,
                                                             uint32_t groups, uint32_t sub_len, uint32_t subs,
-                                                            uint32_t tiles, size_t total, double scale,
+                                                            uint32_t tiles, size_t total, size_t group0, double scale,
                                                             int2* __restrict__ out) {
-  const size_t idx = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][sub][32]
+  const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][sub][32]
   if (idx >= total) return;
   const uint32_t sub = static_cast<uint32_t>((idx >> 5) % subs);
   const size_t lt = (idx >> 5) / subs;
@@ -578,19 +578,19 @@ hipError_t launch_encode_q4(const Tables& t, const uint8_t* w4, const float* sca
   uint8_t* base = static_cast<uint8_t*>(w_q4);
   const size_t lanes = static_cast<size_t>(sh.tiles) * sh.steps * 64;
   const size_t total = static_cast<size_t>(limbs) * sh.tiles * sh.subs * 32;
-  const uint32_t grid = static_cast<uint32_t>((lanes + kThreads - 1) / kThreads);
-  if (zeros)
-    q4_frag_kernel<true><<<grid, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes,
-                                                   reinterpret_cast<v4i*>(base));
-  else
-    q4_frag_kernel<false><<<grid, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes,
-                                                    reinterpret_cast<uint2*>(base));
-  hipError_t e = hipGetLastError();
+  hipError_t e = in_pieces((lanes + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
+    if (zeros)
+      q4_frag_kernel<true><<<groups, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes, first,
+                                                       reinterpret_cast<v4i*>(base));
+    else
+      q4_frag_kernel<false><<<groups, kThreads, 0, s>>>(w4, zeros, d_out, d_in, group, sh.groups, sh.steps, lanes, first,
+                                                        reinterpret_cast<uint2*>(base));
+  });
   if (e != hipSuccess) return e;
-  q4_scale_kernel<<<static_cast<uint32_t>((total + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-      t, scales, zeros != nullptr, d_out, group, sh.groups, sh.sub_len, sh.subs, sh.tiles, total, scale,
-      reinterpret_cast<int2*>(base + sh.frag_bytes));
-  return hipGetLastError();
+  return in_pieces((total + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
+    q4_scale_kernel<<<groups, kThreads, 0, s>>>(t, scales, zeros != nullptr, d_out, group, sh.groups, sh.sub_len, sh.subs,
+                                                sh.tiles, total, first, scale, reinterpret_cast<int2*>(base + sh.frag_bytes));
+  });
 }
 
 hipError_t launch_mac_q4(const Tables& t, const void* w_q4, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,

@@ -210,3 +210,37 @@ def test_add_past_a_launch(gpu_lib, count):
     assert repeats(a, want)
     del a
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("limbs,d_out,d_in", [(16, 4128, 8224), (16, 524256, (1 << 14) + 32)])
+def test_encode_q4_past_a_launch(gpu_lib, limbs, d_out, d_in, zeros):
+    import torch
+    ck = gpu_lib
+    room_for(60 if d_out > 1 << 16 else 8)
+    ctx = ctx_for(ck, 10, 16)
+    g = torch.Generator(device="cuda").manual_seed(950)
+    groups, tiles = d_in // 32, d_out // 32
+    part = torch.randint(0, 256, (32, d_in // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randn((32, groups), generator=g, device="cuda") * 1e-3
+    zero = torch.randint(0, 16, (32, groups), generator=g, device="cuda", dtype=torch.uint8) if zeros else None
+
+    def many(t):
+        return None if t is None else t.expand(tiles, *t.shape).reshape(d_out, -1).contiguous()
+
+    def encode(w, s, z, rows):
+        enc = torch.full((ck.ckks_q4_weight_bytes(ctx, rows, d_in, 32, limbs, zeros),), 0xEE, dtype=torch.uint8, device="cuda")
+        ck.ckks_linear_encode_q4(ctx, w, s, z, rows, d_in, 32, limbs, 2.0 ** 30, enc)
+        return enc
+    two = lambda t: None if t is None else torch.cat([t, t])  # noqa: E731
+    one = encode(two(part), two(scales), two(zero), 64)     # rows are padded to 64
+    enc = encode(many(part), many(scales), many(zero), d_out)
+    frag, sc = groups * 64 * (16 if zeros else 8), groups * 32 * 8
+    assert repeats(enc[:tiles * frag].view(tiles, -1), one[:frag].view(1, -1))
+    padded = -(-tiles // 2) * 2
+    at, small = enc[padded * frag:].view(limbs, padded, sc), one[2 * frag:].view(limbs, 2, sc)
+    for l in range(limbs):
+        assert repeats(at[l, :tiles], small[l, :1])
+    del enc
+    torch.cuda.empty_cache()
