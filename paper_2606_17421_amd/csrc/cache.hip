@@ -639,8 +639,14 @@ hipError_t launch_cache_compact(const Cache& c, int32_t* live, void* workspace, 
 hipError_t launch_cache_gather(const Cache& c, const int32_t* seq, const int32_t* pos, uint32_t count, uint32_t* out,
                                hipStream_t s) {
   const uint32_t pieces = static_cast<uint32_t>((c.row_words + kPieceWords - 1) / kPieceWords);
-  cache_gather_kernel<<<count * pieces, kMoveThreads, 0, s>>>(c, seq, pos, pieces, out);
-  return hipGetLastError();
+  const uint32_t most = pieces < kMostGroups ? kMostGroups / pieces : 1;  // rows of a launch
+  for (uint32_t r = 0; r < count;) {
+    const uint32_t now = count - r < most ? count - r : most;
+    cache_gather_kernel<<<now * pieces, kMoveThreads, 0, s>>>(c, seq + r, pos + r, pieces, out + r * c.row_words);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    r += now;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ckks

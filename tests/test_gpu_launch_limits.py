@@ -244,3 +244,29 @@ def test_encode_q4_past_a_launch(gpu_lib, limbs, d_out, d_in, zeros):
         assert repeats(at[l, :tiles], small[l, :1])
     del enc
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("count,limbs", [((1 << 20) + 7, 1), (300000, 2), ((1 << 24) + 3, 1)])
+def test_gather_past_a_launch(gpu_lib, count, limbs):
+    """Rows of 8 and of 16 KiB, a few over and over, one of them absent: up to 128 GiB."""
+    import torch
+    ck = gpu_lib
+    room_for(150 if count > 1 << 23 else 12)
+    ctx = ctx_for(ck, 10, limbs)
+    cache = ck.Cache.empty(ctx, 3, 2, 1, limbs, 1, 3)
+    rows = residues(ctx, 5, 1, 2)
+    ws = ck.empty_workspace(ck.ckks_cache_workspace_bytes(ctx, cache, ck.CKKS_CACHE_APPEND, 1, 5))
+    ck.ckks_cache_append(ctx, cache, ints([0]), ints([0, 5]), rows, ws)
+    at = ints([0, 3, 4, 9, 1, 2])
+    want = torch.zeros((6, *rows.shape[1:]), dtype=torch.int32, device="cuda")
+    for k, p in enumerate(at.tolist()):
+        if p < 5:
+            want[k] = rows[p]
+    pos = at[torch.arange(count, device="cuda") % 6].contiguous()
+    out = ck.empty_u32((count, *rows.shape[1:]))
+    out.fill_(-1)
+    ck.ckks_cache_gather(ctx, cache, torch.zeros_like(pos), pos, out)
+    assert repeats(out, want)
+    del out
+    torch.cuda.empty_cache()
