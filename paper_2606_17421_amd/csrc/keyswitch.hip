@@ -987,9 +987,14 @@ hipError_t launch_bsgs(const Tables& t, const uint32_t* pt, const uint32_t* ct, 
                           ksk + static_cast<size_t>(n1 - 1) * key_words, rws, nullptr, contiguous(), s, nullptr);
   if (err != hipSuccess) return err;
   const uint32_t* acc = rot_layout(t, count * (n2 - 1), count * (n2 - 1), rws).acc;
-  giant_ext_kernel<<<static_cast<uint32_t>(count * 2 * (L + 1) * n / 64), kThreads, 0, s>>>(
-      t, inner, acc, L, count, n2, galois_of(n1, t.log_n), ext);
-  if ((err = hipGetLastError()) != hipSuccess) return err;
+  const size_t ext_words = 2 * (L + 1) * n;
+  const uint32_t each = static_cast<uint32_t>(ext_words / 64), most = kMostGroups / each;  // an input's workgroups, a launch's inputs
+  for (size_t b = 0; b < count; b += most) {
+    const uint32_t now = count - b < most ? static_cast<uint32_t>(count - b) : most;
+    giant_ext_kernel<<<now * each, kThreads, 0, s>>>(t, inner + b * n2 * ctw, acc + b * (n2 - 1) * ext_words, L, now, n2,
+                                                     galois_of(n1, t.log_n), ext + b * ext_words);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+  }
   return launch_rescale2(t, ext, baby, out, count, L + 1, rws, s);
 }
 

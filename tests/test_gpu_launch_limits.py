@@ -270,3 +270,25 @@ def test_gather_past_a_launch(gpu_lib, count, limbs):
     assert repeats(out, want)
     del out
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_bsgs_of_many_inputs(gpu_lib):
+    """Enough inputs that the giant steps' sums, four lanes a word, pass 2^32 work-items."""
+    import torch
+    ck = gpu_lib
+    room_for(60)
+    ctx = ctx_for(ck, 10, 3)
+    count, n1, n2 = 174763 + 5, 1, 2
+    pt, part = residues(ctx, n1 * n2)[:, :2].contiguous(), residues(ctx, 5, 2, seed=961)[:, :, :2].contiguous()
+    ksk = residues(ctx, 1, 2, 2, seed=962)
+
+    def product(ct, n):
+        ws = ck.empty_workspace(ck.bsgs_workspace_bytes(ctx, n, n1, n2))
+        out = torch.full((n, 2, 1, ctx.n), -1, dtype=torch.int32, device="cuda")
+        ck.ckks_linear_bsgs(ctx, pt, ct, n, n1, n2, ksk, ws, out)
+        return out
+    want = product(part, 5)
+    ct = part[torch.arange(count, device="cuda") % 5]
+    assert repeats(product(ct, count), want)
+    torch.cuda.empty_cache()
