@@ -900,16 +900,22 @@ hipError_t launch_keygen_rotation(const Tables& t, const uint32_t* s_ntt, uint32
                                   hipStream_t s) {
   if (keys == 0) return hipSuccess;
   const uint32_t L = t.L - 1, Lp = L + 1;
-  const size_t n = t.n;
-  keygen_err_kernel<<<grid_for(static_cast<size_t>(keys) * L * n / 4), kThreads, 0, s>>>(t, e, L, keys, ksk);
-  hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  // the b rows: logical row (key * L + digit) * Lp + j is physical row (.. / Lp) * 2 Lp + j
-  err = launch_ntt(t, ksk, static_cast<size_t>(keys) * L * Lp, Lp, false, s, 2 * Lp);
-  if (err != hipSuccess) return err;
-  keygen_combine_kernel<<<grid_for(static_cast<size_t>(keys) * L * Lp * n / 4), kThreads, 0, s>>>(
-      t, s_ntt, a, L, keys, r0, r_step, ksk);
-  return hipGetLastError();
+  const size_t n = t.n, e_words = L * n, a_words = e_words * Lp;  // of a key; its ksk has twice a's
+  const uint32_t most = kMostGroups / grid_for(a_words / 4);      // keys of a launch
+  for (size_t k = 0; k < keys; k += most) {
+    const uint32_t now = keys - k < most ? static_cast<uint32_t>(keys - k) : most;
+    uint32_t* to = ksk + k * 2 * a_words;
+    keygen_err_kernel<<<grid_for(now * e_words / 4), kThreads, 0, s>>>(t, e + k * e_words, L, now, to);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    // the b rows: logical row (key * L + digit) * Lp + j is physical row (.. / Lp) * 2 Lp + j
+    err = launch_ntt(t, to, static_cast<size_t>(now) * L * Lp, Lp, false, s, 2 * Lp);
+    if (err != hipSuccess) return err;
+    keygen_combine_kernel<<<grid_for(now * a_words / 4), kThreads, 0, s>>>(t, s_ntt, a + k * a_words, L, now,
+                                                                           r0 + static_cast<uint32_t>(k) * r_step, r_step, to);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 // Workspace of the BSGS product for `count` input ciphertexts: baby rotations

@@ -292,3 +292,22 @@ def test_bsgs_of_many_inputs(gpu_lib):
     ct = part[torch.arange(count, device="cuda") % 5]
     assert repeats(product(ct, count), want)
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_keys_past_a_launch(gpu_lib):
+    import torch
+    ck = gpu_lib
+    room_for(24)
+    ctx = ctx_for(ck, 10, 3)
+    keys, half = 174763 + 4, ctx.n // 2
+    s, a, e = residues(ctx), residues(ctx, 4, 2), torch.randint(-19, 20, (4, 2, ctx.n), dtype=torch.int32, device="cuda")
+    many = torch.arange(keys, device="cuda") % 4
+
+    def keygen(a, e, n):
+        out = torch.full((n, 2, 2, 3, ctx.n), -1, dtype=torch.int32, device="cuda")
+        ck.ckks_keygen_rotation(ctx, s, 3, half // 2, n, a, e, out)   # rotations by 3 and 3 + N/4 in turn
+        return out
+    want = keygen(a, e, 4)
+    assert repeats(keygen(a[many], e[many], keys), want)
+    torch.cuda.empty_cache()
