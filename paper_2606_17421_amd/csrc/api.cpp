@@ -442,15 +442,22 @@ int ckks_ctx_set_mac_algo(ckks_ctx* ctx, int algo) {
   return ok();
 }
 
+// Rows handed to the batched transforms, N / 16 work-items a row at most, must keep
+// their launches below 2^32 work-items, of which HIP runs what is left in 32 bits: 256 GiB.
+static int check_rows(const ckks_ctx* ctx, size_t count, uint32_t limbs) {
+  const size_t rows = count * limbs;
+  if (rows > 0xFFFFFFFFull / (ctx->n / 16)) return fail(CKKS_E_INVALID_ARG, "too many polynomials (%zu rows)", rows);
+  return CKKS_OK;
+}
+
 static int do_ntt(const ckks_ctx* ctx, uint32_t* polys, uint32_t count, uint32_t limbs, void* stream,
                   bool inverse) {
   if (int rc = check_ctx(ctx)) return rc;
   if (int rc = check_limbs(ctx, limbs, 1)) return rc;
   if (count == 0) return ok();
   if (int rc = check_ptr(polys, "polys")) return rc;
+  if (int rc = check_rows(ctx, count, limbs)) return rc;
   const size_t rows = static_cast<size_t>(count) * limbs;
-  if (rows > 0x7FFFFFFFull / (ctx->log_n == 16 ? 64 : 1))
-    return fail(CKKS_E_INVALID_ARG, "too many polynomials (%zu rows)", rows);
   DeviceGuard guard(ctx->device);
   hipError_t e = ckks::launch_ntt(ctx->t, polys, rows, limbs, inverse, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, inverse ? "intt launch" : "ntt launch");
@@ -486,13 +493,11 @@ int ckks_linear_encode_poly(const ckks_ctx* ctx, const double* slots, uint32_t c
   if (int rc = check_limbs(ctx, limbs, 1)) return rc;
   if (!(scale > 0.0) || !std::isfinite(scale)) return fail(CKKS_E_INVALID_ARG, "scale must be finite and > 0");
   if (count == 0) return ok();
+  if (int rc = check_rows(ctx, count, limbs)) return rc;
   if (int rc = check_ptr(slots, "slots")) return rc;
   if (int rc = check_ptr(pt, "pt")) return rc;
   if (overlaps(pt, size_t(count) * limbs * ctx->n * 4, slots, size_t(count) * (ctx->n / 2) * 8))
     return fail(CKKS_E_INVALID_ARG, "pt overlaps slots");
-  // at N = 2^16 the rows go through the batched transform (64 workgroups per row)
-  if (ctx->log_n == 16 && size_t(count) * limbs > 0x7FFFFFFFull / 64)
-    return fail(CKKS_E_INVALID_ARG, "count x limbs = %zu rows too many", size_t(count) * limbs);
   DeviceGuard guard(ctx->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = ckks::launch_encode_poly(ctx->t, slots, count, limbs, scale, pt, s);
@@ -618,15 +623,6 @@ int ckks_rescale(const ckks_ctx* ctx, const uint32_t* ct_in, uint32_t* ct_out, u
   hipError_t e = ckks::launch_rescale(ctx->t, ct_in, ct_out, count, limbs, workspace,
                                       static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "rescale launch");
-}
-
-// Rows handed to the batched transforms must keep their grids below 2^31
-// workgroups (64 per row in the N = 2^16 block pass).
-static int check_rows(const ckks_ctx* ctx, uint32_t count, uint32_t limbs) {
-  const size_t rows = static_cast<size_t>(count) * limbs;
-  if (rows > 0x7FFFFFFFull / (ctx->log_n == 16 ? 64 : 1))
-    return fail(CKKS_E_INVALID_ARG, "too many polynomials (%zu rows)", rows);
-  return CKKS_OK;
 }
 
 int ckks_encrypt(const ckks_ctx* ctx, const uint32_t* pt, const uint32_t* s_ntt, const uint32_t* a,
@@ -775,6 +771,9 @@ int ckks_linear_bsgs(const ckks_ctx* ctx, const uint32_t* pt, const uint32_t* ct
   if (count == 0) return ok();
   if (int rc = check_rows(ctx, count, static_cast<uint32_t>(Lk * L * (n1 > n2 ? n1 : n2)))) return rc;
   if (static_cast<uint64_t>(n2) * Lk * (n / 256) > 0x7FFFFFFFull) return fail(CKKS_E_INVALID_ARG, "n2=%u too large", n2);
+  // the batched MAC's workgroups of 256, eight rows and two inputs each
+  if (Lk * (n / 256) * ((n2 + 7) / 8) * ((size_t(count) + 1) / 2) > 0xFFFFFFull)
+    return fail(CKKS_E_INVALID_ARG, "count=%u too large", count);
   if (int rc = check_ptr(pt, "pt")) return rc;
   if (int rc = check_ptr(ct_in, "ct_in")) return rc;
   if (n1 + n2 > 2 && check_ptr(ksk, "ksk")) return CKKS_E_INVALID_ARG;
@@ -1193,8 +1192,7 @@ int ckks_cache_decrypt(const ckks_ctx* ctx, const ckks_cache* cache, const int32
   if (int rc = check_ptr(s_ntt, "s_ntt")) return rc;
   if (int rc = check_ptr(m, "m")) return rc;
   const size_t cts = size_t(count) * c.row_cts;
-  if (cts * c.limbs > 0x7FFFFFFFull / (ctx->log_n == 16 ? 64 : 1))
-    return fail(CKKS_E_INVALID_ARG, "count=%u rows too many", count);
+  if (int rc = check_rows(ctx, cts, c.limbs)) return rc;
   if (int rc = check_apart(c, {{m, cts * c.limbs * ctx->n * 4, "m"}},
                            {{seq, size_t(count) * 4, "seq"},
                             {pos, size_t(count) * 4, "pos"},

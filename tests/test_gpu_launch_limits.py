@@ -311,3 +311,24 @@ def test_keys_past_a_launch(gpu_lib):
     want = keygen(a, e, 4)
     assert repeats(keygen(a[many], e[many], keys), want)
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_more_rows_than_a_launch_are_refused(gpu_lib):
+    """256 GiB of rows of 2^10, named by a buffer of a few: the sizes alone are looked at."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 3)
+    some = ck.empty_u32((4, 2, 3, ctx.n))
+    p, lib, rows = some.data_ptr(), ck._lib, 1 << 26
+    cache = ck.Cache.empty(ctx, 1, 1, 1, 3, 1, 1)
+    bad = ck.CKKS_E_INVALID_ARG
+    import ctypes
+    for call in (lambda: lib.ckks_ntt(ctx.handle, p, rows, 1, None), lambda: lib.ckks_intt(ctx.handle, p, rows // 2, 2, None),
+                 lambda: lib.ckks_linear_encode_poly(ctx.handle, p, rows, 1, 1.0, p, None),
+                 lambda: lib.ckks_encrypt(ctx.handle, None, p, p, p, rows, 1, p, None),
+                 lambda: lib.ckks_decrypt(ctx.handle, p, p, rows, 1, p, None),
+                 lambda: lib.ckks_cache_decrypt(ctx.handle, ctypes.byref(cache.struct), p, p, p, rows, p, None)):
+        assert call() == bad
+        assert "too many polynomials" in ck.ckks_last_error()
+    assert lib.ckks_linear_bsgs(ctx.handle, p, p, 1 << 23, 1, 1, None, None, 0, p, None) == bad
+    assert "count" in ck.ckks_last_error()
