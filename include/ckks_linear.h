@@ -248,8 +248,8 @@ size_t ckks_fp8_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in,
  *   w_fp8   device, ckks_fp8_weight_bytes bytes, in a layout of the library's own; must not
  *           overlap the inputs.
  *   bad     device int32 [1], 4-byte aligned, or NULL: the number of weights that are NaN and of scales that are
- *           NaN, infinite or not below 2^63 as |scales * scale / 64|.  Such weights, and the weights of such scales,
- *           count as zero.
+ *           NaN, infinite, not below 2^63 as |scales * scale / 64|, or rounded to zero without being zero.  Such
+ *           weights, and the weights of such scales, count as zero.
  * Run once per layer. */
 int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
                            uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream);

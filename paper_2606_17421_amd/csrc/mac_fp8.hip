@@ -124,9 +124,11 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
   if (row < d_out) {
     const float s = scales[static_cast<size_t>(row / block_rows) * blocks + block];
     const double v = static_cast<double>(s) * scale;
+    const double whole = rint(v);
     const bool fine = fabs(v) < 9223372036854775808.0;  // 2^63; no infinity and no NaN
-    if (fine) r = reduce_f64_int(rint(v), q, tb.q_recip[l]);
-    if (bad && !fine && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
+    if (fine) r = reduce_f64_int(whole, q, tb.q_recip[l]);
+    const bool lost = whole == 0 && v != 0;  // a scale too small for `scale` takes its block's weights with it
+    if (bad && (!fine || lost) && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
   }
 #pragma unroll
   for (int d = 0; d < 3; ++d) {

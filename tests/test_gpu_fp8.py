@@ -218,6 +218,23 @@ def test_scales_past_63_bits_are_counted(gpu_lib):
 
 
 @gpu
+def test_scales_that_round_to_zero_are_counted(gpu_lib):
+    """Halves go to zero (to even); zeros are what they are."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 2)
+    codes, _ = layer(533, 70, 700)
+    scales = np.array([[0.0, -0.0, 0.5, -0.25, 1e-42, 0.51], [1.0, -0.5, 0.5000001, 0.0, -1e-30, 3.0], [2.0] * 6], np.float32)
+    bad = torch.zeros(1, dtype=torch.int32, device="cuda")
+    enc = encode(ck, ctx, codes, scales, 32, 2, 64.0, bad)
+    assert int(bad) == 5
+    ct = gen.uniform_residues(np.random.default_rng(534), (700, 2), ctx.moduli, ctx.n)
+    out = ck.empty_u32((70, 2, 2, ctx.n))
+    ck.ckks_linear_mac_fp8(ctx, enc, ck.to_device(ct), out, 70, 700, 2)
+    assert np.array_equal(ck.to_host_u32(out), OF.mac(codes, scales, ct, 32, 64.0, ctx.moduli).astype(np.uint32))
+
+
+@gpu
 def test_what_is_no_number_is_counted(gpu_lib):
     import torch
     ck = gpu_lib
