@@ -417,6 +417,8 @@ def ckks_linear_encode_fp8(ctx: Context, w8, scales, d_out: int, d_in: int, bloc
         raise ValueError(f"w8 must be float8_e4m3fn or its codes as uint8 (got {w8.dtype})")
     if scales is not None and scales.dtype != torch.float32:
         raise ValueError(f"scales must be float32 (got {scales.dtype})")
+    if bad is not None and bad.dtype != torch.int32:
+        raise ValueError(f"bad must be int32 (got {bad.dtype})")
     blocks = -(-d_out // block_rows) * -(-d_in // 128)
     _check(_lib.ckks_linear_encode_fp8(
         ctx.handle, _ptr(w8, "w8", d_out * d_in, 1), _ptr(scales, "scales", blocks * 4, 4), d_out, d_in, block_rows, limbs,
@@ -441,8 +443,9 @@ def ckks_experts_mac_fp8(ctx: Context, w_fp8, expert, bundle, ct_in, ct_out, d_o
     need = ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs)
     if need and w_fp8.numel() * _words(w_fp8) != experts * need:
         raise ValueError(f"w_fp8 must be [{experts}][{need} bytes] (got {tuple(w_fp8.shape)})")
-    if expert.dtype != torch.int32 or (bundle is not None and bundle.dtype != torch.int32):
-        raise ValueError("expert and bundle must be int32")
+    i32 = torch.int32
+    if expert.dtype != i32 or (bundle is not None and bundle.dtype != i32) or (status is not None and status.dtype != i32):
+        raise ValueError("expert, bundle and status must be int32")
     _check(_lib.ckks_experts_mac_fp8(
         ctx.handle, _ptr(w_fp8, "w_fp8", experts * need, _words(w_fp8)), experts, _ptr(expert, "expert", count * 4, 4),
         _ptr(bundle, "bundle", count * 4, 4, True), count, _ptr(ct_in, "ct_in", bundles * d_in * ct_words * 4, 4), bundles,

@@ -399,6 +399,22 @@ def test_refusals(gpu_lib):
         ck.ckks_fp8_weight_bytes(ctx, d_out, d_in, 3)
 
 
+@gpu
+def test_counts_of_other_types_are_refused(gpu_lib):
+    """Four bytes wide, but no int32: a float would hold the count's bits, not the count."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 1)
+    codes, scales = layer(565, 8, 32)
+    with pytest.raises(ValueError, match="bad must be int32"):
+        encode(ck, ctx, codes, scales, 128, 1, 2.0 ** 30, torch.zeros(1, device="cuda"))
+    enc = encode(ck, ctx, codes, scales, 128, 1, 2.0 ** 30).view(1, -1)
+    ct, out = ck.empty_u32((1, 32, 2, 1, ctx.n)), ck.empty_u32((1, 8, 2, 1, ctx.n))
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="status must be int32"):
+        ck.ckks_experts_mac_fp8(ctx, enc, one, one, ct, out, 8, 32, 1, torch.zeros(1, device="cuda"))
+
+
 def test_null_context_is_rejected_without_a_gpu():
     import paper_2606_17421_amd as ck
     lib, bad = ck._lib, ck.CKKS_E_INVALID_ARG
