@@ -231,8 +231,9 @@ int ckks_linear_mac_q4(const ckks_ctx* ctx, const void* w_q4, const uint32_t* ct
  * w[j][i] = scales[j / block_rows][i / 128] f[j][i].  The plaintext of a weight is
  * rint(64 f) rint(scales * scale / 64), rint rounding half to even: the block's scale
  * is rounded once, and f to a multiple of 2^-6, which is exact for |f| >= 1/8 and
- * within 2^-7 below (2^-16 of the largest e4m3 number, 448).  The rounded scale is off by at most
- * 32 / (|scales| scale) relative to itself, so `scale` should be large against 1 / |scales|.
+ * within 2^-7 below (2^-15.8 of the largest e4m3 number, 448).  That is little for outputs of like sizes, and much for
+ * one whose weights are all small beside its block's largest; ckks_linear_encode_fp8_units keeps those.  The rounded scale is off
+ * by at most 32 / (|scales| scale) relative to itself, so `scale` should be large against 1 / |scales|.
  *
  * Encoded weights take 2 bytes a weight and 12 limbs bytes a row and 128 inputs, with rows and inputs
  * padded to multiples of 32, against the 4 limbs bytes a weight of ckks_linear_encode_scalar. */
@@ -253,6 +254,19 @@ size_t ckks_fp8_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in,
  * Run once per layer. */
 int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
                            uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream);
+
+/* The same with a unit for every output and 128 inputs instead of 64ths throughout, for layers whose outputs differ
+ * in size within a scale's block: the plaintext of a weight is rint(u f) rint(scales * scale / u), u the largest of 64, 128,
+ * 256 and 512 with |u f| <= 28672 for all 128 weights of that output.  A weight is off by at most 2^-14.8 of the
+ * largest of its own 128, and not at all where that one is 56 or less (512ths are e4m3's steps).  In a block whose
+ * rows' sizes spread over 1 : 10^3 ckks_linear_encode_fp8 leaves the smallest row 3% off, this one 0.07% at a
+ * `scale` of 2^31 and weights of 0.02.  A rounded scale is off by at most u / (2 |scales| scale) relative to itself, so
+ * outputs in 512ths ask for a `scale` eight times as large.  The products cost the same.
+ *   bad      as above, a scale counting that rounds to zero in 512ths.
+ *   rounded  device int32 [1], 4-byte aligned, or NULL: the number of weights that are not kept exactly. */
+int ckks_linear_encode_fp8_units(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                                 uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad,
+                                 int32_t* rounded, void* stream);
 
 /* ct x pt MAC with 8-bit weights:  ct_out[j][c][l][k] = sum_i rint(64 f[j][i])
  * rint(scales * scale / 64) ct_in[i][c][l][k] mod q_l, as ckks_linear_mac_scalar over

@@ -40,14 +40,41 @@ def plaintexts(codes, scales, block_rows: int, scale: float) -> np.ndarray:
     return v.astype(object) * s[row][:, col]
 
 
+def units(codes) -> np.ndarray:
+    """The largest u of 64, 128, 256 and 512 with |u f| <= 28672 for all weights of a row and block (d_out, blocks)."""
+    f = np.abs(np.nan_to_num(numbers(codes), nan=0.0))
+    top = np.stack([f[:, b:b + BLOCK].max(axis=1) for b in range(0, f.shape[1], BLOCK)], axis=1)
+    return np.select([u * top <= 28672 for u in (512, 256, 128)], [512, 256, 128], 64)
+
+
+def plaintexts_in_units(codes, scales, block_rows: int, scale: float) -> np.ndarray:
+    """The integers rint(u f) rint(scales * scale / u); zero as in plaintexts, and where a scale rounds to zero for u = 512."""
+    f = np.nan_to_num(numbers(codes), nan=0.0)
+    row, col = np.arange(f.shape[0]) // block_rows, np.arange(f.shape[1]) // BLOCK
+    s = np.asarray(scales, np.float32).astype(np.float64)
+    s = np.where(np.isfinite(s), s, 0.0) * scale
+    s = np.where((abs(s / 64) < 2.0 ** 63) & (np.rint(s / 512) != 0), s, 0.0)[row][:, col]
+    u = units(codes)[:, col]
+    v, whole = np.rint(u * f).astype(np.int64), np.rint(s / u)
+    return v.astype(object) * np.vectorize(int, otypes=[object])(whole)
+
+
+def rounded(codes) -> int:
+    """How many weights plaintexts_in_units does not keep."""
+    f = np.nan_to_num(numbers(codes), nan=0.0)
+    x = units(codes)[:, np.arange(f.shape[1]) // BLOCK] * f
+    return int((x != np.rint(x)).sum())
+
+
 def residues(p, qs) -> np.ndarray:
     """Integers (d_out, d_in) -> uint64 (d_out, d_in, L)."""
     return np.stack([(p % int(q)).astype(np.uint64) for q in qs], axis=-1)
 
 
-def mac(codes, scales, ct, block_rows: int, scale: float, qs, rows=None) -> np.ndarray:
+def mac(codes, scales, ct, block_rows: int, scale: float, qs, rows=None, in_units: bool = False) -> np.ndarray:
     """ct (d_in, 2, L, N) residues -> (len(rows), 2, L, N)."""
-    return mac_scalar(residues(plaintexts(codes, scales, block_rows, scale), qs), ct, qs, rows=rows)
+    integers = plaintexts_in_units if in_units else plaintexts
+    return mac_scalar(residues(integers(codes, scales, block_rows, scale), qs), ct, qs, rows=rows)
 
 
 def combine(gates, y, terms, qs) -> np.ndarray:

@@ -82,6 +82,7 @@ _SIGS = {
     "ckks_linear_mac_q4": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _i32, _vp]),
     "ckks_fp8_weight_bytes": (_sz, [_vp, _u32, _u32, _u32]),
     "ckks_linear_encode_fp8": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _u32, _dbl, _vp, _vp, _vp]),
+    "ckks_linear_encode_fp8_units": (_i32, [_vp, _vp, _vp, _u32, _u32, _u32, _u32, _dbl, _vp, _vp, _vp, _vp]),
     "ckks_linear_mac_fp8": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "ckks_experts_mac_fp8": (_i32, [_vp, _vp, _u32, _vp, _vp, _u32, _vp, _u32, _vp, _u32, _u32, _u32, _vp, _vp]),
     "ckks_experts_combine": (_i32, [_vp, _vp, _vp, _u32, _vp, _u32, _u32, _vp, _u32, _u32, _vp]),
@@ -407,9 +408,7 @@ def _words(t) -> int:
     return t.element_size() if t is not None else 1
 
 
-def ckks_linear_encode_fp8(ctx: Context, w8, scales, d_out: int, d_in: int, block_rows: int, limbs: int, scale: float,
-                           w_fp8, bad=None, stream=None) -> None:
-    """w8: e4m3 weights, as torch.float8_e4m3fn or their codes as uint8; scales float32; bad int32 [1] or None."""
+def _encode_fp8_args(ctx, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, **counts):
     need = ckks_fp8_weight_bytes(ctx, d_out, d_in, limbs)
     if block_rows < 1:
         raise ValueError("block_rows must be positive")
@@ -417,13 +416,26 @@ def ckks_linear_encode_fp8(ctx: Context, w8, scales, d_out: int, d_in: int, bloc
         raise ValueError(f"w8 must be float8_e4m3fn or its codes as uint8 (got {w8.dtype})")
     if scales is not None and scales.dtype != torch.float32:
         raise ValueError(f"scales must be float32 (got {scales.dtype})")
-    if bad is not None and bad.dtype != torch.int32:
-        raise ValueError(f"bad must be int32 (got {bad.dtype})")
+    for name, t in counts.items():
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError(f"{name} must be int32 (got {t.dtype})")
     blocks = -(-d_out // block_rows) * -(-d_in // 128)
-    _check(_lib.ckks_linear_encode_fp8(
-        ctx.handle, _ptr(w8, "w8", d_out * d_in, 1), _ptr(scales, "scales", blocks * 4, 4), d_out, d_in, block_rows, limbs,
-        float(scale), _ptr(w_fp8, "w_fp8", need, _words(w_fp8)), _ptr(bad, "bad", 4, 4, True), _stream(stream)),
-        "ckks_linear_encode_fp8")
+    return (ctx.handle, _ptr(w8, "w8", d_out * d_in, 1), _ptr(scales, "scales", blocks * 4, 4), d_out, d_in, block_rows, limbs,
+            float(scale), _ptr(w_fp8, "w_fp8", need, _words(w_fp8)), *(_ptr(t, name, 4, 4, True) for name, t in counts.items()))
+
+
+def ckks_linear_encode_fp8(ctx: Context, w8, scales, d_out: int, d_in: int, block_rows: int, limbs: int, scale: float,
+                           w_fp8, bad=None, stream=None) -> None:
+    """w8: e4m3 weights, as torch.float8_e4m3fn or their codes as uint8; scales float32; bad int32 [1] or None."""
+    args = _encode_fp8_args(ctx, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad=bad)
+    _check(_lib.ckks_linear_encode_fp8(*args, _stream(stream)), "ckks_linear_encode_fp8")
+
+
+def ckks_linear_encode_fp8_units(ctx: Context, w8, scales, d_out: int, d_in: int, block_rows: int, limbs: int, scale: float,
+                                 w_fp8, bad=None, rounded=None, stream=None) -> None:
+    """ckks_linear_encode_fp8 with a unit for each output and 128 inputs; rounded int32 [1] or None."""
+    args = _encode_fp8_args(ctx, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad=bad, rounded=rounded)
+    _check(_lib.ckks_linear_encode_fp8_units(*args, _stream(stream)), "ckks_linear_encode_fp8_units")
 
 
 def ckks_linear_mac_fp8(ctx: Context, w_fp8, ct_in, ct_out, d_out: int, d_in: int, limbs: int, stream=None) -> None:

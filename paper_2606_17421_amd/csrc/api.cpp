@@ -900,8 +900,9 @@ size_t ckks_fp8_weight_bytes(const ckks_ctx* ctx, uint32_t d_out, uint32_t d_in,
   return ckks::fp8_weight_bytes(d_out, d_in, limbs);
 }
 
-int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
-                           uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream) {
+static int encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                      uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, bool units,
+                      int32_t* rounded, void* stream) {
   if (int rc = check_ctx(ctx)) return rc;
   if (int rc = check_limbs(ctx, limbs, 1)) return rc;
   if (int rc = check_mac_shapes(d_out, d_in)) return rc;
@@ -909,21 +910,36 @@ int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* 
   if (!(scale > 0.0) || !std::isfinite(scale)) return fail(CKKS_E_INVALID_ARG, "scale must be finite and > 0");
   if (bad)
     if (int rc = check_list(bad, "bad")) return rc;
+  if (rounded)
+    if (int rc = check_list(rounded, "rounded")) return rc;
   DeviceGuard guard(ctx->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (d_out == 0 || d_in == 0) {  // nothing is bad in an empty layer
+  if (d_out == 0 || d_in == 0) {  // nothing is bad or rounded in an empty layer
+    if (int rc = check_writes({{bad, 4, "bad"}, {rounded, 4, "rounded"}}, {})) return rc;
     hipError_t e = bad ? ckks::launch_zero(reinterpret_cast<uint32_t*>(bad), 1, s) : hipSuccess;
+    if (e == hipSuccess && rounded) e = ckks::launch_zero(reinterpret_cast<uint32_t*>(rounded), 1, s);
     return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
   }
   if (!w8) return fail(CKKS_E_INVALID_ARG, "w8 is null");
   if (int rc = check_list(scales, "scales")) return rc;
   if (int rc = check_ptr(w_fp8, "w_fp8")) return rc;
   const size_t scale_count = ((size_t(d_out) - 1) / block_rows + 1) * ((size_t(d_in) + 127) / 128);
-  if (int rc = check_writes({{w_fp8, ckks::fp8_weight_bytes(d_out, d_in, limbs), "w_fp8"}, {bad, 4, "bad"}},
+  if (int rc = check_writes({{w_fp8, ckks::fp8_weight_bytes(d_out, d_in, limbs), "w_fp8"}, {bad, 4, "bad"}, {rounded, 4, "rounded"}},
                             {{w8, size_t(d_out) * d_in, "w8"}, {scales, scale_count * 4, "scales"}}))
     return rc;
-  hipError_t e = ckks::launch_encode_fp8(ctx->t, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad, s);
+  hipError_t e = ckks::launch_encode_fp8(ctx->t, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad, units, rounded, s);
   return e == hipSuccess ? ok() : hip_fail(e, "encode_fp8 launch");
+}
+
+int ckks_linear_encode_fp8(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                           uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, void* stream) {
+  return encode_fp8(ctx, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad, false, nullptr, stream);
+}
+
+int ckks_linear_encode_fp8_units(const ckks_ctx* ctx, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
+                                 uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad,
+                                 int32_t* rounded, void* stream) {
+  return encode_fp8(ctx, w8, scales, d_out, d_in, block_rows, limbs, scale, w_fp8, bad, true, rounded, stream);
 }
 
 int ckks_linear_mac_fp8(const ckks_ctx* ctx, const void* w_fp8, const uint32_t* ct_in, uint32_t* ct_out, uint32_t d_out,

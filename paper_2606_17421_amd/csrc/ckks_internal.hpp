@@ -212,7 +212,8 @@ constexpr int32_t kExpertOk = 0, kExpertBadRequest = 1;
 constexpr uint32_t kMaxRequests = 65536;
 size_t fp8_weight_bytes(uint32_t d_out, uint32_t d_in, uint32_t limbs);
 hipError_t launch_encode_fp8(const Tables& t, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
-                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, hipStream_t s);
+                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, bool units,
+                             int32_t* rounded, hipStream_t s);
 hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, const int32_t* expert,
                           const int32_t* bundle, uint32_t count, const uint32_t* ct_in, uint32_t bundles, uint32_t* ct_out,
                           uint32_t d_out, uint32_t d_in, uint32_t limbs, int32_t* status, hipStream_t s);

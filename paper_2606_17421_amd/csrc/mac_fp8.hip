@@ -7,7 +7,9 @@
 //     T[j][b][col] = sum over the 128 inputs of v[j][i] x[i][col].
 // |v| <= 64 * 448 = 28672 is two balanced base-256 digits, the same for every limb, against the
 // residues' four: eight int8 products a modular MAC.  Every step of e4m3 (2^-9) would take three
-// digits and twelve; what the rounding to 64ths costs is 2^-7 at most of a weight below 1/8, 2^-16 of the largest one.
+// digits and twelve; what the rounding to 64ths costs is 2^-7 at most of a weight below 1/8, 2^-15.8 of the largest one.
+// With a unit for each row and block, v = rint(u f) and S = rint(scale Delta / u) for u up to 512, the two digits keep rows that
+// are small beside their block's largest as well; the constants are a row's anyway, so the kernels are the same.
 // T = a + 2^16 b + 2^32 c with a and b from two digit sums each and c from one; a block's scale enters
 // in 64-bit integers, and the sum over the blocks is reduced once an output.
 //
@@ -67,18 +69,45 @@ Shape shape_of(uint32_t d_out, uint32_t d_in, uint32_t limbs) {
   return s;
 }
 
-// rint(64 f) of an e4m3 code, half to even.  A code is a sign, four bits of exponent and three of
+// rint(64 2^fine f) of an e4m3 code, half to even, fine at most 3.  A code is a sign, four bits of exponent and three of
 // mantissa; 512 f is a whole number.  NaN (all of exponent and mantissa set) counts as 0.
-__device__ __forceinline__ int32_t units_of(uint32_t code, bool* nan) {
+__device__ __forceinline__ int32_t units_of(uint32_t code, uint32_t fine, bool* nan, bool* rounded) {
   const uint32_t e = code >> 3 & 15, m = code & 7;
   const uint32_t u = e == 0 ? m : (8 + m) << (e - 1);  // 512 |f|
-  const int32_t v = static_cast<int32_t>((u + 3 + (u >> 3 & 1)) >> 3);
+  const uint32_t drop = 3 - fine, half = (1u << drop) >> 1;
+  const int32_t v = static_cast<int32_t>((u + half - (half != 0 && (u >> drop & 1) == 0)) >> drop);
   *nan = (code & 0x7f) == 0x7f;
+  *rounded = !*nan && (u & ((1u << drop) - 1)) != 0;
   return *nan ? 0 : code & 0x80 ? -v : v;
 }
 
+// The finest unit that two digits hold for all weights of a row and block, 2^-6-fine with 64 2^fine |f| <= 28672, into the
+// places of the constants that fp8_scale_kernel replaces, of every limb.  The size of a number goes with its code.  A lane
+// reads a row's 128 codes one by one: 1024 -> 6144 at 8 limbs takes 41 us encoded so and 20 in 64ths, once a layer.
+__global__ __launch_bounds__(kThreads) void fp8_unit_kernel(const uint8_t* __restrict__ w8, uint32_t d_out, uint32_t d_in,
+                                                            uint32_t blocks, uint32_t tiles, uint32_t limbs, size_t total,
+                                                            size_t group0, int32_t* __restrict__ out) {
+  const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;  // [tile][block][32]
+  if (idx >= total) return;
+  const size_t tb = idx >> 5;
+  const uint32_t block = static_cast<uint32_t>(tb % blocks), row = static_cast<uint32_t>(tb / blocks) * 32 + (idx & 31);
+  uint32_t most = 0;
+  if (row < d_out) {
+    const uint8_t* w = w8 + static_cast<size_t>(row) * d_in;
+    for (uint32_t k = block * kBlock; k < min(d_in, (block + 1) * kBlock); ++k) {
+      const uint32_t size = w[k] & 0x7f;
+      most = max(most, size == 0x7f ? 0 : size);
+    }
+  }
+  const int32_t fine = (most <= 0x66) + (most <= 0x6e) + (most <= 0x76);  // 56, 112 and 224
+  for (uint32_t l = 0; l < limbs; ++l) out[(static_cast<size_t>(l) * tiles * blocks + tb) * 96 + (idx & 31)] = fine;
+}
+
+// With kUnits by what fp8_unit_kernel wrote, else 64ths throughout.
+template <bool kUnits>
 __global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __restrict__ w8, uint32_t d_out, uint32_t d_in,
-                                                            uint32_t steps, size_t lanes, size_t group0, int32_t* bad,
+                                                            uint32_t steps, size_t lanes, size_t group0,
+                                                            const int32_t* __restrict__ units, int32_t* bad, int32_t* rounded,
                                                             v4i* __restrict__ frag) {
   const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;
   if (idx >= lanes) return;
@@ -86,17 +115,20 @@ __global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __res
   const uint32_t step = static_cast<uint32_t>((idx >> 6) % steps), tile = static_cast<uint32_t>((idx >> 6) / steps);
   const uint32_t row = tile * 32 + (lane & 31), k0 = step * kStep + 16 * (lane >> 5);
   const uint8_t* w = w8 + static_cast<size_t>(row) * d_in;
+  const uint32_t blocks = (steps + kBlockSteps - 1) / kBlockSteps;
+  const uint32_t fine = kUnits ? units[(static_cast<size_t>(tile) * blocks + step / kBlockSteps) * 96 + (lane & 31)] : 0;
   v4i f[kDigits];
-  int32_t nans = 0;
+  int32_t nans = 0, off = 0;
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
     uint32_t lo = 0, hi = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t k = k0 + 4 * d + e;
-      bool nan = false;
-      const int32_t v = row < d_out && k < d_in ? units_of(w[k], &nan) : 0;
+      bool nan = false, moved = false;
+      const int32_t v = row < d_out && k < d_in ? units_of(w[k], fine, &nan, &moved) : 0;
       nans += nan;
+      if (kUnits) off += moved;
       const uint32_t b = (static_cast<uint32_t>(v) + 0x8080u) ^ 0x8080u;  // its low two bytes, as int8, are the digits
       lo |= (b & 0xffu) << (8 * e);
       hi |= (b >> 8 & 0xffu) << (8 * e);
@@ -105,14 +137,16 @@ __global__ __launch_bounds__(kThreads) void fp8_frag_kernel(const uint8_t* __res
     f[1][d] = static_cast<int>(hi);
   }
   if (bad && nans) atomicAdd(bad, nans);
+  if (kUnits && rounded && off) atomicAdd(rounded, off);
 #pragma unroll
   for (int d = 0; d < kDigits; ++d) frag[((idx >> 6) * kDigits + d) * 64 + lane] = f[d];
 }
 
+template <bool kUnits>
 __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const float* __restrict__ scales, uint32_t d_out,
                                                              uint32_t block_rows, uint32_t blocks, uint32_t tiles,
-                                                             size_t total, size_t group0, double scale, int32_t* bad,
-                                                             int32_t* __restrict__ out) {
+                                                             size_t total, size_t group0, double scale,
+                                                             int32_t* bad, int32_t* __restrict__ out) {
   const size_t idx = (group0 + blockIdx.x) * kThreads + threadIdx.x;  // [limb][tile][block][32]
   if (idx >= total) return;
   const uint32_t block = static_cast<uint32_t>((idx >> 5) % blocks);
@@ -124,11 +158,10 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
   if (row < d_out) {
     const float s = scales[static_cast<size_t>(row / block_rows) * blocks + block];
     const double v = static_cast<double>(s) * scale;
-    const double whole = rint(v);
-    const bool fine = fabs(v) < 9223372036854775808.0;  // 2^63; no infinity and no NaN
-    if (fine) r = reduce_f64_int(whole, q, tb.q_recip[l]);
-    const bool lost = whole == 0 && v != 0;  // a scale too small for `scale` takes its block's weights with it
-    if (bad && (!fine || lost) && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
+    // no infinity and no NaN; and a scale too small for `scale`, in its finest unit, takes its block's weights with it
+    const bool fine = fabs(v) < 9223372036854775808.0 && (v == 0 || rint(kUnits ? v / 8 : v) != 0);
+    if (fine) r = reduce_f64_int(rint(kUnits ? ldexp(v, -out[(idx >> 5) * 96 + (idx & 31)]) : v), q, tb.q_recip[l]);
+    if (bad && !fine && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
   }
 #pragma unroll
   for (int d = 0; d < 3; ++d) {
@@ -912,20 +945,31 @@ size_t fp8_weight_bytes(uint32_t d_out, uint32_t d_in, uint32_t limbs) {
 }
 
 hipError_t launch_encode_fp8(const Tables& t, const uint8_t* w8, const float* scales, uint32_t d_out, uint32_t d_in,
-                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, hipStream_t s) {
+                             uint32_t block_rows, uint32_t limbs, double scale, void* w_fp8, int32_t* bad, bool units,
+                             int32_t* rounded, hipStream_t s) {
   const Shape sh = shape_of(d_out, d_in, limbs);
   uint8_t* base = static_cast<uint8_t*>(w_fp8);
-  if (bad)
-    if (hipError_t e = launch_zero(reinterpret_cast<uint32_t*>(bad), 1, s); e != hipSuccess) return e;
+  int32_t* constants = reinterpret_cast<int32_t*>(base + sh.frag_bytes);
+  for (int32_t* count : {bad, rounded})
+    if (count)
+      if (hipError_t e = launch_zero(reinterpret_cast<uint32_t*>(count), 1, s); e != hipSuccess) return e;
+  if (units) {
+    const size_t total = static_cast<size_t>(sh.tiles) * sh.blocks * 32;
+    hipError_t e = in_pieces((total + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
+      fp8_unit_kernel<<<groups, kThreads, 0, s>>>(w8, d_out, d_in, sh.blocks, sh.tiles, limbs, total, first, constants);
+    });
+    if (e != hipSuccess) return e;
+  }
   const size_t lanes = static_cast<size_t>(sh.tiles) * sh.steps * 64;
+  const auto frag = units ? fp8_frag_kernel<true> : fp8_frag_kernel<false>;
   hipError_t e = in_pieces((lanes + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
-    fp8_frag_kernel<<<groups, kThreads, 0, s>>>(w8, d_out, d_in, sh.steps, lanes, first, bad, reinterpret_cast<v4i*>(base));
+    frag<<<groups, kThreads, 0, s>>>(w8, d_out, d_in, sh.steps, lanes, first, constants, bad, rounded, reinterpret_cast<v4i*>(base));
   });
   if (e != hipSuccess) return e;
   const size_t total = static_cast<size_t>(limbs) * sh.tiles * sh.blocks * 32;
+  const auto constant = units ? fp8_scale_kernel<true> : fp8_scale_kernel<false>;
   return in_pieces((total + kThreads - 1) / kThreads, [&](uint64_t first, uint32_t groups) {
-    fp8_scale_kernel<<<groups, kThreads, 0, s>>>(t, scales, d_out, block_rows, sh.blocks, sh.tiles, total, first, scale / 64,
-                                                 bad, reinterpret_cast<int32_t*>(base + sh.frag_bytes));
+    constant<<<groups, kThreads, 0, s>>>(t, scales, d_out, block_rows, sh.blocks, sh.tiles, total, first, scale / 64, bad, constants);
   });
 }
 

@@ -42,6 +42,35 @@ def test_distance_to_the_weights():
     assert far[np.abs(f) >= 0.125].max() == 0 and far.max() == 2.0 ** -7
 
 
+def test_a_written_out_layer_in_units():
+    # rows whose largest are 56, 60, 120, 240 and 0: units 512, 256, 128, 64 and 512; 5/512 beside each
+    codes = np.array([[0x66, 0x05], [0x67, 0x05], [0x6F, 0x05], [0x77, 0x85], [0x7F, 0x80]], np.uint8)
+    assert fp8.numbers(codes)[:4, 0].tolist() == [56, 60, 120, 240]
+    assert fp8.units(codes)[:, 0].tolist() == [512, 256, 128, 64, 512]
+    p = fp8.plaintexts_in_units(codes, np.array([[1.0]], np.float32), 128, 512.0 * 3)
+    # 2.5 of 256ths and 1.25, 0.625 of the coarser ones round to 2, 1 and 1
+    assert p.tolist() == [[28672 * 3, 5 * 3], [15360 * 6, 2 * 6], [15360 * 12, 12], [15360 * 24, -24], [0, 0]]
+    assert fp8.rounded(codes) == 3
+
+
+def test_scales_that_vanish_in_512ths_are_zero():
+    codes = np.array([[0x38], [0x7E]], np.uint8)
+    for size, want in ((256.0, [0, 0]), (257.0, [512, 28672 * 4])):
+        assert fp8.plaintexts_in_units(codes, np.array([[1.0]], np.float32), 128, size)[:, 0].tolist() == want
+
+
+def test_distance_to_small_rows():
+    """Each weight within 1 / 28672 of its row's largest, whatever else is in the block, and kept where that is up to 56."""
+    rng = np.random.default_rng(6)
+    f = rng.normal(0, 100, (128, 128)) * np.geomspace(1, 1e-4, 128)[:, None]
+    import torch
+    codes = torch.from_numpy(f).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    f, u = fp8.numbers(codes), fp8.units(codes)
+    top = np.abs(f).max(axis=1, keepdims=True)
+    far = np.abs(np.rint(u * f) / u - f)
+    assert np.all(far <= top / 28672) and np.all(far[top[:, 0] <= 56] == 0) and set(u[:, 0]) == {64, 128, 256, 512}
+
+
 @pytest.mark.parametrize("block_rows", [1, 3, 128])
 def test_mac_is_the_scalar_mac_where_the_scales_are_exact(block_rows):
     rng = np.random.default_rng(4)
