@@ -8,7 +8,8 @@ each expert that any of its tokens has, as one request, and the requests of all
 experts are one call over e4m3 weights with a scale a block.  The outputs are
 rescaled and summed for each bundle, every expert's times the encoded gates of
 its slots (zero for tokens that are not its own), rescaled again, decrypted
-and compared with the layer in floating point.
+and compared with the layer in floating point: over the weights that are encoded, within the
+noise, and over the quantised weights, scales times e4m3 numbers, within that and the encoding's rounding.
 """
 from __future__ import annotations
 
@@ -28,14 +29,18 @@ BLOCK_ROWS, BLOCK, LARGEST = 32, 128, 448.0
 
 
 def quantise(w):
-    """Block-maximum quantisation to e4m3: (weights, scales, the weights that the encoded layer stands for)."""
+    """Block-maximum quantisation to e4m3: (weights, scales, the weights that the encoded layer stands for, the quantised
+    weights, how far the two may be apart)."""
     d_out, d_in = w.shape
     row, col = np.arange(d_out) // BLOCK_ROWS, np.arange(d_in) // BLOCK
     scales = np.zeros((row[-1] + 1, col[-1] + 1), np.float32)
     np.maximum.at(scales, (row[:, None], col[None, :]), (np.abs(w) / LARGEST).astype(np.float32))
     w8 = torch.from_numpy(w / scales[row][:, col]).clamp(-LARGEST, LARGEST).to(torch.float8_e4m3fn)
-    units = np.rint(64 * w8.to(torch.float64).numpy()) * np.rint(scales.astype(np.float64) * (SCALE_W / 64))[row][:, col]
-    return w8, scales, units / SCALE_W
+    f, s = w8.to(torch.float64).numpy(), scales.astype(np.float64)[row][:, col]
+    units = np.rint(64 * f) * np.rint(s * (SCALE_W / 64))
+    # a number is a multiple of 1/64 from 1/8 on, and a scale is rounded to a multiple of 64 / SCALE_W
+    apart = np.where(np.abs(f) < 0.125, s / 128, 0) + np.abs(np.rint(64 * f)) / (2 * SCALE_W)
+    return w8, scales, units / SCALE_W, s * f, apart
 
 
 def slots_of(residues, q, scale, n):
@@ -58,13 +63,15 @@ def main(seed: int = 0) -> dict:
     s = rng.integers(-1, 2, n)
     s_ntt = ck.to_device(np.stack([np.mod(s, p) for p in q]).astype(np.uint32))
     ck.ckks_ntt(ctx, s_ntt, 1, LIMBS)
-    bad, weights = ints([0]), []
+    bad, weights, quantised, apart = ints([0]), [], [], []
     w_fp8 = ck.empty_workspace(EXPERTS * ck.ckks_fp8_weight_bytes(ctx, D_OUT, D_IN, LIMBS)).view(EXPERTS, -1)
     for e in range(EXPERTS):
-        w8, scales, w = quantise(rng.normal(0, 0.02, (D_OUT, D_IN)))
+        w8, scales, w, sf, far = quantise(rng.normal(0, 0.02, (D_OUT, D_IN)))
         ck.ckks_linear_encode_fp8(ctx, w8.cuda(), ck.to_device(scales), D_OUT, D_IN, BLOCK_ROWS, LIMBS, SCALE_W, w_fp8[e], bad)
         assert int(bad) == 0
         weights.append(w)
+        quantised.append(sf)
+        apart.append(far)
 
     # two bundles of tokens; their gates: two experts a token, of the second bundle's tokens none the last
     x = rng.uniform(-1, 1, (BUNDLES, D_IN, n // 2))
@@ -121,8 +128,13 @@ def main(seed: int = 0) -> dict:
     var = ((gates ** 2)[:, :, None] * var_each[None]).sum(axis=1) + rescale / scale_z ** 2
     var = var + (each ** 2).sum(axis=1) * n / 24 / SCALE_G ** 2
     off = np.abs(got - want)
+    # against the quantised weights: six standard deviations and the encoding's rounding, |x| <= 1
+    layer = np.stack([(np.stack([sf @ x[b] for sf in quantised]) * gates[b][:, None]).sum(axis=0) for b in range(BUNDLES)])
+    rounding = np.stack([(np.stack([far.sum(axis=1) for far in apart])[:, :, None] * gates[b][:, None]).sum(axis=0) for b in range(BUNDLES)])
+    from_layer = np.abs(got - layer) / (6 * np.sqrt(var) + rounding)
     result = {"requests": len(requests), "status": status.tolist(), "largest": float(np.abs(want).max()),
-              "worst_error": float(off.max()), "worst_over_sd": float((off / np.sqrt(var)).max())}
+              "worst_error": float(off.max()), "worst_over_sd": float((off / np.sqrt(var)).max()),
+              "worst_from_layer": float(from_layer.max()), "largest_rounding": float(rounding.max())}
     ctx.close()
     return result
 
