@@ -129,6 +129,24 @@ def test_row_tiles_and_passes(gpu_lib, d_out, d_in):
 
 
 @gpu
+@pytest.mark.parametrize("d_out,d_in", [(290, 40), (380, 40), (380, 250), (512, 250), (290, 512), (420, 512), (290, 1000), (380, 1000),
+                                        (420, 1000), (530, 1024), (380, 1100), (290, 1280), (64, 300), (160, 1100)])
+def test_every_row_tile_and_column_wave(gpu_lib, d_out, d_in):
+    """The first and the last row of every row tile, at columns of each of the four waves that are next to each other: a tile or
+    strip that was taken for another one gives residues in range, which only its own rows and columns show."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, MANY)
+    codes, scales = layer(498 + d_in + d_out, d_out, d_in)
+    ct = gen.uniform_residues(np.random.default_rng(499 + d_in), (d_in, 2), ctx.moduli, ctx.n)
+    got = ck.to_host_u32(run(ck, ctx, codes, scales, ct, 128, 2.0 ** 30))
+    rows = sorted({min(r, d_out - 1) for t in range(0, d_out, 32) for r in (t, t + 31)})
+    cols = [3, 38, 75, 127, 130, 161, 192, 255, 515, 550, 580, 639, 897, 930, 975, 1020]
+    of_rows = scales[np.array(rows) // 128]
+    want = OF.mac(codes[rows], of_rows, ct[..., cols], 1, 2.0 ** 30, ctx.moduli).astype(np.uint32)
+    assert np.array_equal(got[rows][..., cols], want)
+
+
+@gpu
 @pytest.mark.parametrize("log_n,limbs", [(10, 1), (10, 3), (11, 2), (12, 2)])
 @pytest.mark.parametrize("d_out,d_in", [(9, 1500), (33, 700), (200, 130), (700, 300), (900, 900), (1100, 1100), (1500, 40)])
 def test_few_columns(gpu_lib, log_n, limbs, d_out, d_in):
