@@ -540,6 +540,8 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
   Weights<kForm> w;
 #pragma unroll
   for (uint32_t s = 0; s < kBlockSteps; ++s)
+    // Always so, a layer of one block has its own kernel; but a branch keeps the compiler from mixing the steps' loads (1000 -> 8 at
+    // 2^14 and 4 limbs: 92.0 us with it, 94.3 without, 94.0 with a scheduling barrier in its place; 300 -> 5: 33.8, 35.1, 34.1).
     if (s == 0 || s < steps) {
       fetch_step(tb, a, job.src, (begin * kBlockSteps + s) * kStep, x[s]);
       w.load_step(src, begin, s);
@@ -714,7 +716,7 @@ __global__ __launch_bounds__(512, 2) void mac_fp8_chunked_kernel(Tables tb, Laye
 //
 // The row tiles that are no multiple of kWaves come first.  Where they are at most half of it (and others
 // follow) two waves take a tile's chunks half and half and their sums meet in LDS.
-// Four waves have at most kFewBlocks blocks, which are never folded.
+// Four waves have at most kFewBlocks blocks, eight at most kFoldBlocks, so the sums need no reduction on the way.
 template <int kWaves, bool kTwice>
 __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb, Layers a, uint32_t splits, uint32_t jobs) {
   constexpr int kPasses = kChunk / kWaves;
@@ -756,7 +758,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
   __syncthreads();
   for (bool going = true; going;) {
     const Modulus q = modulus(tb.q[job.limb]);
-    const int32_t c32 = centred(tb.pow256[job.limb * 8 + 4], q.q);
     Job after = job;
     if (kTwice) going = seek(&after);
     const uint32_t wanted = kTwice && going ? pieces : 0;
@@ -788,7 +789,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mac_fp8_whole_kernel(Tables tb
           if (placed < fetched) place_piece();
           if (fetched < wanted) fetch_piece();
         }
-        if (kWaves == 8 && c != begin && g0 % kFoldBlocks == 0) fold(q, c32, acc);
         read(f, x);
         contract(f, max(my_steps, s0) - s0, f + kBlockSteps * kStepFrags, src, g1, blocks, w[0], x, acc);
         if (!kTwice && kPasses == 2 && last) {
@@ -880,8 +880,8 @@ hipError_t launch_whole(const Tables& t, const Layers& a, uint64_t strips, uint3
   const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>(jobs, t.num_cus * (8 / kWaves)));
   const size_t strip = strip_bytes(a.sh), sums = kWaves * kWaveSums;
   const uint32_t n = static_cast<uint32_t>(jobs);
+  if (a.sh.blocks > (kWaves == 4 ? kFewBlocks : kFoldBlocks)) return hipErrorInvalidConfiguration;
   if constexpr (kWaves == 4) {
-    if (a.sh.blocks > kFewBlocks) return hipErrorInvalidConfiguration;
     // two workgroups a CU; one strip or two (13 requests of 200 -> 333 at 2^11, 2 limbs, before the shorter reduction: 91 -> 88 us)
     if (2 * (2 * strip + sums) <= kLdsBytes)
       mac_fp8_whole_kernel<4, true><<<grid, 256, 2 * strip + sums, s>>>(t, a, splits, n);
