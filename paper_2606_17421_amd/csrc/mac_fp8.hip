@@ -523,12 +523,11 @@ __device__ __forceinline__ void join(uint32_t (&y)[kN], uint32_t q, v4i* sums, u
 // nothing to wait for but the loads, of which those of four steps are in flight.
 constexpr int kThinWaves = 8;  // of a workgroup, at most
 template <Form kForm>
-__global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices,
-                                                                        uint32_t group0) {
+__global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables tb, Layers a, uint32_t slices) {
   __shared__ v4i sums[kThinWaves * kOuts<kForm> * 16];
   Job job;
   const uint32_t waves = blockDim.x / 64, strips = waves / slices;
-  if (!place_of(tb, a, strips * 32, a.sh.tiles, (group0 + blockIdx.x) >> 3, &job)) return;
+  if (!place_of(tb, a, strips * 32, a.sh.tiles, range_of(gridDim.x).first, &job)) return;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strip = wave % strips, slice = wave / strips;
   const uint32_t blocks = a.sh.blocks, each = (blocks + slices - 1) / slices, steps = a.sh.steps;
   const uint32_t begin = min(blocks, slice * each), end = min(blocks, begin + each);
@@ -586,10 +585,9 @@ __global__ __launch_bounds__(kThinWaves * 64, 2) void mac_fp8_thin_kernel(Tables
 // wait for together (64 -> 256 at 2^14 and 4 limbs: 39 us; as chunks through LDS 72).
 constexpr int kShortWaves = 4;  // of a workgroup, next to each other
 template <int kSteps, Form kForm>
-__global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits,
-                                                                          uint32_t group0) {
+__global__ __launch_bounds__(kShortWaves * 64, 2) void mac_fp8_short_kernel(Tables tb, Layers a, uint32_t splits) {
   Job job;
-  if (!place_of(tb, a, kShortWaves * 32, splits, (group0 + blockIdx.x) >> 3, &job)) return;
+  if (!place_of(tb, a, kShortWaves * 32, splits, range_of(gridDim.x).first, &job)) return;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tiles = a.sh.tiles;
   const uint32_t each = (tiles + splits - 1) / splits, begin = job.split * each, end = min(tiles, begin + each);
   if (begin >= end) return;
@@ -841,26 +839,24 @@ hipError_t launch_thin(const Tables& t, const Layers& a, uint64_t waves, hipStre
   uint32_t slices = 1;  // up to eight waves a CU, as many as run at a time (1024 -> 16 at 2^13, 3 limbs, twelve : six, 48.9 : 42.6 us)
   while (slices < kThinWaves && 2 * slices <= a.sh.blocks && 2 * waves * slices <= t.num_cus * 8ull) slices *= 2;
   const uint32_t group = slices < 4 ? 4 : slices;  // waves of a workgroup
-  const uint64_t grid = waves * slices / group;
+  const uint32_t grid = static_cast<uint32_t>(waves * slices / group);
   const auto k = a.d_out <= kFewRows ? mac_fp8_thin_kernel<kFew> : mac_fp8_thin_kernel<kRows>;
-  return in_pieces(grid, [&](uint64_t first, uint32_t groups) {
-    k<<<groups, group * 64, 0, s>>>(t, a, slices, static_cast<uint32_t>(first));
-  });
+  k<<<grid, group * 64, 0, s>>>(t, a, slices);
+  return hipGetLastError();
 }
 
 hipError_t launch_short(const Tables& t, const Layers& a, uint64_t strips, hipStream_t s) {
   // eight waves a CU where the row tiles allow it
   const uint32_t splits = static_cast<uint32_t>(std::min<uint64_t>(a.sh.tiles, (t.num_cus * 8ull + strips - 1) / strips));
-  const uint64_t grid = strips / kShortWaves * splits;
+  const uint32_t grid = static_cast<uint32_t>(strips / kShortWaves * splits);
   const auto k = a.d_out <= kFewRows ? (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kFew>
                                         : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kFew>
                                                           : mac_fp8_short_kernel<4, kFew>)
                                      : (a.sh.steps == 1   ? mac_fp8_short_kernel<1, kColumns>
                                         : a.sh.steps == 2 ? mac_fp8_short_kernel<2, kColumns>
                                                           : mac_fp8_short_kernel<4, kColumns>);
-  return in_pieces(grid, [&](uint64_t first, uint32_t groups) {
-    k<<<groups, kShortWaves * 64, 0, s>>>(t, a, splits, static_cast<uint32_t>(first));
-  });
+  k<<<grid, kShortWaves * 64, 0, s>>>(t, a, splits);
+  return hipGetLastError();
 }
 
 template <int kColWaves>
@@ -911,9 +907,9 @@ Plan plan_whole(const Tables& t, const Shape& sh, uint64_t strips, uint32_t wave
   return best;
 }
 
-hipError_t launch(const Tables& t, const Layers& a, uint32_t count, hipStream_t s) {
+hipError_t launch(const Tables& t, const Layers& a, hipStream_t s) {
   const Shape& sh = a.sh;
-  const uint64_t strips = static_cast<uint64_t>(count) * a.limbs * (2 * t.n / 32);
+  const uint64_t strips = static_cast<uint64_t>(a.count) * a.limbs * (2 * t.n / 32);
   if (sh.blocks == 1) return launch_short(t, a, strips, s);  // 2^14, 4 limbs, short : thin: 64 -> 256 39 : 72 us
   // No more than 32 outputs, or too few columns for the other kernels.  Thin : the best of the others, us, 2^14, 4 limbs:
   // 256 -> 16 31 : 41, 256 -> 64 48 : 45, 1024 -> 64 150 : 140; 2^10, 2 limbs: 512 -> 128 8.2 : 9.3, 1024 -> 256 16 : 18,
@@ -987,7 +983,24 @@ hipError_t launch_mac_fp8(const Tables& t, const void* w_fp8, uint32_t experts, 
     experts_zero_kernel<<<dim3(64, count < 1024 ? count : 1024), kThreads, 0, s>>>(t, a, count);
     return hipGetLastError();
   }
-  return launch(t, a, count, s);
+  // In pieces of as many requests as the short and the thin kernel have kMostGroups workgroups for, of four column strips and
+  // one share of the row tiles each (of fewer strips, where there are many shares).
+  const uint32_t most = kMostGroups / (limbs * (2 * t.n / 32) / 4);
+  for (uint32_t r = 0; r < count; r += most) {
+    Layers part = a;
+    part.count = count - r < most ? count - r : most;
+    part.ct_out += r * (static_cast<size_t>(2) * limbs * t.n * d_out);
+    if (expert) part.expert += r;
+    if (status) part.status += r;
+    if (bundle) {
+      part.bundle += r;
+    } else {  // a request's own number
+      part.ct_in += r * (static_cast<size_t>(2) * limbs * t.n * d_in);
+      part.bundles = bundles > r ? bundles - r : 0;
+    }
+    if (const hipError_t e = launch(t, part, s); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ckks

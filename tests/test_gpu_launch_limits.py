@@ -62,6 +62,27 @@ def test_experts_in_two_pieces(gpu_lib, d_out, d_in):
 
 
 @gpu
+@pytest.mark.parametrize("d_out,d_in", [(1, 1), (3, 130)])
+def test_experts_in_two_pieces_without_a_list_of_bundles(gpu_lib, d_out, d_in):
+    """A request has the bundle of its own number, in the second piece as well; the last two have none."""
+    import torch
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 16)
+    _, enc = experts_of(ck, ctx, 905, 2, d_out, d_in, 128, 16)
+    count, bundles = 4101, 4099
+    few = residues(ctx, 6, d_in, 2)
+    again = torch.arange(bundles, device="cuda") % 6
+    expert = (torch.arange(count, device="cuda") % 2).to(torch.int32)
+    want = ck.empty_u32((6, d_out, 2, 16, ctx.n))
+    ck.ckks_experts_mac_fp8(ctx, enc, expert[:6].contiguous(), None, few, want, d_out, d_in, 16)
+    out, status = ck.empty_u32((count, d_out, 2, 16, ctx.n)), ints([7] * count)
+    out.fill_(-5)
+    ck.ckks_experts_mac_fp8(ctx, enc, expert, None, few[again], out, d_out, d_in, 16, status)
+    assert not status[:bundles].any() and status[bundles:].tolist() == [1, 1]
+    assert repeats(out[:bundles], want) and bool((out[bundles:] == -5).all())
+
+
+@gpu
 @pytest.mark.parametrize("d_in", [1, 130])
 def test_experts_past_2_32_work_items(gpu_lib, d_in):
     """8 GiB of outputs: 2051 requests of 8 limbs of 2^16 coefficients, one output each."""
