@@ -109,7 +109,8 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(Tables tb, const uint
     case 7: return sum_of<7>(s, req);
     case 8: return sum_of<8>(s, req);
   }
-  // more: the list again for every feature, the gates from the caches
+  // more: the list again for every feature, the gates from the caches (6 bundles of 64 features at 2^13 and 3 limbs: 8 terms
+  // 143 us, 4.8 TB/s, 9 terms 178, 4.3, 16 terms 316, 4.1)
   for (uint32_t j = s.first; j < s.last; ++j)
     for (uint32_t c = 0; c < 2; ++c) {
       const size_t at = j * s.ct_words + c * s.half;

@@ -299,7 +299,7 @@ struct Stage {
 // 2q) first (for h < 0 the sum h + 2q is below 2^31 and h itself, unsigned, above; for h >= 0 h is the smaller), the
 // difference lies in (-q, 2q), and two conditional corrections finish.  The bound holds over kFoldBlocks
 // blocks: per block |a| <= 128 (128 * 128 + 256 (128 * 128 + 112 * 128)) < 1.010e9, |b| <= 128 (128 * 128 + 112 *
-// 128 + 256 (128 * 64 + 112 * 128)) < 0.742e9, |c| <= 128 * 112 * 64 < 0.001e9 times centred scales of at
+// 128 + 256 (128 * 64 + 112 * 128)) < 0.743e9, |c| <= 128 * 112 * 64 < 0.001e9 times centred scales of at
 // most q / 2 is 0.877e9 q, eight of them and a sum carried over from earlier blocks, at most q q / 2 < 0.537e9 q, are
 // 7.56e9 q < 1.77 q 2^32 (and below 2^63).
 __device__ __forceinline__ uint32_t reduce(int64_t t, const Modulus& m) {

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import fp8 as OF
-from test_gpu_fp8 import CODES, MANY, ctx_for, encode as encode_64ths, layer
+from test_gpu_fp8 import MANY, ctx_for, encode as encode_64ths, layer
 from workloads import gen
 
 gpu = pytest.mark.gpu
