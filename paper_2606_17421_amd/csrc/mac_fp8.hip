@@ -156,10 +156,9 @@ __global__ __launch_bounds__(kThreads) void fp8_scale_kernel(Tables tb, const fl
   const uint32_t q = tb.q[l];
   uint32_t r = 0;
   if (row < d_out) {
-    const float s = scales[static_cast<size_t>(row / block_rows) * blocks + block];
-    const double v = static_cast<double>(s) * scale;
+    const double s = scales[static_cast<size_t>(row / block_rows) * blocks + block], v = s * scale;
     // no infinity and no NaN; and a scale too small for `scale`, in its finest unit, takes its block's weights with it
-    const bool fine = fabs(v) < 9223372036854775808.0 && (v == 0 || rint(kUnits ? v / 8 : v) != 0);
+    const bool fine = fabs(v) < 9223372036854775808.0 && (s == 0 || rint(kUnits ? v / 8 : v) != 0);
     if (fine) r = reduce_f64_int(rint(kUnits ? ldexp(v, -out[(idx >> 5) * 96 + (idx & 31)]) : v), q, tb.q_recip[l]);
     if (bad && !fine && l == 0 && row % block_rows == 0) atomicAdd(bad, 1);
   }

@@ -154,6 +154,18 @@ def test_what_is_no_number_is_counted(gpu_lib):
 
 
 @gpu
+@pytest.mark.parametrize("encoder", [encode, encode_64ths])
+def test_scales_that_vanish_in_fp64_are_counted(gpu_lib, encoder):
+    """1e-30 * 1e-300 is zero in fp64 already, before anything is rounded; a zero times it is no loss."""
+    ck = gpu_lib
+    ctx = ctx_for(ck, 10, 1)
+    codes, _ = layer(855, 5, 300)
+    bad = ints([0])
+    encoder(ck, ctx, codes, np.array([[1e-30, 0.0, -1e-40]], np.float32), 128, 1, 1e-300, bad)
+    assert int(bad) == 2
+
+
+@gpu
 def test_experts_on_another_stream_and_in_a_graph(gpu_lib):
     """Two experts, one of each encoding, from weights at an odd address."""
     import torch
